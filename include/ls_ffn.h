@@ -42,7 +42,7 @@ typedef enum {
     LS_E_CAPACITY = 6     /* request larger than the HBM block cache */
 } ls_status;
 
-typedef enum { LS_F32 = 0, LS_F16 = 1, LS_BF16 = 2 } ls_dtype;
+typedef enum { LS_F32 = 0, LS_F16 = 1, LS_BF16 = 2, LS_I8 = 3 /* inputs of ls_linear_i8 (ls_ops.h) only */ } ls_dtype;
 
 /* Gating of the gate branch (Eq. 1, Sec. 2.1):
  *  REGLU:          a_j = max(g_j, 0) * u_j

@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liblsffn.so")
-SOURCES = ["ls_api.hip", "ls_kernels.hip", "ls_decode.hip", "ls_mfma.hip", "ls_hash.hip", "ls_stage.hip"]
+SOURCES = ["ls_api.hip", "ls_kernels.hip", "ls_decode.hip", "ls_mfma.hip", "ls_hash.hip", "ls_stage.hip",
+           "ls_ops_api.hip", "ls_rows.hip", "ls_linear.hip", "ls_attend.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -24,11 +25,11 @@ ROOT = os.path.dirname(HERE)
 
 
 def source_digest() -> str:
-    """sha256 over the library's sources (every file in csrc/, the public header and this
+    """sha256 over the library's sources (every file in csrc/, the public headers and this
     build script), each as its path relative to the repository and its bytes, in path order."""
     files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)
              if f.endswith((".hip", ".h", ".cpp"))]
-    files += [os.path.join(ROOT, "include", "ls_ffn.h"), os.path.abspath(__file__)]
+    files += [os.path.join(ROOT, "include", h) for h in ("ls_ffn.h", "ls_ops.h")] + [os.path.abspath(__file__)]
     h = hashlib.sha256()
     for path in sorted(files, key=lambda p: os.path.relpath(p, ROOT)):
         h.update(os.path.relpath(path, ROOT).encode() + b"\0")

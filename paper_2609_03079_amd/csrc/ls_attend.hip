@@ -1,0 +1,563 @@
+// ls_attend.hip - attention of a batch that shares a prefix, over a paged cache.
+//
+//   o_r = sum_j p_rj v_j,   p_rj = exp(scale q_r k_j - m_r) / l_r,   r a query row of one key/value head
+//
+// The prefix's keys serve the rows of every sequence at once (n_seqs n_q G rows per key/value head,
+// G query heads sharing it), a sequence's own keys its n_q G rows.  Both are cut along the keys
+// into parts; each part keeps the running maximum m, sum l and sum of weighted values of its rows
+// (one pass over the keys), and a second kernel joins the parts of a row.
+//
+// The products run transposed, S^T = K Q^T and O^T = V^T P^T, on the 32 x 32 x 16 matrix
+// instructions: a lane then holds one query row's scores, 16 of each 32 keys, so the softmax
+// needs one exchange with the lane that holds the other 16, and the scores become the second
+// product's operand in place: both products may take the keys in any order as long as it is the
+// same, and the values are read from shared memory (transposed on the way) in the order in which
+// the scores lie.
+//
+// Two shapes of workgroup (128 x 64 keys at a time is compute-bound, 32 rows are memory-bound):
+//  - wide: four waves of 32 rows share 64 keys in shared memory;
+//  - narrow (up to 32 rows): each wave takes every fourth 32 keys through its own share of
+//    shared memory, without barriers, and the waves' results are joined at the end.
+// In both the next keys are copied straight to shared memory while the present ones are used.
+#include <algorithm>
+#include <type_traits>
+
+#include "ls_device.h"
+#include "ls_ops_internal.h"
+
+namespace ls {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(1))) void* gptr;
+typedef __attribute__((address_space(3))) void* lptr;
+
+// What masked keys and the padding of a head are read from.
+__device__ const uint32_t g_zero_chunk[4] = {0, 0, 0, 0};
+
+template <typename T>
+using vec8 = std::conditional_t<std::is_same_v<T, _Float16>, f16x8, bf16x8>;
+
+__device__ inline f32x16 mma(const f16x8& a, const f16x8& b, const f32x16& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x16 mma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+struct AttendP {
+    const void* q;
+    int64_t q_token, q_head;
+    void* out;
+    int64_t o_token, o_head;
+    const void* k;
+    const void* v;
+    int64_t page_stride, head_stride, token_stride;
+    int n_pages, page_shift;
+    const int32_t* prefix_pages;
+    const int32_t* pages;
+    int64_t pages_stride;
+    const int32_t* lens;
+    int prefix_len, max_len;
+    int S, n_q, H, KV, G, D;
+    float c;                 // scale log2(e): the softmax runs in powers of two
+    AttendPlan plan;
+    int pre_items, suf_items;  // workgroups of this launch
+    int parts;               // partial results per row
+    bool direct;             // a row has one part, which is the result
+    float* part;             // [rows][parts][D]
+    float* ml;               // [rows][parts][2]
+};
+
+// Chunks (8 elements, 16 bytes) of a row lie at places permuted by its number, so that neither
+// 16 rows at one chunk (keys) nor 4 rows at 4 chunks (values) meet in a bank.
+template <int CPR>
+__device__ inline int swz(int row) {
+    return CPR == 8 ? (((row >> 1) & 1) << 2) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
+}
+
+template <typename T, int DP, bool WIDE>
+struct Shape {
+    static constexpr int NW = WIDE || DP < 256 ? 4 : 2;         // waves
+    static constexpr int KT = WIDE && DP < 256 ? 64 : 32;       // keys at a time
+    static constexpr int CPR = DP / 8;                          // chunks per row
+    static constexpr int RPI = 64 / CPR;                        // rows per copy instruction
+    static constexpr int kRows = WIDE ? KT / NW : KT;           // rows a wave copies
+    static constexpr int kBuf = (WIDE ? 1 : NW) * KT * DP * 2;  // elements of a buffer: keys, then values
+    static constexpr int kTileRows = WIDE ? 128 : 32;
+};
+
+// What a workgroup works on.
+struct Item {
+    const int32_t* table;  // page ids
+    int begin, end;        // keys
+    int kv;                // key/value head
+    int row0, rows;        // first row of its tile, rows of all tiles
+    int seq;               // -1: the prefix
+    int part;              // its place among a row's parts
+    int len;               // the sequence's keys
+};
+
+template <typename T, int DP, bool WIDE>
+__device__ inline bool item_of(const AttendP& p, int b, Item* it) {
+    constexpr int R = Shape<T, DP, WIDE>::kTileRows;
+    if (b < p.pre_items) {
+        it->row0 = b % p.plan.pre_tiles * R;
+        b /= p.plan.pre_tiles;
+        it->kv = b % p.KV;
+        it->part = b / p.KV;
+        it->seq = -1;
+        it->table = p.prefix_pages;
+        it->len = p.prefix_len;
+        it->begin = it->part * p.plan.pre_chunk;
+        it->end = min(p.prefix_len, it->begin + p.plan.pre_chunk);
+        it->rows = p.S * p.n_q * p.G;
+        return true;
+    }
+    b -= p.pre_items;
+    it->row0 = b % p.plan.suf_tiles * R;
+    b /= p.plan.suf_tiles;
+    it->kv = b % p.KV;
+    b /= p.KV;
+    it->seq = b % p.S;
+    const int j = b / p.S;
+    it->table = p.pages + it->seq * p.pages_stride;
+    it->len = min(p.lens[it->seq], p.max_len);
+    it->begin = j * p.plan.suf_chunk;
+    it->end = min(it->len, it->begin + p.plan.suf_chunk);
+    it->rows = p.n_q * p.G;
+    it->part = p.plan.pre_parts + j;
+    return it->begin < it->end || p.direct;
+}
+
+template <typename T, int DP, bool WIDE>
+__global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 ? 2 : 1)) void attend_kernel(const AttendP p) {
+    using Sh = Shape<T, DP, WIDE>;
+    constexpr int NW = Sh::NW, KT = Sh::KT, CPR = Sh::CPR, NF = DP / 16, ND = DP / 32, SUB = KT / 32;
+    // two arrays, not one: a read of one buffer must not wait for the copy into the other
+    __shared__ __attribute__((aligned(16))) T buf0[Sh::kBuf];
+    __shared__ __attribute__((aligned(16))) T buf1[Sh::kBuf];
+    __shared__ float wave_ml[NW][2][32];
+    __shared__ float row_sum[32];
+    Item it;
+    if (!item_of<T, DP, WIDE>(p, blockIdx.x, &it)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, h = lane >> 5;
+
+    // this lane's query row: token and head of it, keys it sees
+    const int row = it.row0 + (WIDE ? wave * 32 : 0) + n;
+    const bool row_ok = row < it.rows;
+    const int rr = row_ok ? row : it.rows - 1;
+    const int g = rr % p.G, tk = rr / p.G;  // token of the batch (prefix) or of the sequence
+    const int64_t token = it.seq < 0 ? tk : (int64_t)it.seq * p.n_q + tk;
+    const int head = it.kv * p.G + g;
+    const int limit = it.seq < 0 ? it.end : min(it.end, it.len - p.n_q + 1 + tk);
+    const int full = it.seq < 0 ? it.end : it.len - p.n_q + 1;  // keys below are seen by every row
+
+    vec8<T> q[NF];
+    {
+        const T* src = static_cast<const T*>(p.q) + token * p.q_token + head * p.q_head;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            const int d = f * 16 + h * 8;
+            q[f] = row_ok && d < p.D ? *reinterpret_cast<const vec8<T>*>(src + d) : vec8<T>{};
+        }
+    }
+    f32x16 o[ND];
+#pragma unroll
+    for (auto& x : o) x = f32x16{};
+    float m = -INFINITY, l = 0.f;
+
+    const T* kbase = static_cast<const T*>(p.k) + it.kv * p.head_stride;
+    const T* vbase = static_cast<const T*>(p.v) + it.kv * p.head_stride;
+    const T* zero = reinterpret_cast<const T*>(g_zero_chunk);
+    const int page_mask = (1 << p.page_shift) - 1;
+
+    // page of key (tile + lane), -1 where there is none
+    auto page_ids = [&](int key0) {
+        const int key = key0 + (lane & (KT - 1));
+        int id = -1;
+        if (key < it.end) id = it.table[key >> p.page_shift];
+        return (unsigned)id < (unsigned)p.n_pages ? id : -1;
+    };
+    auto copy = [&](int key0, int ids, T* buf) {
+        T* kd = buf + (WIDE ? wave * Sh::kRows * DP : wave * KT * DP * 2);
+        T* vd = kd + KT * DP;
+#pragma unroll
+        for (int i = 0; i < Sh::kRows / Sh::RPI; ++i) {
+            const int r = (WIDE ? wave * Sh::kRows : 0) + i * Sh::RPI + lane / CPR;
+            const int chunk = (lane % CPR) ^ swz<CPR>(r);
+            const int id = __shfl(ids, r, 64);
+            const bool ok = id >= 0 && chunk * 8 < p.D;
+            const int64_t at = (int64_t)max(id, 0) * p.page_stride + (int64_t)((key0 + r) & page_mask) * p.token_stride + chunk * 8;
+            __builtin_amdgcn_global_load_lds((gptr)(ok ? kbase + at : zero), (lptr)(kd + i * 512), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((gptr)(ok ? vbase + at : zero), (lptr)(vd + i * 512), 16, 0, 0);
+        }
+    };
+    auto use = [&](int key0, int ids, const T* buf) {
+        if (WIDE && it.row0 + wave * 32 >= it.rows) return;  // no rows: this wave only copies
+        const T* kt = buf + (WIDE ? 0 : wave * KT * DP * 2);
+        const T* vt = kt + KT * DP;
+        f32x16 s[SUB];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            s[u] = f32x16{};
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                const auto k = *reinterpret_cast<const vec8<T>*>(kt + (u * 32 + n) * DP + (((2 * f + h) ^ swz<CPR>(n)) * 8));
+                s[u] = mma(k, q[f], s[u]);
+            }
+        }
+        // score i of a lane belongs to key 8 (i / 4) + 4 h + i % 4 of its 32
+        const uint64_t valid = __ballot(ids >= 0);
+        const bool whole = key0 + KT <= full && key0 + KT <= it.end && (KT == 64 ? ~valid == 0 : (uint32_t)~valid == 0);
+        if (!whole) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = u * 32 + 8 * (i / 4) + 4 * h + i % 4;
+                    if (key0 + key >= limit || !((valid >> key) & 1)) s[u][i] = -INFINITY;
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float next = fmaxf(m, top), base = next == -INFINITY ? 0.f : next * p.c;
+        if (__any(next > m)) {
+            const float scale = __builtin_amdgcn_exp2f(m * p.c - base);  // m = -inf: 0
+            l *= scale;
+#pragma unroll
+            for (auto& x : o) x *= scale;
+            m = next;
+        }
+        vec8<T> pr[2 * SUB];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[u][i], p.c, -base));
+                l += e;
+                pr[2 * u + i / 8][i % 8] = (T)e;
+            }
+        // values: lane -> element d = 32 t + n, keys 16 kk + 8 (j / 4) + 4 h + j % 4
+        auto value = [&](int kk, int t) {
+            const int r4 = (lane & 15) >> 2, col = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), byte = (lane & 1) * 4;
+            const int r0 = 16 * kk + 4 * h + r4, r1 = r0 + 8;
+            typedef __attribute__((address_space(3))) s16x4* lds4;
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vt + r0 * DP + ((t * 4 + col) ^ swz<CPR>(r0)) * 8 + byte));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vt + r1 * DP + ((t * 4 + col) ^ swz<CPR>(r1)) * 8 + byte));
+            struct { s16x4 a, b; } both{x, y};
+            return __builtin_bit_cast(vec8<T>, both);
+        };
+        // Where later tokens of a sequence see keys that earlier ones do not, a weight of zero must
+        // also keep out a value that is no number: only then are the tokens taken one by one.
+        if (it.seq >= 0 && p.n_q > 1 && key0 + KT > full) {
+            bool odd = false;
+#pragma unroll 1
+            for (int kk = 0; kk < 2 * SUB; ++kk)
+#pragma unroll 1
+                for (int t = 0; t < ND; ++t) {
+                    const auto v = value(kk, t);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        odd |= key0 + 16 * kk + 8 * (j / 4) + 4 * h + j % 4 >= full && !(fabsf((float)v[j]) < INFINITY);
+                }
+            if (__any(odd)) {
+#pragma unroll 1
+                for (int i = 0; i < p.n_q; ++i) {
+                    const int seen = full + i;
+#pragma unroll
+                    for (int t = 0; t < ND; ++t) {
+                        f32x16 x = o[t];
+#pragma unroll
+                        for (int kk = 0; kk < 2 * SUB; ++kk) {
+                            auto v = value(kk, t);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (key0 + 16 * kk + 8 * (j / 4) + 4 * h + j % 4 >= seen) v[j] = (T)0.f;
+                            x = mma(v, pr[kk], x);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[t][e] = tk == i ? x[e] : o[t][e];
+                    }
+                }
+                return;
+            }
+        }
+#pragma unroll
+        for (int kk = 0; kk < 2 * SUB; ++kk)
+#pragma unroll
+            for (int t = 0; t < ND; ++t) o[t] = mma(value(kk, t), pr[kk], o[t]);
+    };
+    auto landed = [&] {
+        __builtin_amdgcn_s_waitcnt(0x0070);  // this wave's copies are in shared memory, its reads done
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+        if (WIDE) __builtin_amdgcn_s_barrier();
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    };
+
+    constexpr int kStep = WIDE ? KT : NW * KT;
+    int key = it.begin + (WIDE ? 0 : wave * KT);
+    int ids = page_ids(key), ids1 = page_ids(key + kStep);
+    if (key < it.end) copy(key, ids, buf0);
+    while (key < it.end) {
+        landed();
+        if (key + kStep < it.end) copy(key + kStep, ids1, buf1);
+        int ids2 = page_ids(key + 2 * kStep);
+        use(key, ids, buf0);
+        key += kStep;
+        ids = ids1;
+        ids1 = ids2;
+        if (key >= it.end) break;
+        landed();
+        if (key + kStep < it.end) copy(key + kStep, ids1, buf0);
+        ids2 = page_ids(key + 2 * kStep);
+        use(key, ids, buf1);
+        key += kStep;
+        ids = ids1;
+        ids1 = ids2;
+    }
+    l += __shfl_xor(l, 32, 64);
+
+    const int64_t out_row = token * p.H + head;
+    // four elements of a row: the part's sums, or with a single part the result
+    auto put = [&](int64_t token_, int head_, int d, f32x4 x, float row_l) {
+        if (d >= p.D) return;
+        if (p.direct) {
+            const float inv = row_l == 0.f ? 0.f : 1.f / row_l;
+            Pack<T, 4> v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v.e[i] = (T)(x[i] * inv);
+            store_pack<T, 4>(p.out, token_ * p.o_token + head_ * p.o_head + d, v);
+        } else {
+            *reinterpret_cast<f32x4*>(p.part + ((token_ * p.H + head_) * p.parts + it.part) * p.D + d) = x;
+        }
+    };
+    auto put_ml = [&](float row_m, float row_l) {
+        if (p.direct) return;
+        float* at = p.ml + (out_row * p.parts + it.part) * 2;
+        at[0] = row_m;
+        at[1] = row_l;
+    };
+    if (WIDE) {
+        if (!row_ok) return;
+#pragma unroll
+        for (int t = 0; t < ND; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                f32x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = l == 0.f ? 0.f : o[t][i + e];
+                put(token, head, t * 32 + 2 * i + 4 * h, x, l);
+            }
+        if (h == 0) put_ml(m, l);
+        return;
+    }
+    // narrow: join the waves
+    if (h == 0) {
+        wave_ml[wave][0][n] = m;
+        wave_ml[wave][1][n] = l;
+    }
+    __syncthreads();  // also: every wave is done with its buffers
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, wave_ml[w][0][n]);
+    const float base = top == -INFINITY ? 0.f : top * p.c;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const float wl = wave_ml[w][1][n];
+        if (wl != 0.f) sum += wl * __builtin_amdgcn_exp2f(fmaf(wave_ml[w][0][n], p.c, -base));
+    }
+    float* joined = reinterpret_cast<float*>(buf0);  // [wave][row][DP], 16-byte chunks permuted by the row
+    static_assert(WIDE || sizeof(buf0) >= NW * 32 * DP * 4, "room for the waves' sums");
+    if (row_ok) {
+        const float scale = __builtin_amdgcn_exp2f(fmaf(m, p.c, -base));
+#pragma unroll
+        for (int t = 0; t < ND; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int chunk = t * 8 + i / 2 + h;
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : o[t][i + e] * scale;
+                *reinterpret_cast<f32x4*>(joined + (wave * 32 + n) * DP + (chunk ^ (n & (DP / 4 - 1))) * 4) = v;
+            }
+        if (wave == 0 && h == 0) {
+            row_sum[n] = sum;
+            put_ml(top, sum);
+        }
+    }
+    __syncthreads();
+    const int here = min(32, it.rows - it.row0);
+    for (int i = threadIdx.x; i < here * (DP / 4); i += NW * 64) {
+        const int r = i / (DP / 4), chunk = i % (DP / 4);
+        f32x4 v{};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) v += *reinterpret_cast<const f32x4*>(joined + (w * 32 + r) * DP + (chunk ^ (r & (DP / 4 - 1))) * 4);
+        const int tr = (it.row0 + r) / p.G;
+        put(it.seq < 0 ? tr : (int64_t)it.seq * p.n_q + tr, it.kv * p.G + (it.row0 + r) % p.G, chunk * 4, v, row_sum[r]);
+    }
+}
+
+// Joins the parts of a row: a wave per row, DP / 4 lanes across its elements and the other
+// lanes on other parts.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void join_kernel(const AttendP p) {
+    constexpr int L = DP / 4, GR = 64 / L;
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = (int64_t)p.S * p.n_q * p.H, r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= rows) return;
+    const int64_t token = r / p.H;
+    const int len = min(p.lens[token / p.n_q], p.max_len);
+    // parts that were written: the prefix's unless the slot is idle, and the sequence's that hold keys
+    const int first = len < 0 ? p.plan.pre_parts : 0;
+    const int last = p.plan.pre_parts + (len > 0 ? (len + p.plan.suf_chunk - 1) / p.plan.suf_chunk : 0);
+    const float* ml = p.ml + r * p.parts * 2;
+    float m[2], l[2], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int j = first + i * 64 + lane;
+        m[i] = j < last ? ml[j * 2] : -INFINITY;
+        l[i] = j < last ? ml[j * 2 + 1] : 0.f;
+        top = fmaxf(top, m[i]);
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    const float base = top == -INFINITY ? 0.f : top * p.c;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        m[i] = l[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(fmaf(m[i], p.c, -base));  // now its weight
+        sum += l[i] * m[i];
+    }
+    sum = wave_sum(sum);
+    const int d = (lane % L) * 4, g = lane / L;
+    f32x4 acc{};
+    for (int j0 = first; j0 < last; j0 += GR) {
+        const int j = j0 + g, at = j - first;
+        const float w = __shfl(at < 64 ? m[0] : m[1], at & 63, 64);
+        if (j < last && d < p.D && w != 0.f)
+            acc += *reinterpret_cast<const f32x4*>(p.part + (r * p.parts + j) * p.D + d) * w;
+    }
+#pragma unroll
+    for (int off = L; off < 64; off <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], off, 64);
+    if (g == 0 && d < p.D) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        Pack<T, 4> v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v.e[e] = (T)(acc[e] * inv);
+        store_pack<T, 4>(p.out, token * p.o_token + (r - token * p.H) * p.o_head + d, v);
+    }
+}
+
+template <typename T, int DP>
+hipError_t attend_type(const ls_kv_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws, hipStream_t st) {
+    AttendP p{};
+    p.q = a.q, p.q_token = a.q_token_stride, p.q_head = a.q_head_stride;
+    p.out = a.out, p.o_token = a.out_token_stride, p.o_head = a.out_head_stride;
+    p.k = c.k, p.v = c.v;
+    p.page_stride = c.page_stride, p.head_stride = c.head_stride, p.token_stride = c.token_stride;
+    p.n_pages = c.n_pages, p.page_shift = __builtin_ctz(c.page_size);
+    p.prefix_pages = a.prefix_pages, p.pages = a.pages, p.pages_stride = a.pages_stride, p.lens = a.lens;
+    p.prefix_len = a.prefix_len, p.max_len = a.max_len;
+    p.S = a.n_seqs, p.n_q = a.n_q, p.H = a.n_heads, p.KV = c.n_kv_heads, p.G = a.n_heads / c.n_kv_heads, p.D = c.head_dim;
+    p.c = a.scale * 1.44269504f;
+    p.plan = plan;
+    p.parts = plan.pre_parts + plan.suf_parts;
+    p.direct = plan.pre_parts == 0 && plan.suf_parts == 1;
+    const int64_t rows = (int64_t)p.S * p.n_q * p.H;
+    p.part = static_cast<float*>(ws);
+    p.ml = p.part + rows * p.parts * p.D;
+    const int pre = plan.pre_parts * p.KV * plan.pre_tiles, suf = plan.suf_parts * p.S * p.KV * plan.suf_tiles;
+    auto go = [&](bool wide, int pre_items, int suf_items) {
+        p.pre_items = pre_items;
+        p.suf_items = suf_items;
+        if (pre_items + suf_items == 0) return hipSuccess;
+        const dim3 grid((unsigned)(pre_items + suf_items));
+        if (wide)
+            hipLaunchKernelGGL((attend_kernel<T, DP, true>), grid, dim3(Shape<T, DP, true>::NW * 64), 0, st, p);
+        else
+            hipLaunchKernelGGL((attend_kernel<T, DP, false>), grid, dim3(Shape<T, DP, false>::NW * 64), 0, st, p);
+        return hipGetLastError();
+    };
+    hipError_t e;
+    if (plan.pre_parts == 0 || plan.pre_wide == plan.suf_wide || suf == 0) {
+        e = go(pre ? plan.pre_wide : plan.suf_wide, pre, suf);
+    } else {
+        e = go(plan.pre_wide, pre, 0);
+        if (e == hipSuccess) e = go(plan.suf_wide, 0, suf);
+    }
+    if (e != hipSuccess || p.direct) return e;
+    hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t attend_dim(const ls_kv_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws, hipStream_t st) {
+    if (c.head_dim <= 64) return attend_type<T, 64>(c, a, plan, ws, st);
+    if (c.head_dim <= 128) return attend_type<T, 128>(c, a, plan, ws, st);
+    return attend_type<T, 256>(c, a, plan, ws, st);
+}
+
+}  // namespace
+
+bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan) {
+    const int G = a.n_heads / c.n_kv_heads;
+    const int64_t pre_rows = (int64_t)a.n_seqs * a.n_q * G, suf_rows = (int64_t)a.n_q * G;
+    const int64_t part_bytes = (int64_t)a.n_seqs * a.n_q * a.n_heads * (c.head_dim + 2) * 4;
+    plan->pre_wide = pre_rows > 32;
+    plan->suf_wide = suf_rows > 32;
+    plan->pre_tiles = (int)ceil_div(pre_rows, plan->pre_wide ? 128 : 32);
+    plan->suf_tiles = (int)ceil_div(suf_rows, plan->suf_wide ? 128 : 32);
+    // Workgroups that run at once (by shared memory), and what a workgroup costs beyond its keys (the
+    // chain of loads before its first product, and the join), in keys.
+    auto slots = [&](bool wide) { return n_cu * (wide || c.head_dim <= 64 ? 2 : 1); };
+    constexpr int kStart = 192;
+    // The chunk (a multiple of 128 keys) with the least rounds x (chunk + start), at most half of
+    // kMaxParts parts and half of the workspace for each of prefix and sequences.
+    auto choose = [&](int64_t n_pre, int64_t pre_keys, int64_t n_suf, int64_t suf_keys, int n_slots) {
+        int64_t best = 0;
+        double least = 0;
+        const int64_t most = round_up((size_t)std::max<int64_t>(std::max(pre_keys, suf_keys), 1), 128);
+        for (int64_t chunk = 128;; chunk = std::min(most, chunk + std::max<int64_t>(128, chunk / 8 / 128 * 128))) {
+            const int64_t pp = ceil_div(pre_keys, chunk), sp = ceil_div(suf_keys, chunk);
+            const bool fits = pp <= kMaxParts / 2 && sp <= kMaxParts / 2 && std::max(pp, sp) * part_bytes <= (int64_t)ws_bytes / 2 &&
+                              n_pre * pp + n_suf * sp < (int64_t)1 << 31;
+            if (fits) {
+                const double t = (double)ceil_div(n_pre * pp + n_suf * sp, n_slots) * (chunk + kStart);
+                if (!best || t < least) best = chunk, least = t;
+            }
+            if (chunk >= most) break;
+        }
+        return (int)best;
+    };
+    const int64_t n_pre = a.prefix_len ? (int64_t)c.n_kv_heads * plan->pre_tiles : 0;
+    const int64_t n_suf = (int64_t)a.n_seqs * c.n_kv_heads * plan->suf_tiles;
+    if (plan->pre_wide == plan->suf_wide || !a.prefix_len) {
+        plan->pre_chunk = plan->suf_chunk = choose(n_pre, a.prefix_len, n_suf, a.max_len, slots(plan->suf_wide));
+    } else {
+        plan->pre_chunk = choose(n_pre, a.prefix_len, 0, 0, slots(plan->pre_wide));
+        plan->suf_chunk = choose(0, 0, n_suf, a.max_len, slots(plan->suf_wide));
+    }
+    if (!plan->pre_chunk || !plan->suf_chunk) return false;
+    plan->pre_parts = (int)ceil_div(a.prefix_len, plan->pre_chunk);
+    plan->suf_parts = (int)ceil_div(a.max_len, plan->suf_chunk);
+    if (plan->pre_parts + plan->suf_parts == 0) plan->suf_parts = 1;  // no key anywhere: rows of zeros
+    plan->bytes = (size_t)((plan->pre_parts + plan->suf_parts) * part_bytes);
+    return true;
+}
+
+hipError_t launch_attend(const ls_kv_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws, hipStream_t st) {
+    return c.dtype == LS_F16 ? attend_dim<_Float16>(c, a, plan, ws, st) : attend_dim<__bf16>(c, a, plan, ws, st);
+}
+
+}  // namespace ls

@@ -1,0 +1,270 @@
+// ls_rows.hip - operators that touch every element of a token's rows once: the norms around a
+// block with its gated residual update, and the append of rotated keys and values to a paged cache.
+//
+// Both are bound by HBM (or, for a handful of tokens, by the latency of one pass of loads): a
+// row is read into registers once, everything is computed there in fp32, and the result is
+// written once.
+#include <algorithm>
+
+#include "ls_device.h"
+#include "ls_ops_internal.h"
+
+namespace ls {
+namespace {
+
+// ---- norms ---------------------------------------------------------------------------------
+// Sum over NT threads in a fixed order: lanes of a wave, then the waves in order.
+template <int NT>
+__device__ inline float row_sum(float v, float* part) {
+    v = wave_sum_dpp(v);
+    if (NT == 64) return v;
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) s += part[w];
+    return s;
+}
+
+// One workgroup per token; thread t holds the V-element vectors t, t + NT, ... (C of them) of the
+// row.  All loads are issued before the first sum, so a single token costs one memory round trip
+// and two sums.
+template <typename T, int V, int C, int NT>
+__global__ __launch_bounds__(NT) void norm_kernel(const ls_norm_args p) {
+    __shared__ float part[2][NT / 64];
+    const int64_t row = blockIdx.x;
+    float x[C][V];
+    Pack<T, V> y[C], g[C], wp[C], wh[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int e = ((int)threadIdx.x + NT * c) * V;
+        if (e >= p.d) continue;
+        if (p.y) y[c] = load_pack<T, V>(p.y, row * p.y_stride + e);
+        const auto xv = load_pack<float, V>(p.x, row * p.x_stride + e);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[c][i] = xv.e[i];
+        if (p.y && p.gate) g[c] = load_pack<T, V>(p.gate, row * p.gate_stride + e);
+        if (p.y && p.post_weight) wp[c] = load_pack<T, V>(p.post_weight, e);
+        if (p.h && p.pre_weight) wh[c] = load_pack<T, V>(p.pre_weight, e);
+    }
+    float post = 1.f;
+    if (p.y && p.post_norm) {
+        float ss = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (((int)threadIdx.x + NT * c) * V >= p.d) continue;
+#pragma unroll
+            for (int i = 0; i < V; ++i) ss = fmaf((float)y[c].e[i], (float)y[c].e[i], ss);
+        }
+        post = 1.f / sqrtf(row_sum<NT>(ss, part[0]) / (float)p.d + p.eps);
+    }
+    float ss = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int e = ((int)threadIdx.x + NT * c) * V;
+        if (e >= p.d) continue;
+        Pack<float, V> o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float v = p.x_scale * x[c][i];
+            if (p.y) {
+                float t = (float)y[c].e[i] * post;
+                if (p.post_weight) t *= (float)wp[c].e[i];
+                if (p.gate) t *= (float)g[c].e[i];
+                v = fmaf(p.y_scale, t, v);
+            }
+            x[c][i] = o.e[i] = v;
+            ss = fmaf(v, v, ss);
+        }
+        if (p.x_out) store_pack<float, V>(p.x_out, row * p.x_out_stride + e, o);
+    }
+    if (!p.h) return;
+    const float pre = p.pre_norm ? 1.f / sqrtf(row_sum<NT>(ss, part[1]) / (float)p.d + p.eps) : 1.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int e = ((int)threadIdx.x + NT * c) * V;
+        if (e >= p.d) continue;
+        Pack<T, V> o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float v = x[c][i] * pre;
+            if (p.pre_weight) v *= (float)wh[c].e[i];
+            o.e[i] = (T)v;
+        }
+        store_pack<T, V>(p.h, row * p.h_stride + e, o);
+    }
+}
+
+template <typename T, int V, int C, int NT>
+hipError_t norm_launch(const ls_norm_args& a, hipStream_t st) {
+    hipLaunchKernelGGL((norm_kernel<T, V, C, NT>), dim3(a.n_tokens), dim3(NT), 0, st, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t norm_type(const ls_norm_args& a, int n_cu, hipStream_t st) {
+    const size_t es = sizeof(T);
+    auto row_ok = [&](const void* p, int64_t stride, size_t size) {
+        return !p || (aligned(p, 16) && stride * size % 16 == 0);
+    };
+    const bool vec = a.d % 8 == 0 && row_ok(a.x, a.x_stride, 4) && row_ok(a.x_out, a.x_out_stride, 4) &&
+                     row_ok(a.y, a.y_stride, es) && row_ok(a.gate, a.gate_stride, es) &&
+                     row_ok(a.h, a.h_stride, es) && row_ok(a.post_weight, 0, es) && row_ok(a.pre_weight, 0, es);
+    if (!vec) {  // odd lengths or alignments: one element per access
+        if (a.d <= 1024) return norm_launch<T, 1, 4, 256>(a, st);
+        if (a.d <= 8192) return norm_launch<T, 1, 8, 1024>(a, st);
+        return norm_launch<T, 1, 32, 1024>(a, st);
+    }
+    const int units = a.d / 8;
+    // few tokens: one vector per thread, for the shortest chain; many: fewer, fuller waves
+    const bool few = a.n_tokens < n_cu;
+    if (units <= 64) return norm_launch<T, 8, 1, 64>(a, st);
+    if (units <= 128) return norm_launch<T, 8, 1, 128>(a, st);
+    if (units <= 256) return norm_launch<T, 8, 1, 256>(a, st);
+    if (units <= 512) return few ? norm_launch<T, 8, 1, 512>(a, st) : norm_launch<T, 8, 2, 256>(a, st);
+    if (units <= 1024) return few ? norm_launch<T, 8, 1, 1024>(a, st) : norm_launch<T, 8, 4, 256>(a, st);
+    return norm_launch<T, 8, 4, 1024>(a, st);
+}
+
+// ---- append --------------------------------------------------------------------------------
+struct AppendP {
+    ls_kv_cache c;
+    ls_append_args a;
+    int rot_units, units, v_units;  // vectors of a key or query head that turn, all of them, of a value head
+};
+
+// A thread moves one vector of one head at a time: V pairs that turn (or V / 2 of neighbours), or
+// V elements that are copied.  The vectors of a token's query, key and value heads follow each
+// other; blockIdx.x is the token, blockIdx.y a share of its vectors.
+template <typename T, int V, bool PAIR>
+__global__ __launch_bounds__(256) void append_kernel(const AppendP p) {
+    const ls_append_args& a = p.a;
+    const ls_kv_cache& c = p.c;
+    const int64_t t = blockIdx.x;
+    int pos = 0;
+    if (a.rot_dim) {
+        pos = a.positions[t];
+        if (pos < 0 || pos >= a.n_pos) return;
+    }
+    const int slot = a.slots[t];
+    const bool keep = slot >= 0 && slot < c.n_pages * c.page_size;
+    const int64_t to = keep ? (int64_t)(slot / c.page_size) * c.page_stride + (int64_t)(slot % c.page_size) * c.token_stride : 0;
+    const int qk_heads = a.n_heads + c.n_kv_heads, half = a.rot_dim / 2;
+    const int qk_total = qk_heads * p.units, total = qk_total + (keep ? c.n_kv_heads * p.v_units : 0);
+    const float* cs = a.cos_sin + (int64_t)pos * a.rot_dim;
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < total; i += 256 * gridDim.y) {
+        if (i >= qk_total) {
+            const int j = i - qk_total, h = j / p.v_units, e = (j - h * p.v_units) * V;
+            store_pack<T, V>(c.v, to + h * c.head_stride + e,
+                             load_pack<T, V>(a.v, t * a.v_token_stride + h * a.v_head_stride + e));
+            continue;
+        }
+        const int r = i / p.units, u = i - r * p.units;
+        const bool is_q = r < a.n_heads;
+        if (!is_q && !keep) continue;
+        const int h = is_q ? r : r - a.n_heads;
+        const void* src = is_q ? a.q : a.k;
+        void* dst = is_q ? a.q_out : c.k;
+        const int64_t from = is_q ? t * a.q_token_stride + h * a.q_head_stride : t * a.k_token_stride + h * a.k_head_stride;
+        const int64_t at = is_q ? t * a.q_out_token_stride + h * a.q_out_head_stride : to + h * c.head_stride;
+        if (u >= p.rot_units) {
+            const int e = a.rot_dim + (u - p.rot_units) * V;
+            store_pack<T, V>(dst, at + e, load_pack<T, V>(src, from + e));
+        } else if (!PAIR) {
+            const int e = u * V;
+            auto x = load_pack<T, V>(src, from + e), y = load_pack<T, V>(src, from + half + e);
+            const auto co = load_pack<float, V>(cs, e), si = load_pack<float, V>(cs, half + e);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float l = (float)x.e[k], m = (float)y.e[k];
+                x.e[k] = (T)(l * co.e[k] - m * si.e[k]);
+                y.e[k] = (T)(m * co.e[k] + l * si.e[k]);
+            }
+            store_pack<T, V>(dst, at + e, x);
+            store_pack<T, V>(dst, at + half + e, y);
+        } else {
+            constexpr int W = V < 2 ? 2 : V;  // elements of a unit; single ones go one by one
+            const int e = u * W;
+            T x[W];
+            if (V < 2) {
+                x[0] = static_cast<const T*>(src)[from + e];
+                x[1] = static_cast<const T*>(src)[from + e + 1];
+            } else {
+                const auto v = load_pack<T, W>(src, from + e);
+#pragma unroll
+                for (int k = 0; k < W; ++k) x[k] = v.e[k];
+            }
+            const auto co = load_pack<float, W / 2>(cs, e / 2), si = load_pack<float, W / 2>(cs, half + e / 2);
+            Pack<T, W> o;
+#pragma unroll
+            for (int k = 0; k < W / 2; ++k) {
+                const float l = (float)x[2 * k], m = (float)x[2 * k + 1];
+                o.e[2 * k] = (T)(l * co.e[k] - m * si.e[k]);
+                o.e[2 * k + 1] = (T)(m * co.e[k] + l * si.e[k]);
+            }
+            if (V < 2) {
+                static_cast<T*>(dst)[at + e] = o.e[0];
+                static_cast<T*>(dst)[at + e + 1] = o.e[1];
+            } else {
+                store_pack<T, W>(dst, at + e, o);
+            }
+        }
+    }
+}
+
+template <typename T, int V>
+hipError_t append_launch(const ls_kv_cache& c, const ls_append_args& a, int n_cu, hipStream_t st) {
+    AppendP p{c, a, 0, 0, 0};
+    const bool pair = a.style == LS_ROPE_PAIR;
+    p.rot_units = pair ? a.rot_dim / (V < 2 ? 2 : V) : a.rot_dim / 2 / V;
+    p.units = p.rot_units + (c.head_dim - a.rot_dim) / V;
+    p.v_units = c.head_dim / V;
+    const int64_t total = (int64_t)(a.n_heads + c.n_kv_heads) * p.units + (int64_t)c.n_kv_heads * p.v_units;
+    // few tokens: every vector of a token on a thread of its own; many: a workgroup per token
+    const int64_t wanted = std::max<int64_t>(1, (int64_t)n_cu * 8 / std::max(1, a.n_tokens));
+    const dim3 grid(a.n_tokens, (unsigned)std::min<int64_t>({ceil_div(total, 256), wanted, 65535}));
+    if (pair)
+        hipLaunchKernelGGL((append_kernel<T, V, true>), grid, dim3(256), 0, st, p);
+    else
+        hipLaunchKernelGGL((append_kernel<T, V, false>), grid, dim3(256), 0, st, p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t append_type(const ls_kv_cache& c, const ls_append_args& a, int n_cu, hipStream_t st) {
+    // vectors of v elements: every address and offset that the kernel forms is a multiple of them
+    auto fits = [&](int v) {
+        const int64_t by = std::min<int64_t>(16, (int64_t)v * sizeof(T)), el = by / (int64_t)sizeof(T);
+        const int fl = a.style == LS_ROPE_PAIR ? v / 2 : v;  // cosines of one access
+        for (int64_t s : {c.page_stride, c.head_stride, c.token_stride, a.k_token_stride, a.k_head_stride, a.v_token_stride,
+                          a.v_head_stride, a.q_token_stride, a.q_head_stride, a.q_out_token_stride, a.q_out_head_stride})
+            if (s % el) return false;
+        for (const void* q : {(const void*)c.k, (const void*)c.v, a.k, a.v, a.q, (const void*)a.q_out})
+            if (q && !aligned(q, by)) return false;
+        if (a.rot_dim && !aligned(a.cos_sin, std::min(16, 4 * fl))) return false;
+        return c.head_dim % v == 0 && (a.rot_dim / 2) % fl == 0 && a.rot_dim % v == 0;
+    };
+    if (fits(8)) return append_launch<T, 8>(c, a, n_cu, st);
+    if (fits(4)) return append_launch<T, 4>(c, a, n_cu, st);
+    return append_launch<T, 1>(c, a, n_cu, st);
+}
+
+}  // namespace
+
+hipError_t launch_norm(const ls_norm_args& a, int n_cu, hipStream_t st) {
+    switch (a.dtype) {
+        case LS_F32: return norm_type<float>(a, n_cu, st);
+        case LS_F16: return norm_type<_Float16>(a, n_cu, st);
+        default: return norm_type<__bf16>(a, n_cu, st);
+    }
+}
+
+hipError_t launch_append(const ls_kv_cache& c, const ls_append_args& a, int n_cu, hipStream_t st) {
+    switch (c.dtype) {
+        case LS_F32: return append_type<float>(c, a, n_cu, st);
+        case LS_F16: return append_type<_Float16>(c, a, n_cu, st);
+        default: return append_type<__bf16>(c, a, n_cu, st);
+    }
+}
+
+}  // namespace ls

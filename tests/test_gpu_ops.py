@@ -1,0 +1,662 @@
+"""The decoder layer's operators (ls_ops.h) against their definitions in 64 bits.
+
+Tolerances are element by element and follow from the arithmetic: u is the unit roundoff of the
+output's type (one rounding when it is written), E = 2^-24 that of fp32, and each bound names the
+roundings that it counts."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2609_03079_amd as lsffn  # noqa: E402
+
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+U = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TINY = {torch.float32: 2.0 ** -149, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}  # half a subnormal step
+E = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ops():
+    o = lsffn.Ops()
+    yield o
+    o.close()
+
+
+def rand(shape, seed, dtype=torch.float32, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(dtype).to(DEV)
+
+
+def ints(values):
+    return torch.tensor(values, dtype=torch.int32, device=DEV)
+
+
+def within(got, ref, tol):
+    """Every element of got within tol of ref; NaN and infinities where ref has them."""
+    got, ref = got.double(), ref.double()
+    fine = torch.isfinite(ref)
+    assert torch.equal(torch.isnan(got), torch.isnan(ref))
+    assert torch.equal(got[~fine].nan_to_num(0, 1, -1), ref[~fine].nan_to_num(0, 1, -1))
+    over = ((got - ref).abs() - torch.as_tensor(tol, device=ref.device).expand_as(ref))[fine]
+    assert over.numel() == 0 or float(over.max()) <= 0, f"over its bound by {float(over.max()):.3g}"
+
+
+# ---- norms ---------------------------------------------------------------------------------------
+def norm_ref(x, y, gate, post, wp, pre, wh, xs, ys, eps):
+    """(x', h) in 64 bits, and the magnitude that their roundings are relative to."""
+    x64 = x.double() * xs
+    mag = x64.abs()
+    if y is not None:
+        t = y.double()
+        if post:
+            t = t / (t.square().mean(-1, keepdim=True) + eps).sqrt()
+            if wp is not None:
+                t = t * wp.double()
+        if gate is not None:
+            t = t * gate.double()
+        x64 = x64 + ys * t
+        mag = mag + (ys * t).abs()
+    h = x64
+    scale = torch.ones_like(x64[..., :1])
+    if pre:
+        scale = 1 / (x64.square().mean(-1, keepdim=True) + eps).sqrt()
+        h = h * scale
+    w = wh.double() if wh is not None else torch.ones_like(x64[0])
+    return x64, h * w, mag, scale * w.abs()
+
+
+# A thread adds at most 32 squares in a row, then 6 + 16 sums: 54 roundings, halved by the root;
+# with the quotient, the root, the products and the final sum, under 40 roundings of a term.
+NORM_E = 40 * E
+
+
+def check_norm(ops, T, d, dt, *, y=True, gate=None, post=True, pre=True, weights=True, xs=1.0, ys=1.0, eps=1e-6, seed=0,
+               in_place=False, pad=0, want_x=True, want_h=True, scale=1.0):
+    x = rand((T, d + pad), seed, std=scale)[:, :d]
+    yv = rand((T, d + pad), seed + 1, dt, 3.0 * scale)[:, :d] if y else None
+    gv = {None: None, "channel": lambda: rand((d,), seed + 2, dt), "token": lambda: rand((T, d + pad), seed + 2, dt)[:, :d]}[gate]
+    gv = gv() if gv else None
+    wp = rand((d,), seed + 3, dt) if weights and post and y else None
+    wh = rand((d,), seed + 4, dt) if weights and pre and want_h else None
+    xs, ys = float(np.float32(xs)), float(np.float32(ys))
+    rx, rh, mag, hs = norm_ref(x, yv, gv, post and y, wp, pre, wh, xs, ys, float(np.float32(eps)))
+    x0 = x.clone()
+    x_out = (x if in_place else torch.full((T, d + pad), math.nan, device=DEV)[:, :d]) if want_x else None
+    h = torch.full((T, d + pad), math.nan, device=DEV, dtype=dt)[:, :d] if want_h else None
+    ops.ls_norm_residual(x, y=yv, gate=gv, post_norm=post and y, post_weight=wp, pre_norm=pre, pre_weight=wh, x_scale=xs, y_scale=ys,
+                         eps=eps, x_out=x_out, h=h)
+    if want_x:
+        within(x_out, rx, NORM_E * mag)
+    if not in_place:
+        assert torch.equal(x, x0)
+    if want_h:
+        # h carries the error of x' (scaled), its own norm's, and the rounding when it is written
+        within(h, rh, hs * NORM_E * mag + (NORM_E + U[dt]) * rh.abs() * (1 + NORM_E) + TINY[dt])
+    return x_out, h
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T,d", [(1, 4096), (1, 1), (3, 7), (5, 64), (2, 520), (300, 1032), (2, 2048), (300, 4096), (3, 8192),
+                                 (300, 8192), (2, 16392), (2, 32768), (3, 1000), (2, 1025), (2, 9001), (1, 32767)])
+def test_norm(ops, dtype, T, d):
+    check_norm(ops, T, d, TYPES[dtype], gate="channel", xs=0.9, ys=0.5, seed=T * d)
+
+
+@pytest.mark.parametrize("case", [
+    dict(y=False, post=False), dict(post=False), dict(pre=False), dict(post=False, pre=False, gate="token"),
+    dict(gate="token", ys=-0.25), dict(weights=False, gate="token"), dict(in_place=True), dict(pad=8, gate="token"),
+    dict(pad=3, gate="token"), dict(want_x=False), dict(want_h=False, pre=False), dict(y=False, post=False, want_x=False),
+    dict(eps=0.0), dict(eps=1e-2, scale=1e-3), dict(scale=1e4), dict(xs=0.0)], ids=str)
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_norm_options(ops, dtype, case):
+    if dtype == "f16" and case.get("scale", 1) > 100:
+        case = dict(case, scale=100.0)
+    check_norm(ops, 5, 776, TYPES[dtype], seed=9, **case)
+
+
+def test_norm_zero_rows_and_no_numbers(ops):
+    # a row of zeros stays finite (eps), rows do not touch each other, a NaN fills its own row
+    x, y = rand((4, 512), 1), rand((4, 512), 2, torch.float16)
+    x[1], y[1] = 0, 0
+    y[2, 17] = math.nan
+    h, xo = torch.empty_like(y), torch.empty_like(x)
+    ops.ls_norm_residual(x, y=y, post_norm=True, pre_norm=True, x_out=xo, h=h)
+    assert torch.all(h[1] == 0) and torch.all(torch.isnan(xo[2])) and torch.all(torch.isnan(h[2]))
+    clean = [0, 3]
+    rx, rh, mag, hs = norm_ref(x[clean], y[clean], None, True, None, True, None, 1.0, 1.0, float(np.float32(1e-6)))
+    within(xo[clean], rx, NORM_E * mag)
+    within(h[clean], rh, hs * NORM_E * mag + (NORM_E + U[torch.float16]) * rh.abs() + TINY[torch.float16])
+    ops.ls_norm_residual(x[:0], h=h[:0])  # no tokens: nothing
+
+
+# ---- 8-bit products --------------------------------------------------------------------------------
+def quantised(x):
+    """(integers, fp32 scales) of the definition, in fp32 on the CPU."""
+    x = x.float().cpu().numpy()
+    top = np.abs(x).max(1, keepdims=True)
+    s = (top / np.float32(127)).astype(np.float32)
+    s = np.where(s < np.float32(2.0 ** -126), np.float32(0), s)
+    q = np.rint((x * np.float32(127)).astype(np.float32) / np.where(s > 0, top, np.float32(1)))
+    return torch.from_numpy(np.where(s > 0, q, 0).astype(np.float64)).to(DEV), torch.from_numpy(s[:, 0]).to(DEV)
+
+
+def check_linear(ops, T, k, n, x_type, out_type, *, bias=False, pad=0, seed=0, x=None):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randint(-128, 128, (n, k + 16 * pad), generator=g, dtype=torch.int8).to(DEV)[:, :k]
+    ws, b = rand((n,), seed + 1).abs() * 0.01 + 1e-3, rand((n,), seed + 2) if bias else None
+    xs = None
+    if x_type == "i8":
+        x = torch.randint(-128, 128, (T, k + 16 * pad), generator=g, dtype=torch.int8).to(DEV)[:, :k]
+        xs = rand((T,), seed + 3).abs() * 0.1
+        q, s = x.double(), xs
+    else:
+        x = rand((T, k + 16 * pad), seed + 4, TYPES[x_type])[:, :k] if x is None else x
+        q, s = quantised(x)
+    dt = TYPES[out_type]
+    out = torch.full((T, n + pad), math.nan, device=DEV, dtype=dt)
+    ops.ls_linear_i8(x, w, ws, out[:, :n], x_scale=xs, bias=b)
+    # an exact sum, its conversion, two products and the bias: 4 roundings
+    ref = (q @ w.double().T.contiguous()) * s.double()[:, None] * ws.double()
+    mag = ref.abs() + (b.double().abs() if bias else 0)
+    ref = ref + b.double() if bias else ref
+    within(out[:, :n], ref, 5 * E * mag + U[dt] * ref.abs() * (1 + 8 * E) + TINY[dt])
+    assert pad == 0 or torch.all(torch.isnan(out[:, n:]))  # nothing past a row
+    return out
+
+
+@pytest.mark.parametrize("T", [1, 2, 3, 5, 8, 15, 16, 17, 33, 48, 64, 65, 100, 129, 257, 511])
+@pytest.mark.parametrize("k,n", [(16, 1), (64, 16), (272, 100), (1040, 515)])
+def test_linear_shapes(ops, T, k, n):
+    for x_type, out_type in (("i8", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("f32", "f32")):
+        check_linear(ops, T, k, n, x_type, out_type, bias=T % 2 == 1, pad=T % 3, seed=T + k)
+
+
+@pytest.mark.parametrize("T,k,n", [(1, 4096, 4096), (4, 8192, 1000), (8, 16384, 333), (1, 131056, 40), (70, 4096, 2050), (300, 2048, 4100),
+                                   (1100, 1024, 1300), (2, 20000, 64), (3000, 512, 700)])
+def test_linear_larger(ops, T, k, n):
+    check_linear(ops, T, k, n, "bf16", "bf16", seed=k)
+    check_linear(ops, T, k, n, "i8", "f32", seed=k)
+
+
+def test_linear_extreme_sums_and_tokens(ops):
+    # the largest sums: 128 * 128 * 131056 stays below 2^31
+    k = 131056
+    x, w = torch.full((2, k), -128, dtype=torch.int8, device=DEV), torch.full((3, k), -128, dtype=torch.int8, device=DEV)
+    w[1] = 127
+    out = torch.empty((2, 3), device=DEV)
+    one = torch.ones(3, device=DEV)
+    ops.ls_linear_i8(x, w, one, out, x_scale=one[:2])
+    assert out.tolist() == [[float(np.float32(128 * 128 * k)), float(np.float32(-128 * 127 * k)), float(np.float32(128 * 128 * k))]] * 2
+    # zeros, the smallest numbers, ties, infinities and NaN, token by token
+    for dt in (torch.float16, torch.bfloat16, torch.float32):
+        for T in (6, 70):
+            x = rand((T, 64), 3, dt)
+            x[0] = 0
+            x[1] = 0
+            x[1, 5] = TINY[dt] * 2
+            x[2] = torch.arange(64, dtype=torch.float32).to(dt) + 0.5
+            x[2, 0] = 127
+            x[3, 9] = math.inf
+            x[4, 9] = math.nan
+            w, ws = torch.randint(-127, 128, (20, 64), dtype=torch.int8).to(DEV), torch.ones(20, device=DEV)
+            out = torch.empty((T, 20), device=DEV)
+            ops.ls_linear_i8(x, w, ws, out)
+            assert torch.all(torch.isnan(out[3:5])) and torch.all(out[0] == 0)
+            keep = [i for i in range(T) if i not in (3, 4)]
+            q, s = quantised(x[keep])
+            ref = (q @ w.double().T.contiguous()) * s.double()[:, None]
+            within(out[keep], ref, 5 * E * ref.abs() + 2.0 ** -149)
+    ops.ls_linear_i8(x[:0], w, ws, out[:0])
+
+
+# ---- append ----------------------------------------------------------------------------------------
+def make_cache(pages, kv, page, dim, dt, seed, layout="head"):
+    shape = (pages, kv, page, dim) if layout == "head" else (pages, page, kv, dim)
+    k, v = rand(shape, seed, dt), rand(shape, seed + 1, dt)
+    return (k, v) if layout == "head" else (k.transpose(1, 2), v.transpose(1, 2))
+
+
+def table(n_pos, rot, seed=0):
+    ang = torch.arange(n_pos, dtype=torch.float64)[:, None] * 1e4 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / max(rot, 1)) + seed
+    return torch.cat([ang.cos(), ang.sin()], 1).float().to(DEV)
+
+
+def rope_ref(x, cs, rot, style):
+    """Rotated rows in 64 bits, and the magnitude that their roundings are relative to."""
+    x = x.double()
+    out, mag = x.clone(), torch.zeros_like(x)
+    i = torch.arange(rot // 2)
+    a, b = (i, i + rot // 2) if style == lsffn.LS_ROPE_HALF else (2 * i, 2 * i + 1)
+    c, s = cs.double()[:, None, :rot // 2], cs.double()[:, None, rot // 2:]
+    out[..., a] = x[..., a] * c - x[..., b] * s
+    out[..., b] = x[..., b] * c + x[..., a] * s
+    mag[..., a] = mag[..., b] = (x[..., a].abs() + x[..., b].abs())
+    return out, mag
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T,heads,kv,dim,rot,style,page,layout,in_place", [
+    (1, 32, 32, 128, 128, 0, 16, "head", False), (1, 8, 1, 256, 256, 0, 64, "token", True), (37, 10, 5, 80, 40, 1, 16, "token", False),
+    (37, 10, 5, 80, 40, 0, 16, "head", True), (9, 4, 2, 7, 6, 0, 1, "head", False), (9, 4, 2, 7, 4, 1, 2, "token", True),
+    (130, 6, 3, 112, 56, 0, 128, "head", False), (130, 6, 3, 112, 112, 1, 8, "token", False), (5, 0, 3, 64, 64, 0, 4, "head", False),
+    (300, 3, 1, 1, 0, 0, 4096, "head", False), (2000, 2, 2, 64, 32, 1, 32, "head", False), (3, 5, 5, 1024, 1024, 0, 2, "head", False)])
+def test_append(ops, dtype, T, heads, kv, dim, rot, style, page, layout, in_place):
+    dt = TYPES[dtype]
+    pages = T // page + 3
+    kc, vc = make_cache(pages, kv, page, dim, dt, 1, layout)
+    qkv = rand((T, (heads + 2 * kv) * dim), 3, dt)
+    q, k, v = (x.view(T, -1, dim) for x in qkv.split([heads * dim, kv * dim, kv * dim], 1))
+    g = torch.Generator().manual_seed(T)
+    slots = torch.randperm(pages * page, generator=g)[:T].to(torch.int32)
+    positions = torch.randint(0, 50, (T,), generator=g).to(torch.int32)
+    if T > 4:  # padding, a slot past the cache, positions outside the table
+        slots[1], slots[2], positions[3], positions[4] = -1, pages * page, -1, 50
+    cs = table(50, rot) if rot else None
+    q0, k0, v0 = qkv.clone(), kc.clone(), vc.clone()
+    q_out = None if heads == 0 else q if in_place else torch.full((T, heads, dim), 7.0, device=DEV, dtype=dt)
+    q_before = None if heads == 0 else q_out.clone()
+    ops.ls_kv_append(kc, vc, k, v, positions.to(DEV) if rot else None, slots.to(DEV), cs, q=q if heads else None, q_out=q_out, style=style)
+    placed = torch.tensor([rot == 0 or 0 <= int(p) < 50 for p in positions])
+    kept = placed & (slots >= 0) & (slots < pages * page)
+    at = cs[positions.clamp(0, 49).long().to(DEV)] if rot else torch.zeros((T, 0), device=DEV)
+    src = [x.view(T, -1, dim) for x in q0.split([heads * dim, kv * dim, kv * dim], 1)]
+
+    def check(got, ref, mag):  # two products and a sum in fp32, one rounding when it is written
+        within(got, ref, 4 * E * mag + U[dt] * ref.abs() * (1 + 8 * E) + TINY[dt])
+
+    rk, mk = rope_ref(src[1], at, rot, style)
+    sl = slots[kept].long().to(DEV)
+    pg, pl = sl // page, sl % page
+    check(kc[pg, :, pl], rk[kept.to(DEV)], mk[kept.to(DEV)])
+    assert torch.equal(vc[pg, :, pl], src[2][kept.to(DEV)])
+    k0[pg, :, pl], v0[pg, :, pl] = kc[pg, :, pl], vc[pg, :, pl]
+    assert torch.equal(kc, k0) and torch.equal(vc, v0)  # nothing else was written
+    if heads:
+        rq, mq = rope_ref(src[0], at, rot, style)
+        check(q_out[placed.to(DEV)], rq[placed.to(DEV)], mq[placed.to(DEV)])
+        assert torch.equal(q_out[~placed.to(DEV)], q_before[~placed.to(DEV)])
+
+
+def test_append_offsets_past_32_bits(ops):
+    # pages 70000 of 64 KiB: the last ones lie over 4 GiB from the start of the cache
+    pages, kv, page, dim = 70000, 8, 32, 128
+    kc, vc = (torch.empty((pages, kv, page, dim), dtype=torch.float16, device=DEV) for _ in range(2))
+    k, v = rand((3, kv, dim), 1, torch.float16), rand((3, kv, dim), 2, torch.float16)
+    slots = [pages * page - 1, 33000 * page + 5, 3]
+    ops.ls_kv_append(kc, vc, k, v, None, ints(slots), None)
+    for i, s in enumerate(slots):
+        assert torch.equal(kc[s // page, :, s % page], k[i]) and torch.equal(vc[s // page, :, s % page], v[i])
+    # and the attention reads them there
+    q = rand((1, 16, dim), 3, torch.float16)
+    out = torch.empty_like(q)
+    kc[pages - 1], vc[pages - 1] = rand((kv, page, dim), 4, torch.float16), rand((kv, page, dim), 5, torch.float16)
+    ops.ls_attend(q, kc, vc, ints([[pages - 1]]), ints([page]), out, max_len=page, scale=0.1)
+    small = torch.empty_like(q)
+    ops.ls_attend(q, kc[pages - 1:].clone(), vc[pages - 1:].clone(), ints([[0]]), ints([page]), small, max_len=page, scale=0.1)
+    assert torch.equal(out, small) and torch.any(out != 0)
+
+
+# ---- attention -------------------------------------------------------------------------------------
+def attend_ref(q, kc, vc, pages, lens, n_q, max_len, prefix_pages, prefix_len, scale):
+    """The definition in 64 bits, row by row, and its bound."""
+    n_pages, kv, page, dim = kc.shape
+    heads, dt = q.shape[1], q.dtype
+    G = heads // kv
+    out = torch.zeros((q.shape[0], heads, dim), dtype=torch.float64, device=DEV)
+    tol = torch.zeros_like(out)
+
+    def rows(table_, n):
+        key = torch.arange(n)
+        ids = table_.cpu().long()[key // page] if n else torch.zeros(0, dtype=torch.long)
+        ok = ((ids >= 0) & (ids < n_pages))
+        return (ids.clamp(0, n_pages - 1), key % page), ok
+
+    for s in range(len(lens)):
+        n = int(lens[s])
+        if n < 0:
+            continue
+        n = min(n, max_len)
+        at, ok = rows(pages[s], n) if n else rows(None, 0)
+        if prefix_len:
+            pat, pok = rows(prefix_pages, prefix_len)
+            at, ok = tuple(torch.cat([a, b]) for a, b in zip(pat, at)), torch.cat([pok, ok])
+        for i in range(n_q):
+            m = prefix_len + max(0, n - n_q + i + 1)
+            keep = ok[:m].nonzero().flatten()
+            if not len(keep):
+                continue
+            k = kc[at[0][keep], :, at[1][keep]].double()  # [keys, kv, dim]
+            v = vc[at[0][keep], :, at[1][keep]].double()
+            qq = q[s * n_q + i].double().view(kv, G, dim)
+            sc = torch.einsum("hgd,khd->hgk", qq, k) * scale
+            p = torch.softmax(sc, -1)
+            o = torch.einsum("hgk,khd->hgd", p, v)
+            # a weight: rounded once (u), its score from dim fp32 products and sums, the maximum's
+            # subtraction and the exponential; a weight below the type's normal range is off by half a step
+            e_sc = (dim + 8) * E * torch.einsum("hgd,khd->hgk", qq.abs(), k.abs()).amax(-1, keepdim=True) * scale + 16 * E
+            pv = torch.einsum("hgk,khd->hgd", p, v.abs())
+            t = (U[dt] + 2 * e_sc + len(keep) ** 0.5 * E * 8) * pv + U[dt] * o.abs() + TINY[dt] * (1 + v.abs().sum(0)[:, None])
+            out[s * n_q + i], tol[s * n_q + i] = o.reshape(heads, dim), t.reshape(heads, dim)
+    return out, tol
+
+
+def check_attend(ops, *, lens, heads=4, kv=2, dim=64, dt=torch.float16, prefix=0, n_q=1, page=16, layout="head", max_len=None,
+                 bad_pages=False, seed=0, std=1.0, poison=True, stride_pad=0, spare=0, touch=None):
+    S = len(lens)
+    most = max([0, *lens])
+    max_len = most if max_len is None else max_len
+    n, pre = -(-max_len // page), -(-prefix // page)
+    total = pre + n * S + 2
+    kc, vc = make_cache(total, kv, page, dim, dt, seed, layout)
+    g = torch.Generator().manual_seed(seed)
+    order = torch.randperm(total, generator=g).to(torch.int32)
+    prefix_pages, pages = order[:pre].clone(), order[pre:pre + n * S].view(S, n).clone()
+    if bad_pages:
+        if n > 1:
+            pages[0, 0], pages[S - 1, n // 2] = -1, total
+        if pre > 2:
+            prefix_pages[1], prefix_pages[pre - 1] = -5, 2 ** 31 - 1
+    if poison:  # whatever no row may see is no number
+        seen = torch.zeros((total, page), dtype=torch.bool)
+        for row, m in [(prefix_pages, prefix)] + [(pages[s], min(max(0, lens[s]), max_len)) for s in range(S)]:
+            for j in range(m):
+                if 0 <= row[j // page] < total:
+                    seen[row[j // page], j % page] = True
+        hide = (~seen)[:, None, :, None].to(DEV)
+        kc.masked_fill_(hide, math.nan)
+        vc.masked_fill_(hide, math.inf)
+    if touch:
+        touch(kc, vc, pages, prefix_pages)
+    q = rand((S * n_q, heads + stride_pad, dim), seed + 7, dt, std)[:, :heads]
+    out = torch.full((S * n_q, heads + stride_pad, dim), 5.0, device=DEV, dtype=dt)
+    scale = 1 / math.sqrt(dim)
+    wide = torch.full((S, n + spare), 2 ** 30, dtype=torch.int32)
+    wide[:, :n] = pages
+    args = dict(n_q=n_q, max_len=max_len, prefix_pages=prefix_pages.to(DEV), prefix_len=prefix, scale=scale)
+    ops.ls_attend(q, kc, vc, wide.to(DEV), ints(lens), out[:, :heads], **args)
+    ref, tol = attend_ref(q, kc, vc, pages, lens, n_q, max_len, prefix_pages, prefix, scale)
+    within(out[:, :heads], ref, tol)
+    assert stride_pad == 0 or torch.all(out[:, heads:] == 5.0)
+    again = torch.empty_like(out)[:, :heads]
+    ops.ls_attend(q, kc, vc, wide.to(DEV), ints(lens), again, **args)
+    assert torch.equal(out[:, :heads].nan_to_num(9), again.nan_to_num(9))  # the same bits
+    return out[:, :heads]
+
+
+BOTH = [torch.float16, torch.bfloat16]
+
+
+@pytest.mark.parametrize("dt", BOTH, ids=["f16", "bf16"])
+@pytest.mark.parametrize("length", [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 500, 1300])
+def test_attend_lengths(ops, dt, length):
+    check_attend(ops, lens=[length], dt=dt, seed=length)
+    check_attend(ops, lens=[length, 3, 0, length // 2], prefix=length, dt=dt, seed=length + 1)
+
+
+@pytest.mark.parametrize("dim", [8, 16, 40, 64, 72, 80, 96, 112, 128, 136, 192, 256])
+@pytest.mark.parametrize("prefix,lens,heads,kv", [(0, [70], 3, 3), (77, [5, 200], 8, 2), (150, [40, 1, 90], 40, 1)])
+def test_attend_head_sizes(ops, dim, prefix, lens, heads, kv):
+    for dt in BOTH:
+        check_attend(ops, lens=lens, prefix=prefix, heads=heads, kv=kv, dim=dim, dt=dt, seed=dim)
+
+
+@pytest.mark.parametrize("page", [1, 2, 8, 16, 32, 64, 128, 1024])
+@pytest.mark.parametrize("layout", ["head", "token"])
+def test_attend_pages(ops, page, layout):
+    check_attend(ops, lens=[300, 17], prefix=131, page=page, layout=layout, spare=3, seed=page)
+    check_attend(ops, lens=[300, 17, 64, 65, 128, 2, 9, 40, 77], prefix=131, heads=16, page=page, layout=layout, bad_pages=True, seed=page)
+
+
+@pytest.mark.parametrize("n_q", [1, 2, 3, 5, 8, 16])
+@pytest.mark.parametrize("heads,kv", [(1, 1), (4, 4), (8, 2), (12, 2), (32, 1)])
+def test_attend_query_tokens(ops, n_q, heads, kv):
+    # lengths shorter than n_q leave rows that see nothing, or the prefix alone
+    lens = [n_q, 90, n_q - 1, 0, -1, 1, 64, 65]
+    check_attend(ops, lens=lens, prefix=0, heads=heads, kv=kv, n_q=n_q, dt=torch.bfloat16, seed=n_q)
+    check_attend(ops, lens=lens, prefix=45, heads=heads, kv=kv, n_q=n_q, seed=n_q + 1)
+
+
+@pytest.mark.parametrize("rows", [1, 31, 32, 33, 64, 127, 128, 129, 260])
+def test_attend_row_tiles(ops, rows):
+    check_attend(ops, lens=[(7 * s) % 40 for s in range(rows)], prefix=200, heads=2, kv=2, dim=32, dt=torch.bfloat16, seed=rows)
+
+
+def test_attend_nothing_to_see(ops):
+    out = check_attend(ops, lens=[0, -1, -7], prefix=0, max_len=40)
+    assert torch.all(out == 0)
+    out = check_attend(ops, lens=[0, -1, 0], prefix=0, max_len=0)
+    assert torch.all(out == 0)
+    out = check_attend(ops, lens=[-1, 4, -1], prefix=100)
+    assert torch.all(out[[0, 2]] == 0) and torch.any(out[1] != 0)
+    out = check_attend(ops, lens=[0, -1], prefix=100, max_len=0)  # the prefix alone
+    assert torch.any(out[0] != 0) and torch.all(out[1] == 0)
+
+    def all_bad(kc, vc, pages, prefix_pages):
+        pages.fill_(-1)
+        prefix_pages.fill_(10 ** 6)
+    out = check_attend(ops, lens=[30, 60], prefix=70, touch=all_bad, poison=False)
+    assert torch.all(out == 0)
+
+
+def test_attend_lengths_past_the_bound(ops):
+    # only max_len keys count, whatever the device lengths say
+    check_attend(ops, lens=[500, 20], max_len=100, prefix=10, poison=False)
+    check_attend(ops, lens=[2 ** 31 - 1, 3], max_len=64, poison=False)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("heads,n_q", [(2, 4), (2, 16), (24, 5)])
+def test_attend_a_later_tokens_value_stays_out(ops, bad, heads, n_q):
+    # the last token's value is no number: the tokens before it must not see it, it must itself
+    def touch(kc, vc, pages, prefix_pages):
+        vc[pages[0, 69 // 16], :, 69 % 16, 3] = bad
+    out = check_attend(ops, lens=[70, 30], prefix=50, heads=heads, kv=1, n_q=n_q, touch=touch)
+    finite = torch.isfinite(out)
+    assert torch.all(finite[:n_q - 1]) and not torch.any(finite[n_q - 1, :, 3])
+    assert torch.all(finite[n_q:])
+
+
+def test_attend_no_numbers_in_sight(ops):
+    def touch(kc, vc, pages, prefix_pages):
+        kc[pages[0, 0], 0, 1] = math.nan   # a key of sequence 0, head 0 of 2: its rows alone
+    out = check_attend(ops, lens=[40, 40], touch=touch)
+    assert torch.all(torch.isnan(out[0, :2])) and torch.all(torch.isfinite(out[0, 2:])) and torch.all(torch.isfinite(out[1]))
+
+    def far(kc, vc, pages, prefix_pages):
+        kc.mul_(60.0)
+    check_attend(ops, lens=[200, 33], prefix=100, touch=far, dt=torch.bfloat16, std=30.0, poison=False)  # weights of 0 and 1
+
+
+def test_attend_strides(ops):
+    check_attend(ops, lens=[50, 90], prefix=20, stride_pad=3, layout="token")
+
+
+@pytest.mark.parametrize("lens,prefix,heads,kv,n_q", [([3000] * 2, 9000, 8, 8, 1), ([200 * s for s in range(20)], 5000, 32, 4, 2)])
+def test_attend_longer(ops, lens, prefix, heads, kv, n_q):
+    check_attend(ops, lens=lens, prefix=prefix, heads=heads, kv=kv, n_q=n_q, dim=128, dt=torch.bfloat16, page=64, poison=False)
+
+
+def test_attend_small_workspace():
+    """A workspace that holds fewer parts: the same rows within the bound; one that holds not even
+    two parts of a row is refused."""
+    o = lsffn.Ops(workspace_bytes=1 << 20)
+    check_attend(o, lens=[4000] * 8, prefix=6000, heads=32, kv=32, dim=128, page=64, poison=False)
+    q = torch.zeros((64, 64, 128), dtype=torch.float16, device=DEV)
+    kc, vc = make_cache(4, 64, 16, 128, torch.float16, 0)
+    with pytest.raises(lsffn.LsError) as e:
+        o.ls_attend(q, kc, vc, ints([[0]] * 64), ints([4] * 64), torch.empty_like(q), max_len=4, scale=1.0, prefix_pages=ints([1]),
+                    prefix_len=3)
+    assert e.value.status == lsffn.LS_E_CAPACITY
+    with pytest.raises(lsffn.LsError) as e:
+        o.ls_linear_i8(torch.zeros((300, 4096), device=DEV), torch.zeros((4, 4096), dtype=torch.int8, device=DEV),
+                       torch.ones(4, device=DEV), torch.empty((300, 4), device=DEV))
+    assert e.value.status == lsffn.LS_E_CAPACITY
+    o.close()
+
+
+# ---- streams, graphs, refusals ---------------------------------------------------------------------
+def layer_pass(o, t):
+    """The operators in the order of a decoder layer, on the tensors of `t`."""
+    o.ls_norm_residual(t["x"], pre_norm=True, h=t["h"])
+    o.ls_linear_i8(t["h"], t["w_qkv"], t["s_qkv"], t["qkv"])
+    q, k, v = (a.view(4, -1, 64) for a in t["qkv"].split([512, 128, 128], 1))
+    o.ls_kv_append(t["k"], t["v"], k, v, t["positions"], t["slots"], t["table"], q=q, q_out=t["q"])
+    o.ls_attend(t["q"], t["k"], t["v"], t["pages"], t["lens"], t["o"], max_len=64, prefix_pages=t["prefix"], prefix_len=40, scale=0.125)
+    o.ls_linear_i8(t["o"].view(4, 512), t["w_o"], t["s_o"], t["y"])
+    o.ls_norm_residual(t["x"], y=t["y"], post_norm=True, y_scale=0.5, x_out=t["x_out"])
+
+
+def layer_tensors():
+    g = torch.Generator().manual_seed(5)
+    t = {"x": rand((4, 512), 1), "h": torch.empty((4, 512), dtype=torch.bfloat16, device=DEV),
+         "w_qkv": torch.randint(-127, 128, (768, 512), generator=g, dtype=torch.int8).to(DEV), "s_qkv": torch.full((768,), 1e-3, device=DEV),
+         "w_o": torch.randint(-127, 128, (512, 512), generator=g, dtype=torch.int8).to(DEV), "s_o": torch.full((512,), 1e-3, device=DEV),
+         "qkv": torch.empty((4, 768), dtype=torch.bfloat16, device=DEV), "q": torch.empty((4, 8, 64), dtype=torch.bfloat16, device=DEV),
+         "o": torch.empty((4, 8, 64), dtype=torch.bfloat16, device=DEV), "y": torch.empty((4, 512), dtype=torch.bfloat16, device=DEV),
+         "x_out": torch.empty((4, 512), device=DEV), "table": table(200, 64), "prefix": ints([20, 21, 22]),
+         "pages": torch.arange(16, dtype=torch.int32, device=DEV).view(4, 4), "lens": ints([1, 5, 17, 30]),
+         "slots": ints([0, 64 + 4, 128 + 16, 192 + 29]), "positions": ints([40, 44, 56, 69])}
+    t["k"], t["v"] = make_cache(24, 2, 16, 64, torch.bfloat16, 9)
+    return t
+
+
+def test_graph_replays_read_their_arguments_anew():
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        t = layer_tensors()
+        s.synchronize()
+        o = lsffn.Ops(stream=s)
+        layer_pass(o, t)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            layer_pass(o, t)
+        for step in range(4):
+            for n in ("lens", "positions", "slots"):
+                t[n].add_(1)
+            t["x"].mul_(1.1)
+            graph.replay()
+            s.synchronize()
+            got, k = t["x_out"].clone(), t["k"].clone()
+            t["x_out"].fill_(math.nan)
+            layer_pass(o, t)  # eager, on the same state: the same bits
+            s.synchronize()
+            assert torch.equal(got, t["x_out"]) and torch.equal(k, t["k"]) and torch.all(torch.isfinite(got))
+        o.close()
+
+
+def test_another_stream_gives_the_same_bits(ops):
+    t = layer_tensors()
+    layer_pass(ops, t)
+    ops.ls_ops_sync()
+    want = t["x_out"].clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    o = lsffn.Ops(stream=s)
+    t = layer_tensors()
+    torch.cuda.synchronize()
+    layer_pass(o, t)
+    o.ls_ops_sync()
+    assert torch.equal(t["x_out"], want)
+    o.close()
+
+
+def refused(call, status=lsffn.LS_E_INVAL, text=""):
+    with pytest.raises(lsffn.LsError) as e:
+        call()
+    assert e.value.status == status and text in str(e.value), str(e.value)
+
+
+def test_refusals(ops):
+    x, h16 = rand((2, 64), 0), torch.empty((2, 64), dtype=torch.float16, device=DEV)
+    refused(lambda: ops.ls_norm_residual(x), text="both NULL")
+    refused(lambda: ops.ls_norm_residual(x, post_norm=True, h=h16), text="without y")
+    refused(lambda: ops.ls_norm_residual(x, h=h16, eps=-1.0), text="eps")
+    refused(lambda: ops.ls_norm_residual(x, h=h16, eps=math.nan), text="eps")
+    refused(lambda: ops.ls_norm_residual(rand((1, 32769), 0), x_out=rand((1, 32769), 0)), text="d must be")
+    refused(lambda: ops.ls_norm_residual(x, h=torch.empty((64,), dtype=torch.float16, device=DEV).expand(2, 64)), text="h_stride")
+    for bad in (lambda: ops.ls_norm_residual(x.half(), h=h16), lambda: ops.ls_norm_residual(x, y=x, h=h16),
+                lambda: ops.ls_norm_residual(x, h=h16[:, :32]), lambda: ops.ls_norm_residual(x, h=h16.cpu()),
+                lambda: ops.ls_norm_residual(rand((64, 2), 0).T, h=h16)):
+        with pytest.raises(ValueError):
+            bad()
+
+    x8, w, s = (torch.zeros(a, dtype=torch.int8, device=DEV) for a in ((2, 64), (8, 64), (1,)))
+    ws, xs, out = torch.ones(8, device=DEV), torch.ones(2, device=DEV), torch.empty((2, 8), device=DEV)
+    refused(lambda: ops.ls_linear_i8(x8, w, ws, out), text="x_scale")
+    refused(lambda: ops.ls_linear_i8(x, w, ws, out, x_scale=xs), text="x_scale")
+    refused(lambda: ops.ls_linear_i8(x8[:, :40], w[:, :40], ws, out, x_scale=xs), text="multiple of 16")
+    refused(lambda: ops.ls_linear_i8(torch.zeros(200, dtype=torch.int8, device=DEV)[1:129].view(2, 64), w, ws, out, x_scale=xs), text="aligned")
+    refused(lambda: ops.ls_linear_i8(x8, w, ws, out[0].expand(2, 8), x_scale=xs), text="out_stride")
+    with pytest.raises(ValueError):
+        ops.ls_linear_i8(x8, w, ws.half(), out, x_scale=xs)
+    with pytest.raises(ValueError):
+        ops.ls_linear_i8(x8, w[:, :32], ws, out, x_scale=xs)
+
+    kc, vc = make_cache(4, 2, 16, 64, torch.float16, 0)
+    k, cs, one = rand((2, 2, 64), 1, torch.float16), table(8, 64), ints([0, 1])
+    refused(lambda: ops.ls_kv_append(kc, vc, k, k, None, one, cs), text="positions")
+    refused(lambda: ops.ls_kv_append(kc, vc, k, k, one, one, table(8, 64)[:, :63].contiguous()), text="rot_dim")
+    refused(lambda: ops.ls_kv_append(kc, vc, k, k, one, one, cs, q=k), text="q_out")
+    refused(lambda: ops.ls_kv_append(kc, vc, k, k, one, one, cs, style=2), text="style")
+    refused(lambda: ops.ls_kv_append(*make_cache(4, 2, 12, 64, torch.float16, 0), k, k, one, one, cs), text="power of two")
+    with pytest.raises(ValueError):
+        ops.ls_kv_append(kc, vc.float(), k, k, one, one, cs)
+    with pytest.raises(ValueError):
+        ops.ls_kv_append(kc, vc, k[:, :1], k, one, one, cs)
+    with pytest.raises(ValueError):
+        ops.ls_kv_append(kc, vc, k, k, one.long(), one, cs)
+    with pytest.raises(ValueError):
+        ops.ls_kv_append(kc, vc.transpose(1, 2).contiguous().transpose(1, 2), k, k, one, one, cs)
+
+    q, pages, lens = rand((2, 4, 64), 1, torch.float16), ints([[0, 1], [2, 3]]), ints([20, 3])
+    o = torch.empty_like(q)
+    ok = dict(max_len=32, scale=0.1)
+    ops.ls_attend(q, kc, vc, pages, lens, o, **ok)
+    refused(lambda: ops.ls_attend(q, kc, vc, pages, lens, o, max_len=32, scale=0.0), text="scale")
+    refused(lambda: ops.ls_attend(q, kc, vc, pages, lens, o, max_len=32, scale=math.inf), text="scale")
+    refused(lambda: ops.ls_attend(q, kc, vc, pages, lens, o, max_len=-1, scale=0.1), text="max_len")
+    refused(lambda: ops.ls_attend(q[:, :3], kc, vc, pages, lens, o[:, :3], **ok), text="multiple of n_kv_heads")
+    refused(lambda: ops.ls_attend(rand((34, 4, 64), 1, torch.float16), kc, vc, pages, lens, torch.empty((34, 4, 64), dtype=torch.float16,
+                                                                                                    device=DEV), n_q=17, **ok), text="n_q")
+    f32 = make_cache(4, 2, 16, 64, torch.float32, 0)
+    refused(lambda: ops.ls_attend(q.float(), *f32, pages, lens, o.float(), **ok), status=lsffn.LS_E_UNSUPPORTED)
+    odd = make_cache(4, 2, 16, 60, torch.float16, 0)
+    refused(lambda: ops.ls_attend(rand((2, 4, 60), 1, torch.float16), *odd, pages, lens, torch.empty((2, 4, 60), dtype=torch.float16, device=DEV),
+                                  **ok), text="multiple of 8")
+    with pytest.raises(ValueError):
+        ops.ls_attend(q, kc, vc, pages, lens, o, max_len=33, scale=0.1)
+    with pytest.raises(ValueError):
+        ops.ls_attend(q, kc, vc, pages, lens, o, prefix_pages=ints([0]), prefix_len=17, **ok)
+    with pytest.raises(ValueError):
+        ops.ls_attend(q[:1], kc, vc, pages, lens, o, **ok)
+    # a refused call leaves the context usable
+    ops.ls_attend(q, kc, vc, pages, lens, o, **ok)
+    ops.ls_ops_sync()
+
+
+def test_context_refusals():
+    lib = lsffn.load()
+    h = ctypes.c_void_p()
+    assert lib.ls_ops_create(None, ctypes.byref(h)) == lsffn.LS_E_INVAL and not h.value
+    assert lib.ls_ops_create(ctypes.byref(lsffn.LsOpsDesc(0, None, 1)), ctypes.byref(h)) == lsffn.LS_E_INVAL
+    assert lib.ls_ops_create(ctypes.byref(lsffn.LsOpsDesc(4096, None, 0)), ctypes.byref(h)) == lsffn.LS_E_INVAL
+    assert b"workspace" in lib.ls_ops_last_error(None)
+    assert lib.ls_ops_create(ctypes.byref(lsffn.LsOpsDesc(1 << 50, None, 0)), ctypes.byref(h)) == lsffn.LS_E_NOMEM
+    assert lib.ls_ops_create(ctypes.byref(lsffn.LsOpsDesc(0, None, 0)), None) == lsffn.LS_E_INVAL
+    assert lib.ls_ops_destroy(None) == lsffn.LS_E_INVAL and lib.ls_ops_sync(None) == lsffn.LS_E_INVAL
+    assert lib.ls_norm_residual(None, None) == lsffn.LS_E_INVAL
+    o = lsffn.Ops()
+    for call in (lambda: lib.ls_norm_residual(o.ctx, None), lambda: lib.ls_linear_i8(o.ctx, None), lambda: lib.ls_kv_append(o.ctx, None, None),
+                 lambda: lib.ls_attend(o.ctx, None, None)):
+        assert call() == lsffn.LS_E_INVAL
+    o.close()
