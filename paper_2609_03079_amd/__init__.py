@@ -85,45 +85,6 @@ class LsOpsDesc(ctypes.Structure):
     _fields_ = [("workspace_bytes", ctypes.c_uint64), ("stream", ctypes.c_void_p), ("debug_flags", ctypes.c_uint32)]
 
 
-class LsNormArgs(ctypes.Structure):
-    _fields_ = [("n_tokens", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int), ("post_norm", ctypes.c_int32),
-                ("pre_norm", ctypes.c_int32), ("x_scale", ctypes.c_float), ("y_scale", ctypes.c_float), ("eps", ctypes.c_float),
-                ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("y", ctypes.c_void_p), ("y_stride", ctypes.c_int64),
-                ("gate", ctypes.c_void_p), ("gate_stride", ctypes.c_int64), ("post_weight", ctypes.c_void_p),
-                ("pre_weight", ctypes.c_void_p), ("x_out", ctypes.c_void_p), ("x_out_stride", ctypes.c_int64),
-                ("h", ctypes.c_void_p), ("h_stride", ctypes.c_int64)]
-
-
-class LsLinearI8Args(ctypes.Structure):
-    _fields_ = [("n_tokens", ctypes.c_int32), ("k", ctypes.c_int32), ("n", ctypes.c_int32), ("x_type", ctypes.c_int),
-                ("out_type", ctypes.c_int), ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("x_scale", ctypes.c_void_p),
-                ("w", ctypes.c_void_p), ("w_stride", ctypes.c_int64), ("w_scale", ctypes.c_void_p), ("bias", ctypes.c_void_p),
-                ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64)]
-
-
-class LsKvCache(ctypes.Structure):
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int), ("n_pages", ctypes.c_int32),
-                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
-                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
-
-
-class LsAppendArgs(ctypes.Structure):
-    _fields_ = [("n_tokens", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("n_pos", ctypes.c_int32),
-                ("style", ctypes.c_int), ("k", ctypes.c_void_p), ("k_token_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
-                ("v", ctypes.c_void_p), ("v_token_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
-                ("q", ctypes.c_void_p), ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
-                ("q_out", ctypes.c_void_p), ("q_out_token_stride", ctypes.c_int64), ("q_out_head_stride", ctypes.c_int64),
-                ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("cos_sin", ctypes.c_void_p)]
-
-
-class LsAttendArgs(ctypes.Structure):
-    _fields_ = [("n_seqs", ctypes.c_int32), ("n_q", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("prefix_len", ctypes.c_int32),
-                ("max_len", ctypes.c_int32), ("scale", ctypes.c_float), ("q", ctypes.c_void_p), ("q_token_stride", ctypes.c_int64),
-                ("q_head_stride", ctypes.c_int64), ("out", ctypes.c_void_p), ("out_token_stride", ctypes.c_int64),
-                ("out_head_stride", ctypes.c_int64), ("prefix_pages", ctypes.c_void_p), ("pages", ctypes.c_void_p),
-                ("pages_stride", ctypes.c_int64), ("lens", ctypes.c_void_p)]
-
-
 class LsError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {message}")
@@ -178,10 +139,10 @@ def load():
     lib.ls_ops_destroy.argtypes = [P]
     lib.ls_ops_sync.argtypes = [P]
     lib.ls_ops_last_error.argtypes = [P]
-    lib.ls_norm_residual.argtypes = [P, ctypes.POINTER(LsNormArgs)]
-    lib.ls_linear_i8.argtypes = [P, ctypes.POINTER(LsLinearI8Args)]
-    lib.ls_kv_append.argtypes = [P, ctypes.POINTER(LsKvCache), ctypes.POINTER(LsAppendArgs)]
-    lib.ls_attend.argtypes = [P, ctypes.POINTER(LsKvCache), ctypes.POINTER(LsAttendArgs)]
+    for name in ("ls_norm_residual", "ls_linear_i8"):
+        getattr(lib, name).argtypes = [P, P]
+    for name in ("ls_kv_append", "ls_attend"):
+        getattr(lib, name).argtypes = [P, P, P]
     for name in OPS_EXPORTS:
         getattr(lib, name).restype = ctypes.c_char_p if name == "ls_ops_last_error" else ctypes.c_int
     for name in EXPORTS:
@@ -370,170 +331,35 @@ class Ffn:
         return n.value
 
 
-def _dtype(t, what: str, allowed) -> int:
-    """Library type of a tensor's elements."""
+_native = None
+
+
+def _load_native():
+    """Load the compiled module that marshals the operators' arguments (no fallback)."""
+    global _native
+    if _native is None:
+        load()
+        from . import build as _build
+        if not os.path.exists(_build.BINDING):
+            raise RuntimeError(f"{_build.BINDING} is missing (run __graft_entry__.build())")
+        import torch  # noqa: F401  (the module's symbols are torch's)
+        from . import _lsops
+        if _lsops.digest != _build.source_digest():
+            raise RuntimeError(f"{_build.BINDING} was built from other sources: rebuild it (__graft_entry__.build())")
+        _native = _lsops
+    return _native
+
+
+def Ops(*, workspace_bytes=0, stream=None):
+    """The decoder layer's operators around the FFN (``ls_ops.h``) on one stream: an object whose
+    methods mirror the C entry points (``ls_norm_residual``, ``ls_linear_i8``, ``ls_kv_append``,
+    ``ls_attend``, ``ls_ops_sync``; ``close`` releases it).  Sizes, strides and types are those of
+    the tensors they are given; a tensor that does not fit raises ``ValueError``, a call that the
+    library refuses ``LsError``."""
     import torch
-    ls = {torch.float32: LS_F32, torch.float16: LS_F16, torch.bfloat16: LS_BF16, torch.int8: LS_I8}.get(t.dtype)
-    if ls not in allowed:
-        raise ValueError(f"{what} has type {t.dtype}")
-    return ls
-
-
-def _strides(t, shape, what: str):
-    """Element strides of a device tensor of the given shape, 0 where a dimension has one entry
-    (and 1, not counted, for the last: it must be contiguous)."""
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if not t.is_cuda:
-        raise ValueError(f"{what} is not on the GPU")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{what} is not contiguous in its last dimension")
-    return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(t.dim() - 1)]
-
-
-class Ops:
-    """The decoder layer's operators around the FFN (``ls_ops.h``) on one stream.  Methods mirror
-    the C entry points; sizes, strides and types are those of the tensors they are given."""
-
-    def __init__(self, *, workspace_bytes=0, stream=None):
-        self.lib = load()
-        import torch
-        if stream is None:
-            stream = torch.cuda.current_stream()
-        self.torch_stream = stream
-        h = ctypes.c_void_p()
-        desc = LsOpsDesc(workspace_bytes, ctypes.c_void_p(stream.cuda_stream), 0)
-        self.ctx = None
-        self._check(self.lib.ls_ops_create(ctypes.byref(desc), ctypes.byref(h)))
-        self.ctx = h
-        _live.add(self)
-
-    def _check(self, status: int) -> None:
-        if status != LS_OK:
-            msg = self.lib.ls_ops_last_error(self.ctx)
-            raise LsError(status, msg.decode() if msg else "")
-
-    def close(self):
-        if getattr(self, "ctx", None):
-            self.lib.ls_ops_destroy(self.ctx)
-            self.ctx = None
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
-
-    def ls_ops_sync(self) -> None:
-        self._check(self.lib.ls_ops_sync(self.ctx))
-
-    def ls_norm_residual(self, x, *, y=None, gate=None, post_norm=False, post_weight=None, pre_norm=False, pre_weight=None,
-                         x_scale=1.0, y_scale=1.0, eps=1e-6, x_out=None, h=None) -> None:
-        """x, x_out: fp32 [T, d]; y, h: [T, d]; gate: [d] or [T, d]; the weights: [d]."""
-        T, d = x.shape
-        _dtype(x, "x", (LS_F32,))
-        (xs,) = _strides(x, (T, d), "x")
-        rest = [(t, n) for t, n in ((y, "y"), (h, "h"), (gate, "gate"), (post_weight, "post_weight"), (pre_weight, "pre_weight"))
-                if t is not None]
-        dt = _dtype(rest[0][0], rest[0][1], (LS_F32, LS_F16, LS_BF16)) if rest else LS_F32
-        for t, n in rest:
-            _dtype(t, n, (dt,))
-        ys = _strides(y, (T, d), "y")[0] if y is not None else 0
-        hs = _strides(h, (T, d), "h")[0] if h is not None else 0
-        gs = 0
-        if gate is not None:
-            gs = _strides(gate, (T, d), "gate")[0] if gate.dim() == 2 else 0 * len(_strides(gate, (d,), "gate"))
-        for t, n in ((post_weight, "post_weight"), (pre_weight, "pre_weight")):
-            if t is not None:
-                _strides(t, (d,), n)
-        os_ = 0
-        if x_out is not None:
-            _dtype(x_out, "x_out", (LS_F32,))
-            (os_,) = _strides(x_out, (T, d), "x_out")
-        a = LsNormArgs(T, d, dt, int(post_norm), int(pre_norm), x_scale, y_scale, eps, _ptr(x), xs, _ptr(y), ys, _ptr(gate), gs,
-                       _ptr(post_weight), _ptr(pre_weight), _ptr(x_out), os_, _ptr(h), hs)
-        self._check(self.lib.ls_norm_residual(self.ctx, ctypes.byref(a)))
-
-    def ls_linear_i8(self, x, w, w_scale, out, *, x_scale=None, bias=None) -> None:
-        """x: [T, k] int8 with x_scale fp32 [T], or floating; w: int8 [n, k]; w_scale, bias: fp32 [n]; out: [T, n]."""
-        T, k = x.shape
-        n = w.shape[0]
-        xt = _dtype(x, "x", (LS_I8, LS_F32, LS_F16, LS_BF16))
-        _dtype(w, "w", (LS_I8,))
-        ot = _dtype(out, "out", (LS_F32, LS_F16, LS_BF16))
-        (xs,), (ws,), (os_,) = _strides(x, (T, k), "x"), _strides(w, (n, k), "w"), _strides(out, (T, n), "out")
-        for t, shape, what in ((w_scale, (n,), "w_scale"), (bias, (n,), "bias"), (x_scale, (T,), "x_scale")):
-            if t is not None:
-                _dtype(t, what, (LS_F32,))
-                _strides(t, shape, what)
-        a = LsLinearI8Args(T, k, n, xt, ot, _ptr(x), xs, _ptr(x_scale), _ptr(w), ws, _ptr(w_scale), _ptr(bias), _ptr(out), os_)
-        self._check(self.lib.ls_linear_i8(self.ctx, ctypes.byref(a)))
-
-    @staticmethod
-    def _cache(k_cache, v_cache) -> LsKvCache:
-        """k_cache, v_cache: [n_pages, n_kv_heads, page_size, head_dim], of the same strides in any order."""
-        dt = _dtype(k_cache, "k_cache", (LS_F32, LS_F16, LS_BF16))
-        _dtype(v_cache, "v_cache", (dt,))
-        s = _strides(k_cache, k_cache.shape, "k_cache")
-        if _strides(v_cache, k_cache.shape, "v_cache") != s:
-            raise ValueError("k_cache and v_cache have different strides")
-        n, kv, page, d = k_cache.shape
-        return LsKvCache(_ptr(k_cache), _ptr(v_cache), dt, n, page, kv, d, *s)
-
-    def ls_kv_append(self, k_cache, v_cache, k, v, positions, slots, cos_sin, *, q=None, q_out=None, style=LS_ROPE_HALF) -> None:
-        """k, v: [T, n_kv_heads, head_dim]; q, q_out: [T, n_heads, head_dim]; positions, slots: int32 [T];
-        cos_sin: fp32 [n_pos, rot_dim], or None (with positions None) for a plain append."""
-        import torch
-        c = self._cache(k_cache, v_cache)
-        T = k.shape[0]
-        shape = (T, c.n_kv_heads, c.head_dim)
-        for t, what in ((k, "k"), (v, "v"), (q, "q"), (q_out, "q_out")):
-            if t is not None:
-                _dtype(t, what, (c.dtype,))
-        heads = 0 if q is None else q.shape[1]
-        qs, qos = [0, 0], [0, 0]
-        if q is not None:
-            qs = _strides(q, (T, heads, c.head_dim), "q")
-        if q_out is not None:
-            qos = _strides(q_out, (T, heads, c.head_dim), "q_out")
-        for t, what in ((positions, "positions"), (slots, "slots")):
-            if t is not None and (t.dtype != torch.int32 or _strides(t, (T,), what)):
-                raise ValueError(f"{what} must be int32")
-        n_pos = rot = 0
-        if cos_sin is not None:
-            n_pos, rot = cos_sin.shape
-            _dtype(cos_sin, "cos_sin", (LS_F32,))
-            if not cos_sin.is_contiguous():
-                raise ValueError("cos_sin is not contiguous")
-            _strides(cos_sin, (n_pos, rot), "cos_sin")
-        a = LsAppendArgs(T, heads, rot, n_pos, style, _ptr(k), *_strides(k, shape, "k"), _ptr(v), *_strides(v, shape, "v"),
-                         _ptr(q), *qs, _ptr(q_out), *qos, _ptr(positions), _ptr(slots), _ptr(cos_sin))
-        self._check(self.lib.ls_kv_append(self.ctx, ctypes.byref(c), ctypes.byref(a)))
-
-    def ls_attend(self, q, k_cache, v_cache, pages, lens, out, *, max_len, scale, n_q=1, prefix_pages=None, prefix_len=0) -> None:
-        """q, out: [n_seqs * n_q, n_heads, head_dim]; pages: int32 [n_seqs, pages of a sequence]; lens: int32 [n_seqs];
-        prefix_pages: int32 [pages of the prefix]; max_len: a bound of lens that the caller knows."""
-        import torch
-        c = self._cache(k_cache, v_cache)
-        T, heads, _ = q.shape
-        n_seqs = lens.shape[0]
-        _dtype(q, "q", (c.dtype,))
-        _dtype(out, "out", (c.dtype,))
-        if T != n_seqs * n_q:
-            raise ValueError(f"q has {T} tokens, expected {n_seqs} sequences of {n_q}")
-        qs, os_ = _strides(q, (T, heads, c.head_dim), "q"), _strides(out, (T, heads, c.head_dim), "out")
-        for t, what in ((pages, "pages"), (lens, "lens"), (prefix_pages, "prefix_pages")):
-            if t is not None and (t.dtype != torch.int32 or not t.is_cuda or (t.numel() > 0 and t.stride(-1) != 1)):
-                raise ValueError(f"{what} must be int32 on the GPU, contiguous in its last dimension")
-        if prefix_len > 0 and (prefix_pages is None or prefix_pages.numel() * c.page_size < prefix_len):
-            raise ValueError("prefix_pages hold fewer than prefix_len keys")
-        stride = 0
-        if pages is not None:
-            if pages.dim() != 2 or pages.shape[0] != n_seqs:
-                raise ValueError("pages must have a row for each sequence")
-            if pages.shape[1] * c.page_size < max_len:
-                raise ValueError("pages hold fewer than max_len keys")
-            stride = pages.stride(0) if n_seqs > 1 else pages.shape[1]
-        a = LsAttendArgs(n_seqs, n_q, heads, prefix_len, max_len, scale, _ptr(q), *qs, _ptr(out), *os_, _ptr(prefix_pages),
-                         _ptr(pages), stride, _ptr(lens))
-        self._check(self.lib.ls_attend(self.ctx, ctypes.byref(c), ctypes.byref(a)))
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    o = _load_native().Ops(workspace_bytes, stream.cuda_stream)
+    o.torch_stream = stream   # lives as long as the context that borrows it
+    _live.add(o)
+    return o

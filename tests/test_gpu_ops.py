@@ -660,3 +660,5 @@ def test_context_refusals():
                  lambda: lib.ls_attend(o.ctx, None, None)):
         assert call() == lsffn.LS_E_INVAL
     o.close()
+    o.close()  # a second time does nothing
+    refused(lambda: o.ls_norm_residual(torch.zeros((1, 8), device=DEV), x_out=torch.zeros((1, 8), device=DEV)))
