@@ -32,6 +32,8 @@ extern "C" {
 
 typedef struct ls_ops ls_ops; /* opaque context; owns the workspace */
 
+#define LS_I8 ((ls_dtype)3) /* 8-bit integers: inputs of ls_linear_i8 only */
+
 #define LS_OPS_WORKSPACE_DEFAULT (256ull << 20)
 
 typedef struct {

@@ -35,8 +35,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(1))) void* gptr;
 typedef __attribute__((address_space(3))) void* lptr;
 
-// What masked keys and the padding of a head are read from.
-__device__ const uint32_t g_zero_chunk[4] = {0, 0, 0, 0};
+// What masked keys and the padding of a head are read from: a row of zeros.
+__device__ const uint32_t g_zero_row[128] = {};
 
 template <typename T>
 using vec8 = std::conditional_t<std::is_same_v<T, _Float16>, f16x8, bf16x8>;
@@ -86,7 +86,7 @@ struct Shape {
     static constexpr int CPR = DP / 8;                          // chunks per row
     static constexpr int RPI = 64 / CPR;                        // rows per copy instruction
     static constexpr int kRows = WIDE ? KT / NW : KT;           // rows a wave copies
-    static constexpr int kBuf = (WIDE ? 1 : NW) * KT * DP * 2;  // elements of a buffer: keys, then values
+    static constexpr int kBuf = (WIDE ? 1 : NW) * KT * DP;      // elements of a buffer, of keys or of values
     static constexpr int kTileRows = WIDE ? 128 : 32;
 };
 
@@ -105,10 +105,13 @@ template <typename T, int DP, bool WIDE>
 __device__ inline bool item_of(const AttendP& p, int b, Item* it) {
     constexpr int R = Shape<T, DP, WIDE>::kTileRows;
     if (b < p.pre_items) {
-        it->row0 = b % p.plan.pre_tiles * R;
-        b /= p.plan.pre_tiles;
-        it->kv = b % p.KV;
-        it->part = b / p.KV;
+        // workgroups that follow each other run on different XCDs: the row tiles of the same keys
+        // take every eighth workgroup, so that they share an L2
+        const int group = b / (8 * p.plan.pre_tiles) * 8 + b % 8;
+        if (group >= p.plan.pre_parts * p.KV) return false;
+        it->row0 = b / 8 % p.plan.pre_tiles * R;
+        it->kv = group % p.KV;
+        it->part = group / p.KV;
         it->seq = -1;
         it->table = p.prefix_pages;
         it->len = p.prefix_len;
@@ -133,13 +136,17 @@ __device__ inline bool item_of(const AttendP& p, int b, Item* it) {
     return it->begin < it->end || p.direct;
 }
 
-template <typename T, int DP, bool WIDE>
-__global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 ? 2 : 1)) void attend_kernel(const AttendP p) {
+// MULTI: sequences with several query tokens each, whose last keys only some of them see.
+template <typename T, int DP, bool WIDE, bool MULTI>
+__global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 && !MULTI ? 2 : 1)) void attend_kernel(const AttendP p) {
     using Sh = Shape<T, DP, WIDE>;
+    constexpr bool PIPE = WIDE && !MULTI;  // scores one tile ahead (MULTI's rare path leaves no registers)
     constexpr int NW = Sh::NW, KT = Sh::KT, CPR = Sh::CPR, NF = DP / 16, ND = DP / 32, SUB = KT / 32;
-    // two arrays, not one: a read of one buffer must not wait for the copy into the other
-    __shared__ __attribute__((aligned(16))) T buf0[Sh::kBuf];
-    __shared__ __attribute__((aligned(16))) T buf1[Sh::kBuf];
+    // four arrays, not one: a read of one must not wait for the copy into another
+    __shared__ __attribute__((aligned(16))) T k0[Sh::kBuf];
+    __shared__ __attribute__((aligned(16))) T k1[Sh::kBuf];
+    __shared__ __attribute__((aligned(16))) T v0[Sh::kBuf];
+    __shared__ __attribute__((aligned(16))) T v1[Sh::kBuf];
     __shared__ float wave_ml[NW][2][32];
     __shared__ float row_sum[32];
     Item it;
@@ -155,7 +162,8 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 ?
     const int64_t token = it.seq < 0 ? tk : (int64_t)it.seq * p.n_q + tk;
     const int head = it.kv * p.G + g;
     const int limit = it.seq < 0 ? it.end : min(it.end, it.len - p.n_q + 1 + tk);
-    const int full = it.seq < 0 ? it.end : it.len - p.n_q + 1;  // keys below are seen by every row
+    // keys below are seen by every row (of a sequence; of its part)
+    const int full_len = it.seq < 0 ? it.end : it.len - p.n_q + 1, full = min(it.end, full_len);
 
     vec8<T> q[NF];
     {
@@ -173,93 +181,122 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 ?
 
     const T* kbase = static_cast<const T*>(p.k) + it.kv * p.head_stride;
     const T* vbase = static_cast<const T*>(p.v) + it.kv * p.head_stride;
-    const T* zero = reinterpret_cast<const T*>(g_zero_chunk);
+    const T* zero = reinterpret_cast<const T*>(g_zero_row);
     const int page_mask = (1 << p.page_shift) - 1;
 
-    // page of key (tile + lane), -1 where there is none
-    auto page_ids = [&](int key0) {
+    // The page id of key (tile + lane), -1 where there is none; then its place in the cache, in
+    // elements, -1 where the key is masked.  Each lane does one key of the tile.
+    auto page_id = [&](int key0) {
         const int key = key0 + (lane & (KT - 1));
-        int id = -1;
-        if (key < it.end) id = it.table[key >> p.page_shift];
-        return (unsigned)id < (unsigned)p.n_pages ? id : -1;
+        return key < it.end ? it.table[key >> p.page_shift] : -1;
     };
-    auto copy = [&](int key0, int ids, T* buf) {
-        T* kd = buf + (WIDE ? wave * Sh::kRows * DP : wave * KT * DP * 2);
-        T* vd = kd + KT * DP;
+    auto place = [&](int key0, int id) {
+        const int key = key0 + (lane & (KT - 1));
+        const int64_t at = (int64_t)id * p.page_stride + (int64_t)(key & page_mask) * p.token_stride;
+        return (unsigned)id < (unsigned)p.n_pages ? at : (int64_t)-1;
+    };
+    // Copies a tile's rows, RPI of them an instruction: lane -> row lane / CPR, chunk lane % CPR permuted.
+    const int c_row = lane / CPR;
+    auto copy = [&](const T* base, int64_t at, T* buf) {
+        T* dst = buf + wave * Sh::kRows * DP;
+        const uint64_t from = (uint64_t)(at < 0 ? zero : base + at);
 #pragma unroll
         for (int i = 0; i < Sh::kRows / Sh::RPI; ++i) {
-            const int r = (WIDE ? wave * Sh::kRows : 0) + i * Sh::RPI + lane / CPR;
-            const int chunk = (lane % CPR) ^ swz<CPR>(r);
-            const int id = __shfl(ids, r, 64);
-            const bool ok = id >= 0 && chunk * 8 < p.D;
-            const int64_t at = (int64_t)max(id, 0) * p.page_stride + (int64_t)((key0 + r) & page_mask) * p.token_stride + chunk * 8;
-            __builtin_amdgcn_global_load_lds((gptr)(ok ? kbase + at : zero), (lptr)(kd + i * 512), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((gptr)(ok ? vbase + at : zero), (lptr)(vd + i * 512), 16, 0, 0);
+            const int r0 = (WIDE ? wave * Sh::kRows : 0) + i * Sh::RPI;
+            const int chunk = (lane % CPR) ^ swz<CPR>(c_row) ^ swz<CPR>(r0);  // the bits of the two do not mix
+            const uint32_t lo = __shfl((uint32_t)from, r0 + c_row, 64), hi = __shfl((uint32_t)(from >> 32), r0 + c_row, 64);
+            const T* row = reinterpret_cast<const T*>(((uint64_t)hi << 32) | lo);
+            __builtin_amdgcn_global_load_lds((gptr)(chunk * 8 < p.D ? row + chunk * 8 : zero), (lptr)(dst + i * 512), 16, 0, 0);
         }
     };
-    auto use = [&](int key0, int ids, const T* buf) {
-        if (WIDE && it.row0 + wave * 32 >= it.rows) return;  // no rows: this wave only copies
-        const T* kt = buf + (WIDE ? 0 : wave * KT * DP * 2);
-        const T* vt = kt + KT * DP;
-        f32x16 s[SUB];
-#pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            s[u] = f32x16{};
-#pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                const auto k = *reinterpret_cast<const vec8<T>*>(kt + (u * 32 + n) * DP + (((2 * f + h) ^ swz<CPR>(n)) * 8));
-                s[u] = mma(k, q[f], s[u]);
-            }
-        }
-        // score i of a lane belongs to key 8 (i / 4) + 4 h + i % 4 of its 32
-        const uint64_t valid = __ballot(ids >= 0);
-        const bool whole = key0 + KT <= full && key0 + KT <= it.end && (KT == 64 ? ~valid == 0 : (uint32_t)~valid == 0);
-        if (!whole) {
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = u * 32 + 8 * (i / 4) + 4 * h + i % 4;
-                    if (key0 + key >= limit || !((valid >> key) & 1)) s[u][i] = -INFINITY;
-                }
-        }
-        float top = s[0][0];
+    // Where this lane finds its operands in a tile, in elements: key u * 32 + n, chunk 2 f + h; and for
+    // the values element d = 32 t + n of keys 16 kk + 4 h + 0 .. 3 and + 8 (read by fours, transposed).
+    const int k_at = n * DP + (h ^ swz<CPR>(n)) * 8;  // chunk bits of f are flipped in
+    const int r4 = (lane & 15) >> 2, col = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    const int v_at = (4 * h + r4) * DP + (col ^ swz<CPR>(4 * h + r4)) * 8 + (lane & 1) * 4;
+    const int v_at8 = (4 * h + r4 + 8) * DP + (col ^ swz<CPR>(4 * h + r4 + 8)) * 8 + (lane & 1) * 4;
+    const bool idle_wave = WIDE && it.row0 + wave * 32 >= it.rows;  // no rows: it only copies
+    struct Scores {
+        f32x16 u[SUB];
+        float top;  // the largest of the lane's
+    };
+    auto largest = [](Scores& s) {
+        float top = s.u[0][0];
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s.u[u][i]);
+        s.top = top;
+    };
+    auto scores = [&](const T* buf) {
+        const T* kt = buf + (WIDE ? 0 : wave * KT * DP);
+        Scores s;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) s.u[u] = f32x16{};
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+                s.u[u] = mma(*reinterpret_cast<const vec8<T>*>(kt + (k_at ^ (f * 16)) + u * 32 * DP), q[f], s.u[u]);
+        return s;
+    };
+    // One tile.  PIPE: its scores are in s already, and those of the next tile (keys in kbuf) are
+    // computed while its exponentials are: matrix and vector instructions of one wave run side by
+    // side, so the next copies and the next maximum are part of the same stretch of code.
+    auto use = [&](Scores& s, int key0, int64_t at, const T* vbuf, const T* kbuf, auto&& copies) {
+        if (!PIPE) {
+            s = scores(kbuf);
+            largest(s);
+        }
+        const T* vt = vbuf + (WIDE ? 0 : wave * KT * DP);
+        // score i of a lane belongs to key 8 (i / 4) + 4 h + i % 4 of its 32
+        const uint64_t valid = __ballot(at >= 0);
+        if (key0 + KT > full || (KT == 64 ? ~valid != 0 : (uint32_t)~valid != 0)) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                const int left = limit - key0 - u * 32;  // keys of these 32 that the row sees
+                const uint32_t below = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
+                const uint32_t seen = (below & (uint32_t)(valid >> (u * 32))) >> (4 * h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s.u[u][i] = (seen >> (8 * (i / 4) + i % 4)) & 1 ? s.u[u][i] : -INFINITY;
+            }
+            largest(s);
+        }
+        const float top = fmaxf(s.top, __shfl_xor(s.top, 32, 64));
         const float next = fmaxf(m, top), base = next == -INFINITY ? 0.f : next * p.c;
         if (__any(next > m)) {
-            const float scale = __builtin_amdgcn_exp2f(m * p.c - base);  // m = -inf: 0
+            const float scale = __builtin_amdgcn_exp2f(fmaf(m, p.c, -base));  // m = -inf: 0
             l *= scale;
 #pragma unroll
             for (auto& x : o) x *= scale;
             m = next;
+        }
+        Scores after;
+        if (PIPE) {
+            copies();
+            after = scores(kbuf);
         }
         vec8<T> pr[2 * SUB];
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[u][i], p.c, -base));
+                const float e = __builtin_amdgcn_exp2f(fmaf(s.u[u][i], p.c, -base));
                 l += e;
                 pr[2 * u + i / 8][i % 8] = (T)e;
             }
-        // values: lane -> element d = 32 t + n, keys 16 kk + 8 (j / 4) + 4 h + j % 4
         auto value = [&](int kk, int t) {
-            const int r4 = (lane & 15) >> 2, col = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), byte = (lane & 1) * 4;
-            const int r0 = 16 * kk + 4 * h + r4, r1 = r0 + 8;
             typedef __attribute__((address_space(3))) s16x4* lds4;
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vt + r0 * DP + ((t * 4 + col) ^ swz<CPR>(r0)) * 8 + byte));
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vt + r1 * DP + ((t * 4 + col) ^ swz<CPR>(r1)) * 8 + byte));
+            const T* at = vt + kk * 16 * DP;
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + (v_at ^ (t * 32))));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + (v_at8 ^ (t * 32))));
             struct { s16x4 a, b; } both{x, y};
             return __builtin_bit_cast(vec8<T>, both);
         };
+        bool odd = false;
         // Where later tokens of a sequence see keys that earlier ones do not, a weight of zero must
         // also keep out a value that is no number: only then are the tokens taken one by one.
-        if (it.seq >= 0 && p.n_q > 1 && key0 + KT > full) {
-            bool odd = false;
+        if (MULTI && it.seq >= 0 && key0 + KT > full) {
 #pragma unroll 1
             for (int kk = 0; kk < 2 * SUB; ++kk)
 #pragma unroll 1
@@ -269,32 +306,37 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 ?
                     for (int j = 0; j < 8; ++j)
                         odd |= key0 + 16 * kk + 8 * (j / 4) + 4 * h + j % 4 >= full && !(fabsf((float)v[j]) < INFINITY);
                 }
-            if (__any(odd)) {
-#pragma unroll 1
-                for (int i = 0; i < p.n_q; ++i) {
-                    const int seen = full + i;
-#pragma unroll
-                    for (int t = 0; t < ND; ++t) {
-                        f32x16 x = o[t];
-#pragma unroll
-                        for (int kk = 0; kk < 2 * SUB; ++kk) {
-                            auto v = value(kk, t);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (key0 + 16 * kk + 8 * (j / 4) + 4 * h + j % 4 >= seen) v[j] = (T)0.f;
-                            x = mma(v, pr[kk], x);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[t][e] = tk == i ? x[e] : o[t][e];
-                    }
-                }
-                return;
-            }
         }
+        if (MULTI && __any(odd)) {
+#pragma unroll 1
+            for (int i = 0; i < p.n_q; ++i) {
+                const int seen = full_len + i;
 #pragma unroll
-        for (int kk = 0; kk < 2 * SUB; ++kk)
+                for (int t = 0; t < ND; ++t) {
+                    __builtin_amdgcn_sched_barrier(0);  // one tile's operands at a time: registers
+                    f32x16 x = o[t];
 #pragma unroll
-            for (int t = 0; t < ND; ++t) o[t] = mma(value(kk, t), pr[kk], o[t]);
+                    for (int kk = 0; kk < 2 * SUB; ++kk) {
+                        auto v = value(kk, t);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (key0 + 16 * kk + 8 * (j / 4) + 4 * h + j % 4 >= seen) v[j] = (T)0.f;
+                        x = mma(v, pr[kk], x);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[t][e] = tk == i ? x[e] : o[t][e];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < 2 * SUB; ++kk)
+#pragma unroll
+                for (int t = 0; t < ND; ++t) o[t] = mma(value(kk, t), pr[kk], o[t]);
+        }
+        if (PIPE) {
+            s = after;
+            largest(s);
+        }
     };
     auto landed = [&] {
         __builtin_amdgcn_s_waitcnt(0x0070);  // this wave's copies are in shared memory, its reads done
@@ -303,26 +345,42 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 ?
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
     };
 
+    // While tile j is used, V of j + 1 and K of j + 1 (PIPE: j + 2) arrive.  Past the end PIPE
+    // copies and multiplies tiles of zeros; nothing uses their scores.
     constexpr int kStep = WIDE ? KT : NW * KT;
     int key = it.begin + (WIDE ? 0 : wave * KT);
-    int ids = page_ids(key), ids1 = page_ids(key + kStep);
-    if (key < it.end) copy(key, ids, buf0);
-    while (key < it.end) {
-        landed();
-        if (key + kStep < it.end) copy(key + kStep, ids1, buf1);
-        int ids2 = page_ids(key + 2 * kStep);
-        use(key, ids, buf0);
-        key += kStep;
-        ids = ids1;
-        ids1 = ids2;
-        if (key >= it.end) break;
-        landed();
-        if (key + kStep < it.end) copy(key + kStep, ids1, buf0);
-        ids2 = page_ids(key + 2 * kStep);
-        use(key, ids, buf1);
-        key += kStep;
-        ids = ids1;
-        ids1 = ids2;
+    if (key < it.end) {
+        int64_t at0 = place(key, page_id(key)), at1 = place(key + kStep, page_id(key + kStep));
+        int id2 = page_id(key + 2 * kStep);
+        copy(kbase, at0, k0);
+        copy(vbase, at0, v0);
+        Scores s;
+        if (PIPE) {
+            copy(kbase, at1, k1);
+            landed();
+            s = scores(k0);
+            largest(s);
+        }
+        auto tile = [&](T* ka, T* kb, T* va, T* vb) {  // K of j + 1 in kb (else of j in ka), V of j in va
+            const int64_t at2 = place(key + 2 * kStep, id2);
+            landed();
+            id2 = page_id(key + 3 * kStep);
+            auto copies = [&] {
+                copy(kbase, PIPE ? at2 : at1, PIPE ? ka : kb);
+                copy(vbase, at1, vb);
+            };
+            if (PIPE ? idle_wave : key + kStep < it.end) copies();
+            if (!idle_wave) use(s, key, at0, va, PIPE ? kb : ka, copies);
+            key += kStep;
+            at0 = at1, at1 = at2;
+        };
+        for (;;) {
+            tile(k0, k1, v0, v1);
+            if (key >= it.end) break;
+            tile(k1, k0, v1, v0);
+            if (key >= it.end) break;
+        }
+        landed();  // nothing is under way when the arrays are used again
     }
     l += __shfl_xor(l, 32, 64);
 
@@ -375,8 +433,12 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 ?
         const float wl = wave_ml[w][1][n];
         if (wl != 0.f) sum += wl * __builtin_amdgcn_exp2f(fmaf(wave_ml[w][0][n], p.c, -base));
     }
-    float* joined = reinterpret_cast<float*>(buf0);  // [wave][row][DP], 16-byte chunks permuted by the row
-    static_assert(WIDE || sizeof(buf0) >= NW * 32 * DP * 4, "room for the waves' sums");
+    // [wave][row][DP], 16-byte chunks permuted by the row: half of each row in the keys' array, half in the values'
+    static_assert(WIDE || Sh::kBuf * sizeof(T) >= NW * 32 * DP / 2 * 4, "room for the waves' sums");
+    auto joined = [&](int w, int r, int chunk) {
+        const int c = chunk ^ (r & (DP / 4 - 1)), half = DP / 8;
+        return reinterpret_cast<f32x4*>(c < half ? k0 : v0) + (w * 32 + r) * half + c % half;
+    };
     if (row_ok) {
         const float scale = __builtin_amdgcn_exp2f(fmaf(m, p.c, -base));
 #pragma unroll
@@ -387,7 +449,7 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 ?
                 f32x4 v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : o[t][i + e] * scale;
-                *reinterpret_cast<f32x4*>(joined + (wave * 32 + n) * DP + (chunk ^ (n & (DP / 4 - 1))) * 4) = v;
+                *joined(wave, n, chunk) = v;
             }
         if (wave == 0 && h == 0) {
             row_sum[n] = sum;
@@ -400,7 +462,7 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 ?
         const int r = i / (DP / 4), chunk = i % (DP / 4);
         f32x4 v{};
 #pragma unroll
-        for (int w = 0; w < NW; ++w) v += *reinterpret_cast<const f32x4*>(joined + (w * 32 + r) * DP + (chunk ^ (r & (DP / 4 - 1))) * 4);
+        for (int w = 0; w < NW; ++w) v += *joined(w, r, chunk);
         const int tr = (it.row0 + r) / p.G;
         put(it.seq < 0 ? tr : (int64_t)it.seq * p.n_q + tr, it.kv * p.G + (it.row0 + r) % p.G, chunk * 4, v, row_sum[r]);
     }
@@ -477,16 +539,21 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_attend_args& a, const Atte
     const int64_t rows = (int64_t)p.S * p.n_q * p.H;
     p.part = static_cast<float*>(ws);
     p.ml = p.part + rows * p.parts * p.D;
-    const int pre = plan.pre_parts * p.KV * plan.pre_tiles, suf = plan.suf_parts * p.S * p.KV * plan.suf_tiles;
+    const int pre = (int)round_up(plan.pre_parts * p.KV, 8) * plan.pre_tiles, suf = plan.suf_parts * p.S * p.KV * plan.suf_tiles;
     auto go = [&](bool wide, int pre_items, int suf_items) {
         p.pre_items = pre_items;
         p.suf_items = suf_items;
         if (pre_items + suf_items == 0) return hipSuccess;
-        const dim3 grid((unsigned)(pre_items + suf_items));
-        if (wide)
-            hipLaunchKernelGGL((attend_kernel<T, DP, true>), grid, dim3(Shape<T, DP, true>::NW * 64), 0, st, p);
+        const dim3 grid((unsigned)(pre_items + suf_items)), wide_wg(Shape<T, DP, true>::NW * 64), narrow_wg(Shape<T, DP, false>::NW * 64);
+        const bool multi = p.n_q > 1 && suf_items;
+        if (wide && multi)
+            hipLaunchKernelGGL((attend_kernel<T, DP, true, true>), grid, wide_wg, 0, st, p);
+        else if (wide)
+            hipLaunchKernelGGL((attend_kernel<T, DP, true, false>), grid, wide_wg, 0, st, p);
+        else if (multi)
+            hipLaunchKernelGGL((attend_kernel<T, DP, false, true>), grid, narrow_wg, 0, st, p);
         else
-            hipLaunchKernelGGL((attend_kernel<T, DP, false>), grid, dim3(Shape<T, DP, false>::NW * 64), 0, st, p);
+            hipLaunchKernelGGL((attend_kernel<T, DP, false, false>), grid, narrow_wg, 0, st, p);
         return hipGetLastError();
     };
     hipError_t e;
@@ -531,7 +598,7 @@ bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes,
         for (int64_t chunk = 128;; chunk = std::min(most, chunk + std::max<int64_t>(128, chunk / 8 / 128 * 128))) {
             const int64_t pp = ceil_div(pre_keys, chunk), sp = ceil_div(suf_keys, chunk);
             const bool fits = pp <= kMaxParts / 2 && sp <= kMaxParts / 2 && std::max(pp, sp) * part_bytes <= (int64_t)ws_bytes / 2 &&
-                              n_pre * pp + n_suf * sp < (int64_t)1 << 31;
+                              (n_pre + 8) * (pp + 8) + n_suf * sp < (int64_t)1 << 31;
             if (fits) {
                 const double t = (double)ceil_div(n_pre * pp + n_suf * sp, n_slots) * (chunk + kStart);
                 if (!best || t < least) best = chunk, least = t;
