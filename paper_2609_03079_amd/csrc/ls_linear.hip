@@ -6,6 +6,7 @@
 // |sum| < 2^31 for k < 2^17), so neither the order of the sum nor the kernel chosen changes a bit
 // of the result; the two scales and the bias are applied once, in fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "ls_device.h"
 #include "ls_ops_internal.h"
@@ -32,7 +33,16 @@ struct LinearP {
     void* out;
     int64_t out_stride;
     int T, k, n;
+    int slices, splits;  // tiles: 64-byte slices of k per split; splits of k
+    int32_t* part;       // [splits][T][n] sums of the splits
 };
+
+// Rows that the kernel of one or two tokens holds in shared memory, and tokens that it quantises
+// itself, each workgroup anew: up to 8192 elements (a launch of its own takes 3 us more).
+constexpr int kVecMax = 16384;
+inline bool quantised_on_the_way(const ls_linear_i8_args& a) {
+    return a.x_type != LS_I8 && a.n_tokens <= 2 && (int64_t)a.n_tokens * a.k <= 8192;
+}
 
 template <typename O>
 __device__ inline void put(const LinearP& p, int t, int n, int acc, float s) {
@@ -63,84 +73,103 @@ __device__ inline float token_scale(uint32_t m, float* top) {
     return none ? 0.f : s;
 }
 
-// 127 x / max with one rounding of the quotient: for 16-bit x the product is exact, so this is
-// the definition's value (multiplying by a rounded 127 / max could move a tie).
-__device__ inline int quantise(float x, float top) {
-    return top > 0.f ? (int)rintf(x * 127.f / top) : 0;
+// round(127 x / max), ties to even.  The product with the rounded inverse is off by less than 1e-4,
+// so away from a tie it rounds to the same integer; near one the quotient decides (for 16-bit x
+// 127 x is exact and the quotient rounded once, so a tie is seen as one).  A division for every
+// element made the kernel twice as slow (2048 x 8192 bfloat16: 17.5 us).
+__device__ inline int quantise(float x, float top, float inv) {
+    const float p = x * inv;
+    float r = rintf(p);
+    if (fabsf(p - r) > 0.4999f) r = rintf(x * 127.f / top);
+    return (int)r;
 }
 
-// One workgroup per token; 16 elements per thread and step.
+// One workgroup per token; 8 elements per thread and step.
 template <typename T>
 __global__ __launch_bounds__(256) void quantise_kernel(const void* x, int64_t x_stride, int k, int8_t* q, float* s) {
     __shared__ uint32_t part[4];
     const int64_t t = blockIdx.x;
     const T* row = static_cast<const T*>(x) + t * x_stride;
-    constexpr int kHeld = 4;  // vectors a thread keeps in registers (rows of up to 16384 elements)
-    Pack<T, 16> v[kHeld];
+    constexpr int kHeld = 8, kStep = 256 * 8;  // vectors a thread keeps in registers (rows of up to 16384 elements)
+    Pack<T, 8> v[kHeld];
     uint32_t m = 0;
-    const int step = 256 * 16;
 #pragma unroll
     for (int c = 0; c < kHeld; ++c) {
-        const int e = (int)threadIdx.x * 16 + c * step;
-        if (e < k) {
-            v[c] = load_pack<T, 16>(row, e);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) m = max(m, magnitude((float)v[c].e[i]));
-        }
+        const int e = (int)threadIdx.x * 8 + c * kStep;
+        if (e < k) v[c] = load_pack<T, 8>(row, e);
     }
-    for (int e = (int)threadIdx.x * 16 + kHeld * step; e < k; e += step) {
-        const auto u = load_pack<T, 16>(row, e);
+    auto look = [&](const Pack<T, 8>& u) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) m = max(m, magnitude((float)u.e[i]));
-    }
+        for (int i = 0; i < 8; ++i) m = max(m, magnitude((float)u.e[i]));
+    };
+#pragma unroll
+    for (int c = 0; c < kHeld; ++c)
+        if ((int)threadIdx.x * 8 + c * kStep < k) look(v[c]);
+    for (int e = (int)threadIdx.x * 8 + kHeld * kStep; e < k; e += kStep) look(load_pack<T, 8>(row, e));
     m = wave_max(m);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
     __syncthreads();
     m = max(max(part[0], part[1]), max(part[2], part[3]));
     float top;
-    const float scale = token_scale(m, &top);
+    const float scale = token_scale(m, &top), inv = top > 0.f ? 127.f / top : 0.f;
     if (threadIdx.x == 0) s[t] = scale;
-    auto write = [&](int e, const Pack<T, 16>& u) {
-        Pack<int8_t, 16> o;
+    auto write = [&](int e, const Pack<T, 8>& u) {
+        Pack<int8_t, 8> o;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o.e[i] = (int8_t)quantise((float)u.e[i], top);
-        store_pack<int8_t, 16>(q, t * k + e, o);
+        for (int i = 0; i < 8; ++i) o.e[i] = top > 0.f ? (int8_t)quantise((float)u.e[i], top, inv) : (int8_t)0;
+        store_pack<int8_t, 8>(q, t * k + e, o);
     };
 #pragma unroll
     for (int c = 0; c < kHeld; ++c) {
-        const int e = (int)threadIdx.x * 16 + c * step;
+        const int e = (int)threadIdx.x * 8 + c * kStep;
         if (e < k) write(e, v[c]);
     }
-    for (int e = (int)threadIdx.x * 16 + kHeld * step; e < k; e += step) write(e, load_pack<T, 16>(row, e));
+    for (int e = (int)threadIdx.x * 8 + kHeld * kStep; e < k; e += kStep) write(e, load_pack<T, 8>(row, e));
 }
 
 // ---- tiles through shared memory -----------------------------------------------------------
 // out tile of BM tokens by BN channels; WM x WN waves, each with a (BM / WM) x (BN / WN) part in
-// 32 x 32 matrix tiles.  Both operands come in 128-byte slices of k, copied straight to shared
-// memory two slices deep: slice i + 1 arrives while slice i is multiplied.  A row's eight 16-byte
-// chunks lie at places permuted by its number, so that the 16 rows a read touches together lie in
-// different banks.
-constexpr int kSlice = 128;
+// 32 x 32 matrix tiles.  Both operands come in 64-byte slices of k, copied straight to a ring of
+// four slices in shared memory: a copy takes 1 to 2 us under load and a slice is multiplied in a
+// quarter of that, so three slices are under way while one is used.  (Two slices of 128 bytes, with
+// one under way, took 1.8 us a slice on the 128 x 128 tile, whose products take 0.5.)
+// A row's four 16-byte chunks lie at places permuted by its number, so that the 16 rows a read
+// touches together lie in different banks.
+constexpr int kSlice = 64;
 
-__device__ inline int place(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
+__device__ inline int place(int row, int chunk) { return chunk ^ ((row >> 2) & 3); }
 
+// A workgroup's copies of ROWS rows, slice by slice: 16 rows an instruction.
 template <int ROWS, int WAVES>
-__device__ inline void fetch(const int8_t* base, int64_t stride, int row0, int rows, int k, int k0, int8_t* lds) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    static_assert(ROWS % (8 * WAVES) == 0, "whole instructions");
+struct Fetch {
+    static constexpr int N = ROWS / (16 * WAVES);
+    static_assert(ROWS % (16 * WAVES) == 0, "whole instructions");
+    const int8_t* src[N];  // this lane's chunk of a slice at 0
+
+    __device__ inline void start(const int8_t* base, int64_t stride, int row0, int rows) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int i = 0; i < ROWS / (8 * WAVES); ++i) {
-        const int r0 = (i * WAVES + wave) * 8, r = r0 + (lane >> 3);
-        const int at = k0 + place(r, lane & 7) * 16;
-        const int8_t* src = base + (int64_t)min(row0 + r, rows - 1) * stride + at;
-        if (at >= k) src = reinterpret_cast<const int8_t*>(g_zero_chunk);
-        __builtin_amdgcn_global_load_lds((gptr)src, (lptr)(lds + r0 * kSlice), 16, 0, 0);
+        for (int i = 0; i < N; ++i) {
+            const int r = (i * WAVES + wave) * 16 + (lane >> 2);
+            src[i] = base + (int64_t)min(row0 + r, rows - 1) * stride + place(r, lane & 3) * 16;
+        }
     }
-}
+    // The slice at k0, of which bytes below `last` count.
+    __device__ inline void copy(int k0, int last, int8_t* lds) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r0 = (i * WAVES + wave) * 16;
+            const int8_t* from = src[i] + k0;
+            if (k0 + kSlice > last && k0 + place(r0 + (lane >> 2), lane & 3) * 16 >= last) from = reinterpret_cast<const int8_t*>(g_zero_chunk);
+            __builtin_amdgcn_global_load_lds((gptr)from, (lptr)(lds + r0 * kSlice), 16, 0, 0);
+        }
+    }
+};
 
 template <int BM, int BN, int WM, int WN>
 struct Tile {
-    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32, kWaves = WM * WN;
+    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
     i32x16 acc[TM][TN];
 
     __device__ inline void multiply(const int8_t* a, const int8_t* b) {
@@ -164,40 +193,64 @@ struct Tile {
     }
 };
 
+// All but this wave's newest N copies have landed, its reads of shared memory are done, and so for
+// the other waves.
+template <int N>
 __device__ inline void arrive() {
-    __builtin_amdgcn_s_waitcnt(0x0070);  // this wave's copies have landed, its reads are done
+    static_assert(N < 64, "the counter");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     __builtin_amdgcn_s_barrier();
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 
+// k in p.splits parts, one workgroup each (blockIdx.y): where the tiles alone would leave compute
+// units idle.  Their sums meet in finish_kernel.
 template <typename O, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const LinearP p, int tiles_n) {
-    // four arrays, not one: a read of one slice must not wait for the copy into the other
-    __shared__ __attribute__((aligned(16))) int8_t a0[BM * kSlice];
-    __shared__ __attribute__((aligned(16))) int8_t a1[BM * kSlice];
-    __shared__ __attribute__((aligned(16))) int8_t b0[BN * kSlice];
-    __shared__ __attribute__((aligned(16))) int8_t b1[BN * kSlice];
+__global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void tile_kernel(const LinearP p, int tiles_n) {
+    // eight arrays, not one: a read of one slice must not wait for the copies into the others
+    __shared__ __attribute__((aligned(16))) int8_t a0[BM * kSlice], a1[BM * kSlice], a2[BM * kSlice], a3[BM * kSlice];
+    __shared__ __attribute__((aligned(16))) int8_t b0[BN * kSlice], b1[BN * kSlice], b2[BN * kSlice], b3[BN * kSlice];
     const int t0 = (blockIdx.x / tiles_n) * BM, n0 = (blockIdx.x % tiles_n) * BN;
+    const int first = blockIdx.y * p.slices * kSlice, last = min(p.k, first + p.slices * kSlice);
     Tile<BM, BN, WM, WN> tile;
 #pragma unroll
     for (auto& r : tile.acc)
         for (auto& v : r) v = i32x16{};
     constexpr int W = WM * WN;
-    auto copy = [&](int k0, int8_t* a, int8_t* b) {
-        fetch<BM, W>(p.q, p.q_stride, t0, p.T, p.k, k0, a);
-        fetch<BN, W>(p.w, p.w_stride, n0, p.n, p.k, k0, b);
+    Fetch<BM, W> fa;
+    Fetch<BN, W> fb;
+    fa.start(p.q, p.q_stride, t0, p.T);
+    fb.start(p.w, p.w_stride, n0, p.n);
+    constexpr int kCopies = fa.N + fb.N;  // of a slice, by each wave
+    // Slices are taken in turn from one that depends on the workgroup (rows a power of two apart would
+    // all ask the same memory channel at once: 2048 x 8192 x 10240 241 -> 223 us), and past the end
+    // slices of zeros: the count under way stays the same, and the ring's four steps are one loop
+    // without exits (whose copies of the sums cost more than the products).
+    const int n_slices = (last - first + kSlice - 1) / kSlice;
+    const int turn = (int)(blockIdx.x % tiles_n / 8 % 4) * 4 % n_slices;
+    auto copy = [&](int i, int8_t* a, int8_t* b) {
+        int at = i + turn;
+        at -= at >= n_slices ? n_slices : 0;
+        const int k0 = i < n_slices ? first + at * kSlice : last;
+        fa.copy(k0, last, a);
+        fb.copy(k0, last, b);
     };
     copy(0, a0, b0);
-    for (int k0 = 0; k0 < p.k; k0 += 2 * kSlice) {
-        arrive();
-        if (k0 + kSlice < p.k) copy(k0 + kSlice, a1, b1);
-        tile.multiply(a0, b0);
-        if (k0 + kSlice >= p.k) break;
-        arrive();
-        if (k0 + 2 * kSlice < p.k) copy(k0 + 2 * kSlice, a0, b0);
-        tile.multiply(a1, b1);
+    copy(1, a1, b1);
+    copy(2, a2, b2);
+    auto step = [&](int i, const int8_t* a, const int8_t* b, int8_t* a_next, int8_t* b_next) {
+        arrive<2 * kCopies>();
+        copy(i + 3, a_next, b_next);
+        tile.multiply(a, b);
+    };
+    for (int i = 0; i < n_slices; i += 4) {
+        step(i, a0, b0, a3, b3);
+        step(i + 1, a1, b1, a0, b0);
+        step(i + 2, a2, b2, a1, b1);
+        step(i + 3, a3, b3, a2, b2);
     }
+    __builtin_amdgcn_s_waitcnt(0x0070);  // no copy into shared memory outlives the workgroup
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int m0 = t0 + (wave / WN) * (BM / WM), c0 = n0 + (wave % WN) * (BN / WN) + (lane & 31);
 #pragma unroll
@@ -206,93 +259,352 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const LinearP p, int
         for (int g = 0; g < 16; ++g) {
             const int t = m0 + i * 32 + 8 * (g / 4) + 4 * (lane >> 5) + g % 4;
             if (t >= p.T) continue;
-            const float s = p.s[t];
+            const float s = p.splits > 1 ? 0.f : p.s[t];
 #pragma unroll
             for (int j = 0; j < tile.TN; ++j) {
                 const int n = c0 + j * 32;
-                if (n < p.n) put<O>(p, t, n, tile.acc[i][j][g], s);
+                if (n >= p.n) continue;
+                if (p.splits > 1)
+                    p.part[((int64_t)blockIdx.y * p.T + t) * p.n + n] = tile.acc[i][j][g];
+                else
+                    put<O>(p, t, n, tile.acc[i][j][g], s);
             }
         }
 }
 
-// ---- few tokens ----------------------------------------------------------------------------
-// Bound by reading w once: each wave takes 16 rows of w and a slice of k, its weights going from
-// memory straight into matrix operands (16 rows x 64 bytes per instruction), and the eight
-// waves of a workgroup add their sums through shared memory.  MT groups of 16 tokens share each
-// weight operand.
-template <typename O, int MT>
-__global__ __launch_bounds__(512) void skinny_kernel(const LinearP p) {
-    constexpr int W = 8;
-    __shared__ int sums[W][MT][64][4];
+template <typename O>
+__global__ __launch_bounds__(256) void finish_kernel(const LinearP p) {
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= p.n) return;
+    for (int t = blockIdx.y; t < p.T; t += gridDim.y) {
+        int v = 0;
+        for (int i = 0; i < p.splits; ++i) v += p.part[((int64_t)i * p.T + t) * p.n + n];
+        put<O>(p, t, n, v, p.s[t]);
+    }
+}
+
+// ---- one or two tokens ---------------------------------------------------------------------
+// Bound by reading w once.  A wave takes whole rows of w, two at a time, a kilobyte of consecutive
+// bytes an instruction (16 rows x 64 bytes, as the matrix operands want them, reach 5 TB/s where
+// this reaches 6.2 on 8192 x 28672), and multiplies on the vector ALU, four products an instruction.
+// The tokens lie in shared memory; floating ones are quantised on the way there while the first
+// weights are under way.
+constexpr int kVecWaves = 4, kVecRows = 2;
+
+__device__ inline int wave_add(int v) {
+#pragma unroll
+    for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+
+template <typename O, typename X, int TT>
+__global__ __launch_bounds__(kVecWaves * 64) void vec_kernel(const LinearP p, const void* x, int64_t x_stride) {
+    constexpr int R = kVecRows, C = 4, kBlock = C * 1024;  // rows of a wave; kilobytes of each in flight
+    __shared__ __attribute__((aligned(16))) int8_t xs[TT][kVecMax];
+    __shared__ uint32_t part[TT][kVecWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
+    const int n0 = (blockIdx.x * kVecWaves + wave) * R;
+    const int8_t* row[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) row[j] = p.w + (int64_t)min(n0 + j, p.n - 1) * p.w_stride;
+    i32x4 a[C][R];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < R; ++j)  // (past the row its last bytes: they meet zeros)
+                a[c][j] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(row[j] + min(k0 + c * 1024 + lane * 16, p.k - 16)));
+    };
+    load(0);
+    const int padded = (p.k + kBlock - 1) / kBlock * kBlock;
+    float scale[TT];
+    if constexpr (std::is_same_v<X, int8_t>) {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            scale[t] = p.s[t];
+            for (int e = tid * 16; e < padded; e += kVecWaves * 1024)
+                *reinterpret_cast<i32x4*>(&xs[t][e]) = e < p.k ? *reinterpret_cast<const i32x4*>(p.q + t * p.q_stride + e) : i32x4{};
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            uint32_t m = 0;
+            for (int e = tid * 8; e < p.k; e += kVecWaves * 512) {
+                const auto u = load_pack<X, 8>(x, t * x_stride + e);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = max(m, magnitude((float)u.e[i]));
+            }
+            m = wave_max(m);
+            if (lane == 0) part[t][wave] = m;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int w = 0; w < kVecWaves; ++w) m = max(m, part[t][w]);
+            float top;
+            scale[t] = token_scale(m, &top);
+            const float inv = top > 0.f ? 127.f / top : 0.f;
+            for (int e = tid * 8; e < padded; e += kVecWaves * 512) {
+                Pack<int8_t, 8> o{};
+                if (e < p.k && top > 0.f) {
+                    const auto u = load_pack<X, 8>(x, t * x_stride + e);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o.e[i] = (int8_t)quantise((float)u.e[i], top, inv);
+                }
+                store_pack<int8_t, 8>(&xs[t][0], e, o);
+            }
+        }
+    }
+    __syncthreads();
+    int acc[R][TT] = {};
+    for (int k0 = 0; k0 < p.k; k0 += kBlock) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const i32x4 q = *reinterpret_cast<const i32x4*>(&xs[t][k0 + c * 1024 + lane * 16]);
+#pragma unroll
+                for (int j = 0; j < R; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[j][t] = __builtin_amdgcn_sdot4(a[c][j][e], q[e], acc[j][t], false);
+            }
+        if (k0 + kBlock < p.k) load(k0 + kBlock);
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const int v = wave_add(acc[j][t]);
+            if (lane == 0 && n0 + j < p.n) put<O>(p, t, n0 + j, v, scale[t]);
+        }
+}
+
+template <typename O, typename X>
+hipError_t vec(const LinearP& p, const void* x, int64_t x_stride, hipStream_t st) {
+    const dim3 grid((unsigned)ceil_div(p.n, kVecWaves * kVecRows)), block(kVecWaves * 64);
+    if (p.T == 1)
+        hipLaunchKernelGGL((vec_kernel<O, X, 1>), grid, block, 0, st, p, x, x_stride);
+    else
+        hipLaunchKernelGGL((vec_kernel<O, X, 2>), grid, block, 0, st, p, x, x_stride);
+    return hipGetLastError();
+}
+
+// ---- up to 16 tokens -----------------------------------------------------------------------
+// Also bound by reading w once.  Each wave takes 16 rows of w and a quarter of k, its weights going
+// from memory straight into matrix operands (16 rows x 64 bytes per instruction, the other half of
+// the lines in the next); the four waves of a workgroup add their sums through shared memory.
+template <typename O>
+__global__ __launch_bounds__(256) void skinny_kernel(const LinearP p) {
+    constexpr int W = 4, U = 8;  // waves; steps in flight
+    __shared__ int sums[W][64][4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * 16;
     const int steps = (p.k + 63) / 64, s0 = steps * wave / W, s1 = steps * (wave + 1) / W;
-    const int8_t* wr = p.w + (int64_t)min(n0 + r, p.n - 1) * p.w_stride + g * 16;
-    const int8_t* qr[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) qr[m] = p.q + (int64_t)min(m * 16 + r, p.T - 1) * p.q_stride + g * 16;
-    i32x4 acc[MT] = {};
-    constexpr int U = 4;  // steps in flight
+    const int8_t* wr = p.w + (int64_t)min(n0 + r, p.n - 1) * p.w_stride;
+    const int8_t* qr = p.q + (int64_t)min(r, p.T - 1) * p.q_stride;
+    i32x4 acc = {};
     for (int s = s0; s < s1; s += U) {
-        i32x4 a[U], b[U][MT];
+        i32x4 a[U], b[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int at = (s + u) * 64;
-            const bool in = s + u < s1 && at + g * 16 < p.k;
-            a[u] = in ? __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wr + at)) : i32x4{};
-#pragma unroll
-            for (int m = 0; m < MT; ++m) b[u][m] = in ? *reinterpret_cast<const i32x4*>(qr[m] + at) : i32x4{};
+            const int at = (s + u) * 64 + g * 16, from = s + u < s1 && at < p.k ? at : 0;
+            a[u] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wr + from));
+            b[u] = *reinterpret_cast<const i32x4*>(qr + from);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int m = 0; m < MT; ++m) acc[m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u], b[u][m], acc[m], 0, 0, 0);
+        for (int u = 0; u < U; ++u) {
+            const bool in = s + u < s1 && (s + u) * 64 + g * 16 < p.k;  // past the end: a factor of zero
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u], in ? b[u] : i32x4{}, acc, 0, 0, 0);
+        }
     }
-#pragma unroll
-    for (int m = 0; m < MT; ++m) *reinterpret_cast<i32x4*>(sums[wave][m][lane]) = acc[m];
+    *reinterpret_cast<i32x4*>(sums[wave][lane]) = acc;
     __syncthreads();
     // lane l of the matrix layout: token l % 16, channels 4 (l / 16) .. + 3
-    for (int i = threadIdx.x; i < MT * 256; i += W * 64) {
-        const int m = i >> 8, l = (i >> 2) & 63, c = i & 3;
+    const int l = threadIdx.x >> 2, c = threadIdx.x & 3, t = l & 15, n = n0 + 4 * (l >> 4) + c;
+    int v = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) v += sums[w][l][c];
+    if (t < p.T && n < p.n) put<O>(p, t, n, v, p.s[t]);
+}
+
+// ---- up to 48 tokens -----------------------------------------------------------------------
+// The tokens weigh as much as the weights here: each wave copies 256-byte slices of 32 rows of w
+// and of the tokens to shared memory of its own, every fourth slice, without barriers (37 tokens
+// x 5120 x 5120: 10.0 us; with both operands straight from memory 18.6, by tiles with k split 15.7).
+template <typename O, int MT>
+__global__ __launch_bounds__(256) void slice_kernel(const LinearP p) {
+    constexpr int W = 4, RW = 32, RX = 16 * MT, kBytes = 256;
+    __shared__ __attribute__((aligned(16))) int8_t buf0[W * (RW + RX) * kBytes];
+    __shared__ __attribute__((aligned(16))) int8_t buf1[W * (RW + RX) * kBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * RW;
+    i32x4 acc[2][MT] = {};
+    // four rows an instruction; a row's 16 chunks permuted by its number (banks)
+    auto copy = [&](int k0, int8_t* buf) {
+        int8_t* dst = buf + wave * (RW + RX) * kBytes;
+#pragma unroll
+        for (int i = 0; i < (RW + RX) / 4; ++i) {
+            const int r4 = i * 4 + (lane >> 4), at = k0 + ((lane & 15) ^ (r4 & 15)) * 16;
+            const int8_t* src = i < RW / 4 ? p.w + (int64_t)min(n0 + r4, p.n - 1) * p.w_stride
+                                           : p.q + (int64_t)min(r4 - RW, p.T - 1) * p.q_stride;
+            if (i >= RW / 4 && i * 4 - RW >= p.T) continue;  // rows of no token: their sums are dropped
+            __builtin_amdgcn_global_load_lds((gptr)(at < p.k ? src + at : reinterpret_cast<const int8_t*>(g_zero_chunk)),
+                                             (lptr)(dst + i * 1024), 16, 0, 0);
+        }
+    };
+    auto use = [&](const int8_t* buf) {
+        const int8_t* src = buf + wave * (RW + RX) * kBytes;
+#pragma unroll
+        for (int kk = 0; kk < kBytes / 64; ++kk) {
+            const int chunk = ((kk * 4 + g) ^ r) * 16;
+            i32x4 a[2], b[MT];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) a[i] = *reinterpret_cast<const i32x4*>(src + (i * 16 + r) * kBytes + chunk);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) b[m] = *reinterpret_cast<const i32x4*>(src + (RW + m * 16 + r) * kBytes + chunk);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) acc[i][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[m], acc[i][m], 0, 0, 0);
+        }
+    };
+    auto landed = [] {  // the wave's copies are in shared memory, its reads done
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    };
+    int k0 = wave * kBytes;
+    if (k0 < p.k) {
+        copy(k0, buf0);
+        for (;;) {
+            landed();
+            if (k0 + W * kBytes < p.k) copy(k0 + W * kBytes, buf1);
+            use(buf0);
+            if ((k0 += W * kBytes) >= p.k) break;
+            landed();
+            if (k0 + W * kBytes < p.k) copy(k0 + W * kBytes, buf0);
+            use(buf1);
+            if ((k0 += W * kBytes) >= p.k) break;
+        }
+    }
+    __syncthreads();
+    int* sums = reinterpret_cast<int*>(buf0);  // [wave][2][MT][64][4]
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) *reinterpret_cast<i32x4*>(sums + (((wave * 2 + i) * MT + m) * 64 + lane) * 4) = acc[i][m];
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * MT * 256; e += W * 64) {
+        const int i = e / (MT * 256), m = (e >> 8) % MT, l = (e >> 2) & 63, c = e & 3;
         int v = 0;
 #pragma unroll
-        for (int w = 0; w < W; ++w) v += sums[w][m][l][c];
-        const int t = m * 16 + (l & 15), n = n0 + 4 * (l >> 4) + c;
+        for (int w = 0; w < W; ++w) v += sums[w * 2 * MT * 256 + e];
+        const int t = m * 16 + (l & 15), n = n0 + i * 16 + 4 * (l >> 4) + c;
         if (t < p.T && n < p.n) put<O>(p, t, n, v, p.s[t]);
     }
 }
 
-template <typename O>
-hipError_t product(const LinearP& p, int n_cu, hipStream_t st) {
-    if (p.T <= 64) {
-        const dim3 grid((unsigned)ceil_div(p.n, 16));
-        switch ((p.T + 15) / 16) {
-            case 1: hipLaunchKernelGGL((skinny_kernel<O, 1>), grid, dim3(512), 0, st, p); break;
-            case 2: hipLaunchKernelGGL((skinny_kernel<O, 2>), grid, dim3(512), 0, st, p); break;
-            case 3: hipLaunchKernelGGL((skinny_kernel<O, 3>), grid, dim3(512), 0, st, p); break;
-            default: hipLaunchKernelGGL((skinny_kernel<O, 4>), grid, dim3(512), 0, st, p);
+// ---- choice of tiles -----------------------------------------------------------------------
+// The tile shapes, by tokens and channels: workgroups that run at once on a compute unit, and the
+// time of a 64-byte slice of k with the unit full and with one workgroup on it, as measured on
+// 512 and 2048 tokens of k = 8192 (us).
+struct TileShape {
+    int bm, bn, per_cu;
+    double full_us, lone_us;
+};
+constexpr TileShape kTiles[] = {{64, 128, 3, 0.60, 0.48}, {128, 128, 2, 0.60, 0.55}, {256, 256, 1, 0.98, 0.98}};
+constexpr int kMaxSplits = 8;
+
+// Shape and splits of k with the least estimated time for T x n: rounds of workgroups x (slices +
+// start), and for a split the traffic of its sums.
+struct TilePlan {
+    int shape, splits, slices;
+    double us;
+};
+TilePlan plan_tiles(int64_t T, int64_t k, int64_t n, int n_cu, size_t room) {
+    const int64_t slices = ceil_div(k, kSlice);
+    TilePlan best{0, 1, (int)slices, 0};
+    for (int i = 0; i < 3; ++i)
+        for (int s = 1; s <= kMaxSplits; ++s) {
+            const int64_t per = round_up(ceil_div(slices, s), 4);
+            if (s > 1 && ((uint64_t)s * T * n * 4 > room || ceil_div(slices, per) != s)) continue;
+            const int64_t wgs = ceil_div(T, kTiles[i].bm) * ceil_div(n, kTiles[i].bn) * s, slots = (int64_t)n_cu * kTiles[i].per_cu;
+            const double slice_us = wgs <= n_cu ? kTiles[i].lone_us : kTiles[i].full_us;
+            const double us = ceil_div(wgs, slots) * (per * slice_us + 3.0) + (s > 1 ? 4.0 + (double)s * T * n * 8 / 4e6 : 0.0);
+            if (best.us == 0 || us < best.us) best = {i, s, (int)per, us};
         }
-        return hipGetLastError();
-    }
-    const int tn = (int)ceil_div(p.n, 128);
-    const int64_t tiles = ceil_div(p.T, 128) * tn;
-    hipLaunchKernelGGL((tile_kernel<O, 128, 128, 2, 2>), dim3((unsigned)tiles), dim3(256), 0, st, p, tn);
+    return best;
+}
+
+template <typename O, int BM, int BN, int WM, int WN>
+hipError_t tiles(const LinearP& p, hipStream_t st) {
+    const int tn = (int)ceil_div(p.n, BN);
+    hipLaunchKernelGGL((tile_kernel<O, BM, BN, WM, WN>), dim3((unsigned)(ceil_div(p.T, BM) * tn), p.splits), dim3(WM * WN * 64), 0, st, p, tn);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    hipLaunchKernelGGL(finish_kernel<O>, dim3((unsigned)ceil_div(p.n, 256), (unsigned)std::min(p.T, 65535)), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 
-}  // namespace
-
-size_t linear_workspace(const ls_linear_i8_args& a) {
-    if (a.x_type == LS_I8) return 0;
-    return round_up((size_t)a.n_tokens * a.k, 256) + round_up((size_t)a.n_tokens * 4, 256);
+template <typename O>
+hipError_t tiles_of(LinearP p, const TilePlan& plan, int32_t* part, hipStream_t st) {
+    p.splits = plan.splits, p.slices = plan.slices, p.part = part;
+    switch (plan.shape) {
+        case 0: return tiles<O, 64, 128, 2, 2>(p, st);
+        case 1: return tiles<O, 128, 128, 2, 2>(p, st);
+        default: return tiles<O, 256, 256, 2, 4>(p, st);
+    }
 }
 
-hipError_t launch_linear(const ls_linear_i8_args& a, void* ws, int n_cu, hipStream_t st) {
-    LinearP p{static_cast<const int8_t*>(a.x), a.x_stride, a.x_scale, a.w, a.w_stride, a.w_scale, a.bias, a.out,
-              a.out_stride, a.n_tokens, a.k, a.n};
+template <typename O>
+hipError_t product(const LinearP& p, int32_t* part, size_t room, int n_cu, hipStream_t st) {
+    if (p.T <= 2 && p.k <= kVecMax) return vec<O, int8_t>(p, nullptr, 0, st);
+    if (p.T <= 48) {
+        const dim3 by32((unsigned)ceil_div(p.n, 32));
+        if (p.T <= 16)
+            hipLaunchKernelGGL(skinny_kernel<O>, dim3((unsigned)ceil_div(p.n, 16)), dim3(256), 0, st, p);
+        else if (p.T <= 32)
+            hipLaunchKernelGGL((slice_kernel<O, 2>), by32, dim3(256), 0, st, p);
+        else
+            hipLaunchKernelGGL((slice_kernel<O, 3>), by32, dim3(256), 0, st, p);
+        return hipGetLastError();
+    }
+    const TilePlan whole = plan_tiles(p.T, p.k, p.n, n_cu, room);
+    // The largest tiles in whole rounds, the channels left over by the best shape for them, where
+    // that is faster: 2048 x 8192 x 10240 is 1.25 rounds of 256 x 256 tiles.
+    const int64_t rows = ceil_div(p.T, 256), columns = ceil_div(p.n, 256), rounds = rows * columns / n_cu;
+    const int64_t first = rounds * n_cu / rows;  // columns of tiles in those rounds
+    if (first > 0 && first < columns) {
+        const int64_t slices = ceil_div(p.k, kSlice), n1 = first * 256;
+        const TilePlan rest = plan_tiles(p.T, p.k, p.n - n1, n_cu, room);
+        if (rounds * (round_up(slices, 4) * kTiles[2].full_us + 3.0) + rest.us + 2.0 < whole.us) {
+            LinearP a = p, b = p;
+            a.n = (int)n1;
+            hipError_t e = tiles_of<O>(a, {2, 1, (int)round_up(slices, 4), 0}, part, st);
+            if (e != hipSuccess) return e;
+            b.n = p.n - a.n;
+            b.w += n1 * p.w_stride;
+            b.w_scale += n1;
+            if (b.bias) b.bias += n1;
+            b.out = static_cast<O*>(p.out) + n1;
+            return tiles_of<O>(b, rest, part, st);
+        }
+    }
+    return tiles_of<O>(p, whole, part, st);
+}
+
+template <typename O>
+hipError_t linear(const ls_linear_i8_args& a, LinearP p, uint8_t* ws, size_t ws_bytes, int n_cu, hipStream_t st) {
+    const size_t used = linear_workspace(a);
     if (a.x_type != LS_I8) {
-        int8_t* q = static_cast<int8_t*>(ws);
-        float* s = reinterpret_cast<float*>(q + round_up((size_t)a.n_tokens * a.k, 256));
+        if (quantised_on_the_way(a)) {
+            if (a.x_type == LS_F32) return vec<O, float>(p, a.x, a.x_stride, st);
+            if (a.x_type == LS_F16) return vec<O, _Float16>(p, a.x, a.x_stride, st);
+            return vec<O, __bf16>(p, a.x, a.x_stride, st);
+        }
+        int8_t* q = reinterpret_cast<int8_t*>(ws);
+        float* s = reinterpret_cast<float*>(ws + round_up((size_t)a.n_tokens * a.k, 256));
         const dim3 grid(a.n_tokens), block(256);
         if (a.x_type == LS_F32)
             hipLaunchKernelGGL(quantise_kernel<float>, grid, block, 0, st, a.x, a.x_stride, a.k, q, s);
@@ -302,14 +614,26 @@ hipError_t launch_linear(const ls_linear_i8_args& a, void* ws, int n_cu, hipStre
             hipLaunchKernelGGL(quantise_kernel<__bf16>, grid, block, 0, st, a.x, a.x_stride, a.k, q, s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        p.q = q;
-        p.q_stride = a.k;
-        p.s = s;
+        p.q = q, p.q_stride = a.k, p.s = s;
     }
+    return product<O>(p, reinterpret_cast<int32_t*>(ws + used), ws_bytes - used, n_cu, st);
+}
+
+}  // namespace
+
+size_t linear_workspace(const ls_linear_i8_args& a) {
+    if (a.x_type == LS_I8 || quantised_on_the_way(a)) return 0;
+    return round_up((size_t)a.n_tokens * a.k, 256) + round_up((size_t)a.n_tokens * 4, 256);
+}
+
+hipError_t launch_linear(const ls_linear_i8_args& a, void* ws, size_t ws_bytes, int n_cu, hipStream_t st) {
+    const LinearP p{static_cast<const int8_t*>(a.x), a.x_stride, a.x_scale, a.w, a.w_stride, a.w_scale, a.bias, a.out, a.out_stride,
+                    a.n_tokens, a.k, a.n, 0, 1, nullptr};
+    uint8_t* at = static_cast<uint8_t*>(ws);
     switch (a.out_type) {
-        case LS_F32: return product<float>(p, n_cu, st);
-        case LS_F16: return product<_Float16>(p, n_cu, st);
-        default: return product<__bf16>(p, n_cu, st);
+        case LS_F32: return linear<float>(a, p, at, ws_bytes, n_cu, st);
+        case LS_F16: return linear<_Float16>(a, p, at, ws_bytes, n_cu, st);
+        default: return linear<__bf16>(a, p, at, ws_bytes, n_cu, st);
     }
 }
 

@@ -167,7 +167,7 @@ ls_status ls_linear_i8(ls_ops* c, const ls_linear_i8_args* a) {
     const size_t need = ls::linear_workspace(*a);
     if (need > c->ws_bytes)
         return fail(c, LS_E_CAPACITY, "the quantised tokens take %zu bytes, the workspace has %zu", need, c->ws_bytes);
-    return launched(c, ls::launch_linear(*a, c->ws, c->n_cu, c->stream), "ls_linear_i8");
+    return launched(c, ls::launch_linear(*a, c->ws, c->ws_bytes, c->n_cu, c->stream), "ls_linear_i8");
 }
 
 ls_status ls_kv_append(ls_ops* c, const ls_kv_cache* kv, const ls_append_args* a) {

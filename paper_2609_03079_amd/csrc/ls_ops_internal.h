@@ -19,7 +19,8 @@ hipError_t launch_append(const ls_kv_cache& c, const ls_append_args& a, int n_cu
 // ---- 8-bit products (ls_linear.hip) --------------------------------------------------------
 // Workspace that the call needs: the quantised tokens and their scales, where they go through memory.
 size_t linear_workspace(const ls_linear_i8_args& a);
-hipError_t launch_linear(const ls_linear_i8_args& a, void* ws, int n_cu, hipStream_t st);
+// ws_bytes: what there is; what is left of it may hold sums of a k that is split.
+hipError_t launch_linear(const ls_linear_i8_args& a, void* ws, size_t ws_bytes, int n_cu, hipStream_t st);
 
 // ---- attention (ls_attend.hip) -------------------------------------------------------------
 constexpr int kMaxParts = 128;  // partial results of one row, at most
