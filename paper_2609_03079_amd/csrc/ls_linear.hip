@@ -37,13 +37,6 @@ struct LinearP {
     int32_t* part;       // [splits][T][n] sums of the splits
 };
 
-// Rows that the kernel of one or two tokens holds in shared memory, and tokens that it quantises
-// itself, each workgroup anew: up to 8192 elements (a launch of its own takes 3 us more).
-constexpr int kVecMax = 16384;
-inline bool quantised_on_the_way(const ls_linear_i8_args& a) {
-    return a.x_type != LS_I8 && a.n_tokens <= 2 && (int64_t)a.n_tokens * a.k <= 8192;
-}
-
 template <typename O>
 __device__ inline void put(const LinearP& p, int t, int n, int acc, float s) {
     float v = (float)acc * s * p.w_scale[n];
@@ -55,10 +48,28 @@ __device__ inline void put(const LinearP& p, int t, int n, int acc, float s) {
 // |x| as ordered integers: an infinity is 0x7f800000, a NaN above it.
 __device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// Over the 64 lanes by lane exchanges within the registers; the result is in every lane.
+template <int CTRL, int ROWS>
+__device__ inline int dpp(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
 __device__ inline uint32_t wave_max(uint32_t m) {
-#pragma unroll
-    for (int off = 32; off; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off, 64));
-    return m;
+    m = max(m, (uint32_t)dpp<0xb1, 0xf>((int)m));   // quad_perm [1,0,3,2]
+    m = max(m, (uint32_t)dpp<0x4e, 0xf>((int)m));   // quad_perm [2,3,0,1]
+    m = max(m, (uint32_t)dpp<0x141, 0xf>((int)m));  // row_half_mirror
+    m = max(m, (uint32_t)dpp<0x140, 0xf>((int)m));  // row_mirror
+    m = max(m, (uint32_t)dpp<0x142, 0xa>((int)m));  // row_bcast:15
+    m = max(m, (uint32_t)dpp<0x143, 0xc>((int)m));  // row_bcast:31
+    return (uint32_t)__builtin_amdgcn_readlane((int)m, 63);
+}
+__device__ inline int wave_add(int v) {
+    v += dpp<0xb1, 0xf>(v);
+    v += dpp<0x4e, 0xf>(v);
+    v += dpp<0x141, 0xf>(v);
+    v += dpp<0x140, 0xf>(v);
+    v += dpp<0x142, 0xa>(v);
+    v += dpp<0x143, 0xc>(v);
+    return __builtin_amdgcn_readlane(v, 63);
 }
 
 // The scale of a token from its largest magnitude, and what its elements are divided by (0: all zero).
@@ -283,56 +294,53 @@ __global__ __launch_bounds__(256) void finish_kernel(const LinearP p) {
     }
 }
 
-// ---- one or two tokens ---------------------------------------------------------------------
-// Bound by reading w once.  A wave takes whole rows of w, two at a time, a kilobyte of consecutive
-// bytes an instruction (16 rows x 64 bytes, as the matrix operands want them, reach 5 TB/s where
-// this reaches 6.2 on 8192 x 28672), and multiplies on the vector ALU, four products an instruction.
-// The tokens lie in shared memory; floating ones are quantised on the way there while the first
-// weights are under way.
-constexpr int kVecWaves = 4, kVecRows = 2;
+// ---- up to four tokens ---------------------------------------------------------------------
+// Bound by reading w once.  One workgroup of 16 waves per compute unit; a wave takes whole rows of
+// w, one after the other, four kilobytes at a time, a kilobyte of consecutive bytes an instruction,
+// the next four under way while these are multiplied on the vector ALU (four products an
+// instruction).  The tokens lie in shared memory; floating ones are quantised on the way there, by
+// every workgroup, while its first weights are under way: one token x 4096 x 12288 takes 10.1 us
+// (8.7 from 8-bit inputs; 13.2 with small workgroups, each of which quantised the token again).
+// 16 rows x 64 bytes an instruction, as the matrix operands want them, take 12.6.
+constexpr int kVecWaves = 16, kVecBlock = 4096;
 
-__device__ inline int wave_add(int v) {
-#pragma unroll
-    for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
-}
+inline size_t vec_shared(int T, int k) { return (size_t)T * round_up(k, kVecBlock); }
+inline bool vec_takes(int T, int k) { return T <= 4 && vec_shared(T == 3 ? 4 : T, k) <= 65536; }
 
 template <typename O, typename X, int TT>
 __global__ __launch_bounds__(kVecWaves * 64) void vec_kernel(const LinearP p, const void* x, int64_t x_stride) {
-    constexpr int R = kVecRows, C = 4, kBlock = C * 1024;  // rows of a wave; kilobytes of each in flight
-    __shared__ __attribute__((aligned(16))) int8_t xs[TT][kVecMax];
+    constexpr int C = kVecBlock / 1024;
+    extern __shared__ __attribute__((aligned(16))) int8_t xs[];  // [TT][padded]
     __shared__ uint32_t part[TT][kVecWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
-    const int n0 = (blockIdx.x * kVecWaves + wave) * R;
-    const int8_t* row[R];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x;
+    const int blocks = (p.k + kVecBlock - 1) / kVecBlock, padded = blocks * kVecBlock;
+    const int rows = gridDim.x * kVecWaves;  // at a time
+    int n = blockIdx.x + gridDim.x * wave, block = 0;
+    i32x4 a[2][C];
+    auto load = [&](i32x4 (&to)[C], int row, int b) {
 #pragma unroll
-    for (int j = 0; j < R; ++j) row[j] = p.w + (int64_t)min(n0 + j, p.n - 1) * p.w_stride;
-    i32x4 a[C][R];
-    auto load = [&](int k0) {
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int j = 0; j < R; ++j)  // (past the row its last bytes: they meet zeros)
-                a[c][j] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(row[j] + min(k0 + c * 1024 + lane * 16, p.k - 16)));
+        for (int c = 0; c < C; ++c)  // (past the row its last bytes: they meet zeros)
+            to[c] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(
+                p.w + (int64_t)row * p.w_stride + min(b * kVecBlock + c * 1024 + lane * 16, p.k - 16)));
     };
-    load(0);
-    const int padded = (p.k + kBlock - 1) / kBlock * kBlock;
+    if (n < p.n) load(a[0], n, 0);
     float scale[TT];
     if constexpr (std::is_same_v<X, int8_t>) {
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            scale[t] = p.s[t];
+            const int tt = min(t, p.T - 1);
+            scale[t] = p.s[tt];
             for (int e = tid * 16; e < padded; e += kVecWaves * 1024)
-                *reinterpret_cast<i32x4*>(&xs[t][e]) = e < p.k ? *reinterpret_cast<const i32x4*>(p.q + t * p.q_stride + e) : i32x4{};
+                *reinterpret_cast<i32x4*>(xs + t * padded + e) = e < p.k ? *reinterpret_cast<const i32x4*>(p.q + tt * p.q_stride + e) : i32x4{};
         }
     } else {
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             uint32_t m = 0;
-            for (int e = tid * 8; e < p.k; e += kVecWaves * 512) {
-                const auto u = load_pack<X, 8>(x, t * x_stride + e);
+            for (int e = tid * 4; e < p.k; e += kVecWaves * 256) {
+                const auto u = load_pack<X, 4>(x, min(t, p.T - 1) * x_stride + e);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) m = max(m, magnitude((float)u.e[i]));
+                for (int i = 0; i < 4; ++i) m = max(m, magnitude((float)u.e[i]));
             }
             m = wave_max(m);
             if (lane == 0) part[t][wave] = m;
@@ -346,48 +354,58 @@ __global__ __launch_bounds__(kVecWaves * 64) void vec_kernel(const LinearP p, co
             float top;
             scale[t] = token_scale(m, &top);
             const float inv = top > 0.f ? 127.f / top : 0.f;
-            for (int e = tid * 8; e < padded; e += kVecWaves * 512) {
-                Pack<int8_t, 8> o{};
+            for (int e = tid * 4; e < padded; e += kVecWaves * 256) {
+                Pack<int8_t, 4> o{};
                 if (e < p.k && top > 0.f) {
-                    const auto u = load_pack<X, 8>(x, t * x_stride + e);
+                    const auto u = load_pack<X, 4>(x, min(t, p.T - 1) * x_stride + e);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) o.e[i] = (int8_t)quantise((float)u.e[i], top, inv);
+                    for (int i = 0; i < 4; ++i) o.e[i] = (int8_t)quantise((float)u.e[i], top, inv);
                 }
-                store_pack<int8_t, 8>(&xs[t][0], e, o);
+                store_pack<int8_t, 4>(xs, t * padded + e, o);
             }
         }
     }
     __syncthreads();
-    int acc[R][TT] = {};
-    for (int k0 = 0; k0 < p.k; k0 += kBlock) {
+    if (n >= p.n) return;
+    int acc[TT] = {};
+    // this block of the row, its sum if it is the row's last; the next one loaded meanwhile.  False: that was all.
+    auto step = [&](const i32x4 (&now)[C], i32x4 (&next)[C]) {
+        int row = n, b = block + 1;
+        if (b == blocks) b = 0, row += rows;
+        if (row < p.n) load(next, row, b);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
-                const i32x4 q = *reinterpret_cast<const i32x4*>(&xs[t][k0 + c * 1024 + lane * 16]);
+                const i32x4 q = *reinterpret_cast<const i32x4*>(xs + t * padded + block * kVecBlock + c * 1024 + lane * 16);
 #pragma unroll
-                for (int j = 0; j < R; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[j][t] = __builtin_amdgcn_sdot4(a[c][j][e], q[e], acc[j][t], false);
+                for (int e = 0; e < 4; ++e) acc[t] = __builtin_amdgcn_sdot4(now[c][e], q[e], acc[t], false);
             }
-        if (k0 + kBlock < p.k) load(k0 + kBlock);
-    }
+        if (b == 0) {
 #pragma unroll
-    for (int j = 0; j < R; ++j)
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const int v = wave_add(acc[j][t]);
-            if (lane == 0 && n0 + j < p.n) put<O>(p, t, n0 + j, v, scale[t]);
+            for (int t = 0; t < TT; ++t) {
+                const int v = wave_add(acc[t]);
+                acc[t] = 0;
+                if (lane == 0 && t < p.T) put<O>(p, t, n, v, scale[t]);
+            }
         }
+        n = row, block = b;
+        return n < p.n;
+    };
+    while (step(a[0], a[1]) && step(a[1], a[0])) {
+    }
 }
 
 template <typename O, typename X>
-hipError_t vec(const LinearP& p, const void* x, int64_t x_stride, hipStream_t st) {
-    const dim3 grid((unsigned)ceil_div(p.n, kVecWaves * kVecRows)), block(kVecWaves * 64);
+hipError_t vec(const LinearP& p, const void* x, int64_t x_stride, int n_cu, hipStream_t st) {
+    const dim3 grid((unsigned)std::min<int64_t>(n_cu, ceil_div(p.n, kVecWaves))), block(kVecWaves * 64);
+    const size_t shared = vec_shared(p.T == 3 ? 4 : p.T, p.k);
     if (p.T == 1)
-        hipLaunchKernelGGL((vec_kernel<O, X, 1>), grid, block, 0, st, p, x, x_stride);
+        hipLaunchKernelGGL((vec_kernel<O, X, 1>), grid, block, shared, st, p, x, x_stride);
+    else if (p.T == 2)
+        hipLaunchKernelGGL((vec_kernel<O, X, 2>), grid, block, shared, st, p, x, x_stride);
     else
-        hipLaunchKernelGGL((vec_kernel<O, X, 2>), grid, block, 0, st, p, x, x_stride);
+        hipLaunchKernelGGL((vec_kernel<O, X, 4>), grid, block, shared, st, p, x, x_stride);
     return hipGetLastError();
 }
 
@@ -559,7 +577,7 @@ hipError_t tiles_of(LinearP p, const TilePlan& plan, int32_t* part, hipStream_t 
 
 template <typename O>
 hipError_t product(const LinearP& p, int32_t* part, size_t room, int n_cu, hipStream_t st) {
-    if (p.T <= 2 && p.k <= kVecMax) return vec<O, int8_t>(p, nullptr, 0, st);
+    if (vec_takes(p.T, p.k)) return vec<O, int8_t>(p, nullptr, 0, n_cu, st);
     if (p.T <= 48) {
         const dim3 by32((unsigned)ceil_div(p.n, 32));
         if (p.T <= 16)
@@ -598,10 +616,10 @@ template <typename O>
 hipError_t linear(const ls_linear_i8_args& a, LinearP p, uint8_t* ws, size_t ws_bytes, int n_cu, hipStream_t st) {
     const size_t used = linear_workspace(a);
     if (a.x_type != LS_I8) {
-        if (quantised_on_the_way(a)) {
-            if (a.x_type == LS_F32) return vec<O, float>(p, a.x, a.x_stride, st);
-            if (a.x_type == LS_F16) return vec<O, _Float16>(p, a.x, a.x_stride, st);
-            return vec<O, __bf16>(p, a.x, a.x_stride, st);
+        if (vec_takes(p.T, p.k)) {
+            if (a.x_type == LS_F32) return vec<O, float>(p, a.x, a.x_stride, n_cu, st);
+            if (a.x_type == LS_F16) return vec<O, _Float16>(p, a.x, a.x_stride, n_cu, st);
+            return vec<O, __bf16>(p, a.x, a.x_stride, n_cu, st);
         }
         int8_t* q = reinterpret_cast<int8_t*>(ws);
         float* s = reinterpret_cast<float*>(ws + round_up((size_t)a.n_tokens * a.k, 256));
@@ -622,7 +640,7 @@ hipError_t linear(const ls_linear_i8_args& a, LinearP p, uint8_t* ws, size_t ws_
 }  // namespace
 
 size_t linear_workspace(const ls_linear_i8_args& a) {
-    if (a.x_type == LS_I8 || quantised_on_the_way(a)) return 0;
+    if (a.x_type == LS_I8 || vec_takes(a.n_tokens, a.k)) return 0;
     return round_up((size_t)a.n_tokens * a.k, 256) + round_up((size_t)a.n_tokens * 4, 256);
 }
 
