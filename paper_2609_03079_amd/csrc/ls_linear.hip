@@ -301,7 +301,6 @@ __global__ __launch_bounds__(256) void finish_kernel(const LinearP p) {
 // instruction).  The tokens lie in shared memory; floating ones are quantised on the way there, by
 // every workgroup, while its first weights are under way: one token x 4096 x 12288 takes 10.1 us
 // (8.7 from 8-bit inputs; 13.2 with small workgroups, each of which quantised the token again).
-// 16 rows x 64 bytes an instruction, as the matrix operands want them, take 12.6.
 constexpr int kVecWaves = 16, kVecBlock = 4096;
 
 inline size_t vec_shared(int T, int k) { return (size_t)T * round_up(k, kVecBlock); }
@@ -409,56 +408,20 @@ hipError_t vec(const LinearP& p, const void* x, int64_t x_stride, int n_cu, hipS
     return hipGetLastError();
 }
 
-// ---- up to 16 tokens -----------------------------------------------------------------------
-// Also bound by reading w once.  Each wave takes 16 rows of w and a quarter of k, its weights going
-// from memory straight into matrix operands (16 rows x 64 bytes per instruction, the other half of
-// the lines in the next); the four waves of a workgroup add their sums through shared memory.
-template <typename O>
-__global__ __launch_bounds__(256) void skinny_kernel(const LinearP p) {
-    constexpr int W = 4, U = 8;  // waves; steps in flight
-    __shared__ int sums[W][64][4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16;
-    const int steps = (p.k + 63) / 64, s0 = steps * wave / W, s1 = steps * (wave + 1) / W;
-    const int8_t* wr = p.w + (int64_t)min(n0 + r, p.n - 1) * p.w_stride;
-    const int8_t* qr = p.q + (int64_t)min(r, p.T - 1) * p.q_stride;
-    i32x4 acc = {};
-    for (int s = s0; s < s1; s += U) {
-        i32x4 a[U], b[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = (s + u) * 64 + g * 16, from = s + u < s1 && at < p.k ? at : 0;
-            a[u] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wr + from));
-            b[u] = *reinterpret_cast<const i32x4*>(qr + from);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool in = s + u < s1 && (s + u) * 64 + g * 16 < p.k;  // past the end: a factor of zero
-            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u], in ? b[u] : i32x4{}, acc, 0, 0, 0);
-        }
-    }
-    *reinterpret_cast<i32x4*>(sums[wave][lane]) = acc;
-    __syncthreads();
-    // lane l of the matrix layout: token l % 16, channels 4 (l / 16) .. + 3
-    const int l = threadIdx.x >> 2, c = threadIdx.x & 3, t = l & 15, n = n0 + 4 * (l >> 4) + c;
-    int v = 0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) v += sums[w][l][c];
-    if (t < p.T && n < p.n) put<O>(p, t, n, v, p.s[t]);
-}
-
 // ---- up to 48 tokens -----------------------------------------------------------------------
-// The tokens weigh as much as the weights here: each wave copies 256-byte slices of 32 rows of w
-// and of the tokens to shared memory of its own, every fourth slice, without barriers (37 tokens
-// x 5120 x 5120: 10.0 us; with both operands straight from memory 18.6, by tiles with k split 15.7).
-template <typename O, int MT>
-__global__ __launch_bounds__(256) void slice_kernel(const LinearP p) {
-    constexpr int W = 4, RW = 32, RX = 16 * MT, kBytes = 256;
+// Few enough that reading w sets the pace, too many for the vector ALU: each wave copies 256-byte
+// slices of 16 NR rows of w and of the tokens to shared memory of its own, every W-th slice, without
+// barriers, one slice ahead, and the waves' sums are added at the end.  8 tokens x 5120 x 5120 6.4 us,
+// x 8192 x 28672 46 us (with both operands read straight into the matrix operands, 16 rows x 64 bytes
+// an instruction, 14.3 and 53.7); 37 tokens x 5120 x 5120 10.0 us (by tiles with k split 15.7).
+template <typename O, int MT, int NR, int W>
+__global__ __launch_bounds__(W * 64) void slice_kernel(const LinearP p) {
+    constexpr int RW = 16 * NR, RX = 16 * MT, kBytes = 256;
     __shared__ __attribute__((aligned(16))) int8_t buf0[W * (RW + RX) * kBytes];
     __shared__ __attribute__((aligned(16))) int8_t buf1[W * (RW + RX) * kBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * RW;
-    i32x4 acc[2][MT] = {};
+    i32x4 acc[NR][MT] = {};
     // four rows an instruction; a row's 16 chunks permuted by its number (banks)
     auto copy = [&](int k0, int8_t* buf) {
         int8_t* dst = buf + wave * (RW + RX) * kBytes;
@@ -477,13 +440,13 @@ __global__ __launch_bounds__(256) void slice_kernel(const LinearP p) {
 #pragma unroll
         for (int kk = 0; kk < kBytes / 64; ++kk) {
             const int chunk = ((kk * 4 + g) ^ r) * 16;
-            i32x4 a[2], b[MT];
+            i32x4 a[NR], b[MT];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) a[i] = *reinterpret_cast<const i32x4*>(src + (i * 16 + r) * kBytes + chunk);
+            for (int i = 0; i < NR; ++i) a[i] = *reinterpret_cast<const i32x4*>(src + (i * 16 + r) * kBytes + chunk);
 #pragma unroll
             for (int m = 0; m < MT; ++m) b[m] = *reinterpret_cast<const i32x4*>(src + (RW + m * 16 + r) * kBytes + chunk);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < NR; ++i)
 #pragma unroll
                 for (int m = 0; m < MT; ++m) acc[i][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[m], acc[i][m], 0, 0, 0);
         }
@@ -507,20 +470,26 @@ __global__ __launch_bounds__(256) void slice_kernel(const LinearP p) {
         }
     }
     __syncthreads();
-    int* sums = reinterpret_cast<int*>(buf0);  // [wave][2][MT][64][4]
+    int* sums = reinterpret_cast<int*>(buf0);  // [wave][NR][MT][64][4]
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NR; ++i)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) *reinterpret_cast<i32x4*>(sums + (((wave * 2 + i) * MT + m) * 64 + lane) * 4) = acc[i][m];
+        for (int m = 0; m < MT; ++m) *reinterpret_cast<i32x4*>(sums + (((wave * NR + i) * MT + m) * 64 + lane) * 4) = acc[i][m];
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * MT * 256; e += W * 64) {
+    for (int e = threadIdx.x; e < NR * MT * 256; e += W * 64) {
         const int i = e / (MT * 256), m = (e >> 8) % MT, l = (e >> 2) & 63, c = e & 3;
         int v = 0;
 #pragma unroll
-        for (int w = 0; w < W; ++w) v += sums[w * 2 * MT * 256 + e];
+        for (int w = 0; w < W; ++w) v += sums[w * NR * MT * 256 + e];
         const int t = m * 16 + (l & 15), n = n0 + i * 16 + 4 * (l >> 4) + c;
         if (t < p.T && n < p.n) put<O>(p, t, n, v, p.s[t]);
     }
+}
+
+template <typename O, int MT, int NR, int W>
+hipError_t slices(const LinearP& p, hipStream_t st) {
+    hipLaunchKernelGGL((slice_kernel<O, MT, NR, W>), dim3((unsigned)ceil_div(p.n, 16 * NR)), dim3(W * 64), 0, st, p);
+    return hipGetLastError();
 }
 
 // ---- choice of tiles -----------------------------------------------------------------------
@@ -579,14 +548,9 @@ template <typename O>
 hipError_t product(const LinearP& p, int32_t* part, size_t room, int n_cu, hipStream_t st) {
     if (vec_takes(p.T, p.k)) return vec<O, int8_t>(p, nullptr, 0, n_cu, st);
     if (p.T <= 48) {
-        const dim3 by32((unsigned)ceil_div(p.n, 32));
-        if (p.T <= 16)
-            hipLaunchKernelGGL(skinny_kernel<O>, dim3((unsigned)ceil_div(p.n, 16)), dim3(256), 0, st, p);
-        else if (p.T <= 32)
-            hipLaunchKernelGGL((slice_kernel<O, 2>), by32, dim3(256), 0, st, p);
-        else
-            hipLaunchKernelGGL((slice_kernel<O, 3>), by32, dim3(256), 0, st, p);
-        return hipGetLastError();
+        if (p.T <= 16) return slices<O, 1, 1, 4>(p, st);
+        if (p.T <= 32) return slices<O, 2, 2, 4>(p, st);
+        return slices<O, 3, 2, 4>(p, st);
     }
     const TilePlan whole = plan_tiles(p.T, p.k, p.n, n_cu, room);
     // The largest tiles in whole rounds, the channels left over by the best shape for them, where
