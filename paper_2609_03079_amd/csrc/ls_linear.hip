@@ -500,7 +500,7 @@ struct TileShape {
     int bm, bn, per_cu;
     double full_us, lone_us;
 };
-constexpr TileShape kTiles[] = {{64, 128, 3, 0.60, 0.48}, {128, 128, 2, 0.60, 0.55}, {256, 256, 1, 0.98, 0.98}};
+constexpr TileShape kTiles[] = {{64, 128, 3, 0.75, 0.45}, {128, 128, 2, 0.75, 0.53}, {256, 256, 1, 1.20, 1.20}};
 constexpr int kMaxSplits = 8;
 
 // Shape and splits of k with the least estimated time for T x n: rounds of workgroups x (slices +
