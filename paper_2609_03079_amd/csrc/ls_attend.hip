@@ -48,6 +48,20 @@ __device__ inline f32x16 mma(const bf16x8& a, const bf16x8& b, const f32x16& c) 
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+// Quotients of 0 <= n < 2^31 by a number the host knows: a product and a shift.
+struct Div {
+    uint32_t m;
+    int shift, d;
+    Div() = default;
+    explicit Div(int d_) : d(d_) {
+        int log = 0;
+        while ((int64_t)1 << log < d_) ++log;
+        shift = 31 + log;
+        m = (uint32_t)((((uint64_t)1 << shift) + (uint32_t)d_ - 1) / (uint32_t)d_);
+    }
+    __host__ __device__ inline int of(int n) const { return (int)(((uint64_t)(uint32_t)n * m) >> shift); }
+};
+
 struct AttendP {
     const void* q;
     int64_t q_token, q_head;
@@ -63,6 +77,7 @@ struct AttendP {
     const int32_t* lens;
     int prefix_len, max_len;
     int S, n_q, H, KV, G, D;
+    Div by_S, by_n_q, by_H, by_KV, by_G, by_pre_tiles, by_suf_tiles, by_suf_chunk;
     float c;                 // scale log2(e): the softmax runs in powers of two
     AttendPlan plan;
     int pre_items, suf_items;  // workgroups of this launch
@@ -101,39 +116,35 @@ struct Item {
     int len;               // the sequence's keys
 };
 
-template <typename T, int DP, bool WIDE>
+// The part of the work that a workgroup takes; its sequence's length is not looked up yet.
+template <int R>
 __device__ inline bool item_of(const AttendP& p, int b, Item* it) {
-    constexpr int R = Shape<T, DP, WIDE>::kTileRows;
     if (b < p.pre_items) {
         // workgroups that follow each other run on different XCDs: the row tiles of the same keys
         // take every eighth workgroup, so that they share an L2
-        const int group = b / (8 * p.plan.pre_tiles) * 8 + b % 8;
+        const int eighth = b >> 3, turn = p.by_pre_tiles.of(eighth), group = turn * 8 + (b & 7);
         if (group >= p.plan.pre_parts * p.KV) return false;
-        it->row0 = b / 8 % p.plan.pre_tiles * R;
-        it->kv = group % p.KV;
-        it->part = group / p.KV;
+        it->row0 = (eighth - turn * p.plan.pre_tiles) * R;
+        it->part = p.by_KV.of(group);
+        it->kv = group - it->part * p.KV;
         it->seq = -1;
         it->table = p.prefix_pages;
-        it->len = p.prefix_len;
         it->begin = it->part * p.plan.pre_chunk;
         it->end = min(p.prefix_len, it->begin + p.plan.pre_chunk);
         it->rows = p.S * p.n_q * p.G;
         return true;
     }
     b -= p.pre_items;
-    it->row0 = b % p.plan.suf_tiles * R;
-    b /= p.plan.suf_tiles;
-    it->kv = b % p.KV;
-    b /= p.KV;
-    it->seq = b % p.S;
-    const int j = b / p.S;
+    const int tile = b, rest = p.by_suf_tiles.of(b), of_kv = p.by_KV.of(rest), j = p.by_S.of(of_kv);
+    it->row0 = (tile - rest * p.plan.suf_tiles) * R;
+    it->kv = rest - of_kv * p.KV;
+    it->seq = of_kv - j * p.S;
     it->table = p.pages + it->seq * p.pages_stride;
-    it->len = min(p.lens[it->seq], p.max_len);
     it->begin = j * p.plan.suf_chunk;
-    it->end = min(it->len, it->begin + p.plan.suf_chunk);
+    it->end = min(p.max_len, it->begin + p.plan.suf_chunk);
     it->rows = p.n_q * p.G;
     it->part = p.plan.pre_parts + j;
-    return it->begin < it->end || p.direct;
+    return true;
 }
 
 // MULTI: sequences with several query tokens each, whose last keys only some of them see.
@@ -150,15 +161,29 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 &
     __shared__ float wave_ml[NW][2][32];
     __shared__ float row_sum[32];
     Item it;
-    if (!item_of<T, DP, WIDE>(p, blockIdx.x, &it)) return;
+    if (!item_of<Sh::kTileRows>(p, blockIdx.x, &it)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, h = lane >> 5;
+
+    // The first page ids are on their way before the sequence's length is known: the table holds
+    // max_len keys.  Each lane looks up one key of a tile; -1 where there is none.
+    constexpr int kStep = WIDE ? KT : NW * KT;
+    int key = it.begin + (WIDE ? 0 : wave * KT);
+    auto page_id = [&](int key0) {
+        const int at = key0 + (lane & (KT - 1));
+        return at < it.end ? it.table[at >> p.page_shift] : -1;
+    };
+    const int first0 = page_id(key), first1 = page_id(key + kStep);
+    int id2 = page_id(key + 2 * kStep);
+    it.len = it.seq < 0 ? p.prefix_len : min(p.lens[it.seq], p.max_len);
+    it.end = min(it.end, it.len);
+    if (it.begin >= it.end && !p.direct) return;
 
     // this lane's query row: token and head of it, keys it sees
     const int row = it.row0 + (WIDE ? wave * 32 : 0) + n;
     const bool row_ok = row < it.rows;
     const int rr = row_ok ? row : it.rows - 1;
-    const int g = rr % p.G, tk = rr / p.G;  // token of the batch (prefix) or of the sequence
+    const int tk = p.by_G.of(rr), g = rr - tk * p.G;  // token of the batch (prefix) or of the sequence
     const int64_t token = it.seq < 0 ? tk : (int64_t)it.seq * p.n_q + tk;
     const int head = it.kv * p.G + g;
     const int limit = it.seq < 0 ? it.end : min(it.end, it.len - p.n_q + 1 + tk);
@@ -184,16 +209,11 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 &
     const T* zero = reinterpret_cast<const T*>(g_zero_row);
     const int page_mask = (1 << p.page_shift) - 1;
 
-    // The page id of key (tile + lane), -1 where there is none; then its place in the cache, in
-    // elements, -1 where the key is masked.  Each lane does one key of the tile.
-    auto page_id = [&](int key0) {
-        const int key = key0 + (lane & (KT - 1));
-        return key < it.end ? it.table[key >> p.page_shift] : -1;
-    };
+    // A key's place in the cache, in elements, -1 where it is masked.
     auto place = [&](int key0, int id) {
         const int key = key0 + (lane & (KT - 1));
         const int64_t at = (int64_t)id * p.page_stride + (int64_t)(key & page_mask) * p.token_stride;
-        return (unsigned)id < (unsigned)p.n_pages ? at : (int64_t)-1;
+        return (unsigned)id < (unsigned)p.n_pages && key < it.end ? at : (int64_t)-1;
     };
     // Copies a tile's rows, RPI of them an instruction: lane -> row lane / CPR, chunk lane % CPR permuted.
     const int c_row = lane / CPR;
@@ -347,11 +367,8 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 &
 
     // While tile j is used, V of j + 1 and K of j + 1 (PIPE: j + 2) arrive.  Past the end PIPE
     // copies and multiplies tiles of zeros; nothing uses their scores.
-    constexpr int kStep = WIDE ? KT : NW * KT;
-    int key = it.begin + (WIDE ? 0 : wave * KT);
     if (key < it.end) {
-        int64_t at0 = place(key, page_id(key)), at1 = place(key + kStep, page_id(key + kStep));
-        int id2 = page_id(key + 2 * kStep);
+        int64_t at0 = place(key, first0), at1 = place(key + kStep, first1);
         copy(kbase, at0, k0);
         copy(vbase, at0, v0);
         Scores s;
@@ -463,50 +480,77 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 &
         f32x4 v{};
 #pragma unroll
         for (int w = 0; w < NW; ++w) v += *joined(w, r, chunk);
-        const int tr = (it.row0 + r) / p.G;
-        put(it.seq < 0 ? tr : (int64_t)it.seq * p.n_q + tr, it.kv * p.G + (it.row0 + r) % p.G, chunk * 4, v, row_sum[r]);
+        const int tr = p.by_G.of(it.row0 + r);
+        put(it.seq < 0 ? tr : (int64_t)it.seq * p.n_q + tr, it.kv * p.G + it.row0 + r - tr * p.G, chunk * 4, v, row_sum[r]);
     }
 }
 
+template <int CTRL, int ROWS>
+__device__ inline float max_dpp(float v) {
+    const int x = __float_as_int(v);
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(x, x, CTRL, ROWS, 0xf, false)));
+}
+__device__ inline float wave_max(float v) {
+    v = max_dpp<0xb1, 0xf>(v);   // quad_perm [1,0,3,2]
+    v = max_dpp<0x4e, 0xf>(v);   // quad_perm [2,3,0,1]
+    v = max_dpp<0x141, 0xf>(v);  // row_half_mirror
+    v = max_dpp<0x140, 0xf>(v);  // row_mirror
+    v = max_dpp<0x142, 0xa>(v);  // row_bcast:15
+    v = max_dpp<0x143, 0xc>(v);  // row_bcast:31
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
 // Joins the parts of a row: a wave per row, DP / 4 lanes across its elements and the other
-// lanes on other parts.
+// lanes on other parts.  Bound by latency: the sequence's length, the maxima and sums and the first
+// parts are all asked for at once, parts that turn out never to have been written among them (their
+// weight is zero, and they are not looked at).
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void join_kernel(const AttendP p) {
-    constexpr int L = DP / 4, GR = 64 / L;
+    constexpr int L = DP / 4, GR = 64 / L, U = 4;
     const int lane = threadIdx.x & 63;
-    const int64_t rows = (int64_t)p.S * p.n_q * p.H, r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int rows = p.S * p.n_q * p.H, r = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (r >= rows) return;
-    const int64_t token = r / p.H;
-    const int len = min(p.lens[token / p.n_q], p.max_len);
+    const int token = p.by_H.of(r), seq = p.by_n_q.of(token);
+    const float* ml = p.ml + (int64_t)r * p.parts * 2;
+    const float* part = p.part + (int64_t)r * p.parts * p.D;
+    const int d = (lane % L) * 4, g = lane / L, dd = min(d, p.D - 4);
+    float m[2], l[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int j = min(i * 64 + lane, p.parts - 1);
+        m[i] = ml[j * 2];
+        l[i] = ml[j * 2 + 1];
+    }
+    f32x4 v[U];
+    auto ask = [&](int j0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const f32x4*>(part + (int64_t)min(j0 + u * GR + g, p.parts - 1) * p.D + dd);
+    };
+    ask(0);
+    const int len = min(p.lens[seq], p.max_len);
     // parts that were written: the prefix's unless the slot is idle, and the sequence's that hold keys
     const int first = len < 0 ? p.plan.pre_parts : 0;
-    const int last = p.plan.pre_parts + (len > 0 ? (len + p.plan.suf_chunk - 1) / p.plan.suf_chunk : 0);
-    const float* ml = p.ml + r * p.parts * 2;
-    float m[2], l[2], top = -INFINITY;
+    const int last = p.plan.pre_parts + (len > 0 ? p.by_suf_chunk.of(len + p.plan.suf_chunk - 1) : 0);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int j = first + i * 64 + lane;
-        m[i] = j < last ? ml[j * 2] : -INFINITY;
-        l[i] = j < last ? ml[j * 2 + 1] : 0.f;
-        top = fmaxf(top, m[i]);
+        const int j = i * 64 + lane;
+        const bool in = j >= first && j < last;
+        m[i] = in ? m[i] : -INFINITY;
+        l[i] = in ? l[i] : 0.f;
     }
+    const float top = wave_max(fmaxf(m[0], m[1])), base = top == -INFINITY ? 0.f : top * p.c;
 #pragma unroll
-    for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    const float base = top == -INFINITY ? 0.f : top * p.c;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        m[i] = l[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(fmaf(m[i], p.c, -base));  // now its weight
-        sum += l[i] * m[i];
-    }
-    sum = wave_sum(sum);
-    const int d = (lane % L) * 4, g = lane / L;
+    for (int i = 0; i < 2; ++i) m[i] = l[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(fmaf(m[i], p.c, -base));  // now its weight
+    const float sum = wave_sum_dpp(l[0] * m[0] + l[1] * m[1]);
     f32x4 acc{};
-    for (int j0 = first; j0 < last; j0 += GR) {
-        const int j = j0 + g, at = j - first;
-        const float w = __shfl(at < 64 ? m[0] : m[1], at & 63, 64);
-        if (j < last && d < p.D && w != 0.f)
-            acc += *reinterpret_cast<const f32x4*>(p.part + (r * p.parts + j) * p.D + d) * w;
+    for (int j0 = 0; j0 < last; j0 += U * GR) {
+        if (j0) ask(j0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * GR + g;
+            const float w = __shfl(j < 64 ? m[0] : m[1], j & 63, 64);
+            if (j < last && w != 0.f) acc += v[u] * w;
+        }
     }
 #pragma unroll
     for (int off = L; off < 64; off <<= 1)
@@ -514,10 +558,10 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendP p) {
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], off, 64);
     if (g == 0 && d < p.D) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        Pack<T, 4> v;
+        Pack<T, 4> o;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v.e[e] = (T)(acc[e] * inv);
-        store_pack<T, 4>(p.out, token * p.o_token + (r - token * p.H) * p.o_head + d, v);
+        for (int e = 0; e < 4; ++e) o.e[e] = (T)(acc[e] * inv);
+        store_pack<T, 4>(p.out, token * p.o_token + (r - token * p.H) * p.o_head + d, o);
     }
 }
 
@@ -534,6 +578,8 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_attend_args& a, const Atte
     p.S = a.n_seqs, p.n_q = a.n_q, p.H = a.n_heads, p.KV = c.n_kv_heads, p.G = a.n_heads / c.n_kv_heads, p.D = c.head_dim;
     p.c = a.scale * 1.44269504f;
     p.plan = plan;
+    p.by_S = Div(p.S), p.by_n_q = Div(p.n_q), p.by_H = Div(p.H), p.by_KV = Div(p.KV), p.by_G = Div(p.G);
+    p.by_pre_tiles = Div(plan.pre_tiles), p.by_suf_tiles = Div(plan.suf_tiles), p.by_suf_chunk = Div(plan.suf_chunk);
     p.parts = plan.pre_parts + plan.suf_parts;
     p.direct = plan.pre_parts == 0 && plan.suf_parts == 1;
     const int64_t rows = (int64_t)p.S * p.n_q * p.H;
