@@ -96,7 +96,7 @@ __device__ inline int swz(int row) {
 
 template <typename T, int DP, bool WIDE>
 struct Shape {
-    static constexpr int NW = WIDE || DP < 256 ? 4 : 2;         // waves
+    static constexpr int NW = WIDE ? 4 : 2;                     // waves
     static constexpr int KT = WIDE && DP < 256 ? 64 : 32;       // keys at a time
     static constexpr int CPR = DP / 8;                          // chunks per row
     static constexpr int RPI = 64 / CPR;                        // rows per copy instruction
@@ -116,10 +116,10 @@ struct Item {
     int len;               // the sequence's keys
 };
 
-// The part of the work that a workgroup takes; its sequence's length is not looked up yet.
+// Share `b` of the prefix's or of the sequences' work; a sequence's length is not looked up yet.
 template <int R>
-__device__ inline bool item_of(const AttendP& p, int b, Item* it) {
-    if (b < p.pre_items) {
+__device__ inline bool item_of(const AttendP& p, bool prefix, int b, Item* it) {
+    if (prefix) {
         // workgroups that follow each other run on different XCDs: the row tiles of the same keys
         // take every eighth workgroup, so that they share an L2
         const int eighth = b >> 3, turn = p.by_pre_tiles.of(eighth), group = turn * 8 + (b & 7);
@@ -134,7 +134,6 @@ __device__ inline bool item_of(const AttendP& p, int b, Item* it) {
         it->rows = p.S * p.n_q * p.G;
         return true;
     }
-    b -= p.pre_items;
     const int tile = b, rest = p.by_suf_tiles.of(b), of_kv = p.by_KV.of(rest), j = p.by_S.of(of_kv);
     it->row0 = (tile - rest * p.plan.suf_tiles) * R;
     it->kv = rest - of_kv * p.KV;
@@ -148,20 +147,15 @@ __device__ inline bool item_of(const AttendP& p, int b, Item* it) {
 }
 
 // MULTI: sequences with several query tokens each, whose last keys only some of them see.
+// The four arrays are four, not one: a read of one must not wait for the copy into another.
 template <typename T, int DP, bool WIDE, bool MULTI>
-__global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 && !MULTI ? 2 : 1)) void attend_kernel(const AttendP p) {
+__device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* k0, T* k1, T* v0, T* v1, float (*wave_ml)[2][32],
+                                       float* row_sum) {
     using Sh = Shape<T, DP, WIDE>;
     constexpr bool PIPE = WIDE && !MULTI;  // scores one tile ahead (MULTI's rare path leaves no registers)
     constexpr int NW = Sh::NW, KT = Sh::KT, CPR = Sh::CPR, NF = DP / 16, ND = DP / 32, SUB = KT / 32;
-    // four arrays, not one: a read of one must not wait for the copy into another
-    __shared__ __attribute__((aligned(16))) T k0[Sh::kBuf];
-    __shared__ __attribute__((aligned(16))) T k1[Sh::kBuf];
-    __shared__ __attribute__((aligned(16))) T v0[Sh::kBuf];
-    __shared__ __attribute__((aligned(16))) T v1[Sh::kBuf];
-    __shared__ float wave_ml[NW][2][32];
-    __shared__ float row_sum[32];
     Item it;
-    if (!item_of<Sh::kTileRows>(p, blockIdx.x, &it)) return;
+    if (!item_of<Sh::kTileRows>(p, prefix, b, &it)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, h = lane >> 5;
 
@@ -485,6 +479,39 @@ __global__ __launch_bounds__((Shape<T, DP, WIDE>::NW * 64), (WIDE && DP <= 128 &
     }
 }
 
+// Which shapes a launch holds.  BOTH: a wide prefix beside narrow sequences, eight workgroups of one after
+// eight of the other (one for each XCD).
+enum Roles { NARROW, WIDE_ROWS, BOTH };
+
+template <typename T, int DP, Roles ROLES, bool MULTI>
+__global__ __launch_bounds__((Shape<T, DP, ROLES != NARROW>::NW * 64), (ROLES != NARROW && DP <= 128 && (ROLES == BOTH || !MULTI) ? 2 : 1)) void attend_kernel(const AttendP p) {
+    constexpr int kBuf = Shape<T, DP, ROLES != NARROW>::kBuf;
+    static_assert(ROLES != BOTH || kBuf == Shape<T, DP, false>::kBuf, "one size serves both shapes");
+    __shared__ __attribute__((aligned(16))) T k0[kBuf], k1[kBuf], v0[kBuf], v1[kBuf];
+    __shared__ float wave_ml[Shape<T, DP, false>::NW][2][32], row_sum[32];
+    int b = blockIdx.x;
+    if constexpr (ROLES == BOTH) {
+        const int both = 2 * min(p.pre_items, p.suf_items / 8 * 8);  // pre_items is a multiple of 8
+        bool prefix;
+        if (b < both) {
+            prefix = !((b >> 3) & 1);
+            b = (b >> 4) * 8 + (b & 7);
+        } else {
+            prefix = b - both / 2 < p.pre_items;
+            b -= both / 2;
+            if (!prefix) b -= p.pre_items - both / 2;
+        }
+        if (prefix) {
+            attend<T, DP, true, false>(p, true, b, k0, k1, v0, v1, wave_ml, row_sum);
+        } else if (threadIdx.x < Shape<T, DP, false>::NW * 64) {
+            attend<T, DP, false, MULTI>(p, false, b, k0, k1, v0, v1, wave_ml, row_sum);
+        }
+    } else {
+        const bool prefix = b < p.pre_items;
+        attend<T, DP, ROLES == WIDE_ROWS, MULTI>(p, prefix, prefix ? b : b - p.pre_items, k0, k1, v0, v1, wave_ml, row_sum);
+    }
+}
+
 template <int CTRL, int ROWS>
 __device__ inline float max_dpp(float v) {
     const int x = __float_as_int(v);
@@ -586,28 +613,38 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_attend_args& a, const Atte
     p.part = static_cast<float*>(ws);
     p.ml = p.part + rows * p.parts * p.D;
     const int pre = (int)round_up(plan.pre_parts * p.KV, 8) * plan.pre_tiles, suf = plan.suf_parts * p.S * p.KV * plan.suf_tiles;
-    auto go = [&](bool wide, int pre_items, int suf_items) {
+    auto go = [&](Roles roles, int pre_items, int suf_items) {
         p.pre_items = pre_items;
         p.suf_items = suf_items;
-        if (pre_items + suf_items == 0) return hipSuccess;
-        const dim3 grid((unsigned)(pre_items + suf_items)), wide_wg(Shape<T, DP, true>::NW * 64), narrow_wg(Shape<T, DP, false>::NW * 64);
+        const dim3 grid((unsigned)(pre_items + suf_items)), narrow_wg(Shape<T, DP, false>::NW * 64), wide_wg(256);
         const bool multi = p.n_q > 1 && suf_items;
-        if (wide && multi)
-            hipLaunchKernelGGL((attend_kernel<T, DP, true, true>), grid, wide_wg, 0, st, p);
-        else if (wide)
-            hipLaunchKernelGGL((attend_kernel<T, DP, true, false>), grid, wide_wg, 0, st, p);
-        else if (multi)
-            hipLaunchKernelGGL((attend_kernel<T, DP, false, true>), grid, narrow_wg, 0, st, p);
-        else
-            hipLaunchKernelGGL((attend_kernel<T, DP, false, false>), grid, narrow_wg, 0, st, p);
+        if (roles == NARROW) {
+            if (multi)
+                hipLaunchKernelGGL((attend_kernel<T, DP, NARROW, true>), grid, narrow_wg, 0, st, p);
+            else
+                hipLaunchKernelGGL((attend_kernel<T, DP, NARROW, false>), grid, narrow_wg, 0, st, p);
+        } else if (roles == WIDE_ROWS) {
+            if (multi)
+                hipLaunchKernelGGL((attend_kernel<T, DP, WIDE_ROWS, true>), grid, wide_wg, 0, st, p);
+            else
+                hipLaunchKernelGGL((attend_kernel<T, DP, WIDE_ROWS, false>), grid, wide_wg, 0, st, p);
+        } else if constexpr (DP <= 128) {
+            if (multi)
+                hipLaunchKernelGGL((attend_kernel<T, DP, BOTH, true>), grid, wide_wg, 0, st, p);
+            else
+                hipLaunchKernelGGL((attend_kernel<T, DP, BOTH, false>), grid, wide_wg, 0, st, p);
+        }
         return hipGetLastError();
     };
+    const Roles pre_role = plan.pre_wide ? WIDE_ROWS : NARROW, suf_role = plan.suf_wide ? WIDE_ROWS : NARROW;
     hipError_t e;
-    if (plan.pre_parts == 0 || plan.pre_wide == plan.suf_wide || suf == 0) {
-        e = go(pre ? plan.pre_wide : plan.suf_wide, pre, suf);
+    if (pre == 0 || suf == 0 || pre_role == suf_role) {
+        e = go(pre ? pre_role : suf_role, pre, suf);
+    } else if (plan.together) {
+        e = go(BOTH, pre, suf);
     } else {
-        e = go(plan.pre_wide, pre, 0);
-        if (e == hipSuccess) e = go(plan.suf_wide, 0, suf);
+        e = go(pre_role, pre, 0);
+        if (e == hipSuccess) e = go(suf_role, 0, suf);
     }
     if (e != hipSuccess || p.direct) return e;
     hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, p);
@@ -631,22 +668,25 @@ bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes,
     plan->suf_wide = suf_rows > 32;
     plan->pre_tiles = (int)ceil_div(pre_rows, plan->pre_wide ? 128 : 32);
     plan->suf_tiles = (int)ceil_div(suf_rows, plan->suf_wide ? 128 : 32);
-    // Workgroups that run at once (by shared memory), and what a workgroup costs beyond its keys (the
-    // chain of loads before its first product, and the join), in keys.
-    auto slots = [&](bool wide) { return n_cu * (wide || c.head_dim <= 64 ? 2 : 1); };
-    constexpr int kStart = 192;
-    // The chunk (a multiple of 128 keys) with the least rounds x (chunk + start), at most half of
-    // kMaxParts parts and half of the workspace for each of prefix and sequences.
-    auto choose = [&](int64_t n_pre, int64_t pre_keys, int64_t n_suf, int64_t suf_keys, int n_slots) {
+    // Workgroups that run at once on a compute unit (by shared memory and registers); the time of a key
+    // and of a start and end, as measured with the unit full (us).
+    const int wide_cu = c.head_dim <= 128 ? 2 : 1, narrow_cu = c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 2 : 1;
+    const double by_dim = (c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256) / 128.0;
+    auto item_us = [&](bool wide, int64_t chunk) { return chunk * by_dim * (wide ? 0.050 : 0.038) + (wide ? 4.0 : 5.5); };
+    const double part_us = 2.0 * part_bytes / 5e6;  // written, and read by the join
+    // The chunk (a multiple of 128 keys) with the least estimated time, at most half of kMaxParts parts
+    // and half of the workspace for each of prefix and sequences: rounds of workgroups, and the parts.
+    auto choose = [&](bool wide, int64_t n_pre, int64_t pre_keys, int64_t n_suf, int64_t suf_keys) {
         int64_t best = 0;
         double least = 0;
+        const int64_t slots = (int64_t)n_cu * (wide ? wide_cu : narrow_cu);
         const int64_t most = round_up((size_t)std::max<int64_t>(std::max(pre_keys, suf_keys), 1), 128);
         for (int64_t chunk = 128;; chunk = std::min(most, chunk + std::max<int64_t>(128, chunk / 8 / 128 * 128))) {
-            const int64_t pp = ceil_div(pre_keys, chunk), sp = ceil_div(suf_keys, chunk);
+            const int64_t pp = ceil_div(pre_keys, chunk), sp = ceil_div(suf_keys, chunk), items = n_pre * pp + n_suf * sp;
             const bool fits = pp <= kMaxParts / 2 && sp <= kMaxParts / 2 && std::max(pp, sp) * part_bytes <= (int64_t)ws_bytes / 2 &&
-                              (n_pre + 8) * (pp + 8) + n_suf * sp < (int64_t)1 << 31;
+                              (n_pre + 8) * (pp + 8) + n_suf * sp < (int64_t)1 << 30;
             if (fits) {
-                const double t = (double)ceil_div(n_pre * pp + n_suf * sp, n_slots) * (chunk + kStart);
+                const double t = item_us(wide, chunk) * ceil_div(items, slots) + (pp + sp) * part_us;
                 if (!best || t < least) best = chunk, least = t;
             }
             if (chunk >= most) break;
@@ -656,15 +696,20 @@ bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes,
     const int64_t n_pre = a.prefix_len ? (int64_t)c.n_kv_heads * plan->pre_tiles : 0;
     const int64_t n_suf = (int64_t)a.n_seqs * c.n_kv_heads * plan->suf_tiles;
     if (plan->pre_wide == plan->suf_wide || !a.prefix_len) {
-        plan->pre_chunk = plan->suf_chunk = choose(n_pre, a.prefix_len, n_suf, a.max_len, slots(plan->suf_wide));
+        plan->pre_chunk = plan->suf_chunk = choose(plan->suf_wide, n_pre, a.prefix_len, n_suf, a.max_len);
     } else {
-        plan->pre_chunk = choose(n_pre, a.prefix_len, 0, 0, slots(plan->pre_wide));
-        plan->suf_chunk = choose(0, 0, n_suf, a.max_len, slots(plan->suf_wide));
+        plan->pre_chunk = choose(plan->pre_wide, n_pre, a.prefix_len, 0, 0);
+        plan->suf_chunk = choose(plan->suf_wide, 0, 0, n_suf, a.max_len);
     }
     if (!plan->pre_chunk || !plan->suf_chunk) return false;
     plan->pre_parts = (int)ceil_div(a.prefix_len, plan->pre_chunk);
     plan->suf_parts = (int)ceil_div(a.max_len, plan->suf_chunk);
     if (plan->pre_parts + plan->suf_parts == 0) plan->suf_parts = 1;  // no key anywhere: rows of zeros
+    // A wide prefix and narrow sequences in one launch where all their workgroups run at once (5 x 4 tokens
+    // behind 333 keys 20.4 -> 16.3 us).  Larger ones apart: the sequences' stream through the caches takes
+    // from the prefix more than running beside it gives (64 sequences behind 32768 keys 149 -> 184 us).
+    plan->together = plan->pre_parts && plan->suf_parts && plan->pre_wide && !plan->suf_wide && c.head_dim <= 128 &&
+                     n_pre * plan->pre_parts + 8 * plan->pre_tiles + n_suf * plan->suf_parts <= 2 * n_cu;
     plan->bytes = (size_t)((plan->pre_parts + plan->suf_parts) * part_bytes);
     return true;
 }
