@@ -105,6 +105,12 @@ struct Shape {
     static constexpr int kTileRows = WIDE ? 128 : 32;
 };
 
+// The value of lane ^ 32.
+__device__ inline float other_half(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
 // What a workgroup works on.
 struct Item {
     const int32_t* table;  // page ids
@@ -210,13 +216,36 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         return (unsigned)id < (unsigned)p.n_pages && key < it.end ? at : (int64_t)-1;
     };
     // Copies a tile's rows, RPI of them an instruction: lane -> row lane / CPR, chunk lane % CPR permuted.
+    // 16 rows that are all there lie in one page (of 16 keys or more): one address for the wave and
+    // fixed places for the lanes.  Otherwise each lane asks the row's lane for its address.
     const int c_row = lane / CPR;
+    const bool regular = page_mask >= 15 && p.D == DP && p.token_stride < 1 << 24;
+    uint32_t c_at[16 / Sh::RPI];  // bytes
+#pragma unroll
+    for (int i = 0; i < 16 / Sh::RPI; ++i) {
+        const int r = i * Sh::RPI + c_row;
+        c_at[i] = ((uint32_t)r * (uint32_t)p.token_stride + ((lane % CPR) ^ swz<CPR>(r)) * 8) * sizeof(T);
+    }
     auto copy = [&](const T* base, int64_t at, T* buf) {
         T* dst = buf + wave * Sh::kRows * DP;
+        const int first = WIDE ? wave * Sh::kRows : 0;
+        const uint32_t all = Sh::kRows == 32 ? ~0u : (1u << Sh::kRows % 32) - 1;
+        if (Sh::kRows % 16 == 0 && regular && ((uint32_t)(__ballot(at >= 0) >> first) & all) == all) {
+#pragma unroll
+            for (int g = 0; g < Sh::kRows / 16; ++g) {
+                const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)at, first + g * 16);
+                const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(at >> 32), first + g * 16);
+                const char* rows = reinterpret_cast<const char*>(base + (int64_t)(((uint64_t)hi << 32) | lo));
+#pragma unroll
+                for (int i = 0; i < 16 / Sh::RPI; ++i)
+                    __builtin_amdgcn_global_load_lds((gptr)(rows + c_at[i]), (lptr)(dst + g * 16 * DP + i * 512), 16, 0, 0);
+            }
+            return;
+        }
         const uint64_t from = (uint64_t)(at < 0 ? zero : base + at);
 #pragma unroll
         for (int i = 0; i < Sh::kRows / Sh::RPI; ++i) {
-            const int r0 = (WIDE ? wave * Sh::kRows : 0) + i * Sh::RPI;
+            const int r0 = first + i * Sh::RPI;
             const int chunk = (lane % CPR) ^ swz<CPR>(c_row) ^ swz<CPR>(r0);  // the bits of the two do not mix
             const uint32_t lo = __shfl((uint32_t)from, r0 + c_row, 64), hi = __shfl((uint32_t)(from >> 32), r0 + c_row, 64);
             const T* row = reinterpret_cast<const T*>(((uint64_t)hi << 32) | lo);
@@ -256,8 +285,8 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     };
     // One tile.  PIPE: its scores are in s already, and those of the next tile (keys in kbuf) are
     // computed while its exponentials are: matrix and vector instructions of one wave run side by
-    // side, so the next copies and the next maximum are part of the same stretch of code.
-    auto use = [&](Scores& s, int key0, int64_t at, const T* vbuf, const T* kbuf, auto&& copies) {
+    // side, so the next maximum is part of the same stretch of code.
+    auto use = [&](Scores& s, int key0, int64_t at, const T* vbuf, const T* kbuf) {
         if (!PIPE) {
             s = scores(kbuf);
             largest(s);
@@ -276,7 +305,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
             }
             largest(s);
         }
-        const float top = fmaxf(s.top, __shfl_xor(s.top, 32, 64));
+        const float top = fmaxf(s.top, other_half(s.top));
         const float next = fmaxf(m, top), base = next == -INFINITY ? 0.f : next * p.c;
         if (__any(next > m)) {
             const float scale = __builtin_amdgcn_exp2f(fmaf(m, p.c, -base));  // m = -inf: 0
@@ -286,10 +315,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
             m = next;
         }
         Scores after;
-        if (PIPE) {
-            copies();
-            after = scores(kbuf);
-        }
+        if (PIPE) after = scores(kbuf);
         vec8<T> pr[2 * SUB];
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
@@ -376,12 +402,11 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
             const int64_t at2 = place(key + 2 * kStep, id2);
             landed();
             id2 = page_id(key + 3 * kStep);
-            auto copies = [&] {
+            if (PIPE || key + kStep < it.end) {
                 copy(kbase, PIPE ? at2 : at1, PIPE ? ka : kb);
                 copy(vbase, at1, vb);
-            };
-            if (PIPE ? idle_wave : key + kStep < it.end) copies();
-            if (!idle_wave) use(s, key, at0, va, PIPE ? kb : ka, copies);
+            }
+            if (!idle_wave) use(s, key, at0, va, PIPE ? kb : ka);
             key += kStep;
             at0 = at1, at1 = at2;
         };
@@ -393,7 +418,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         }
         landed();  // nothing is under way when the arrays are used again
     }
-    l += __shfl_xor(l, 32, 64);
+    l += other_half(l);
 
     const int64_t out_row = token * p.H + head;
     // four elements of a row: the part's sums, or with a single part the result
