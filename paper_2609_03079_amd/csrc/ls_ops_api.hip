@@ -140,7 +140,7 @@ ls_status ls_norm_residual(ls_ops* c, const ls_norm_args* a) {
                    element_aligned(a->gate, a->dtype) && element_aligned(a->post_weight, a->dtype) &&
                    element_aligned(a->pre_weight, a->dtype) && element_aligned(a->h, a->dtype),
                "a pointer is not aligned to its type");
-    return launched(c, ls::launch_norm(*a, c->n_cu, c->stream), "ls_norm_residual");
+    return launched(c, ls::launch_norm(*a, c->stream), "ls_norm_residual");
 }
 
 ls_status ls_linear_i8(ls_ops* c, const ls_linear_i8_args* a) {
@@ -190,7 +190,7 @@ ls_status ls_kv_append(ls_ops* c, const ls_kv_cache* kv, const ls_append_args* a
     LS_REQUIRE(element_aligned(a->k, kv->dtype) && element_aligned(a->v, kv->dtype) && element_aligned(a->q, kv->dtype) &&
                    element_aligned(a->q_out, kv->dtype) && ls::aligned(a->positions, 4) && ls::aligned(a->slots, 4) && ls::aligned(a->cos_sin, 4),
                "a pointer is not aligned to its type");
-    return launched(c, ls::launch_append(*kv, *a, c->n_cu, c->stream), "ls_kv_append");
+    return launched(c, ls::launch_append(*kv, *a, c->stream), "ls_kv_append");
 }
 
 ls_status ls_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a) {

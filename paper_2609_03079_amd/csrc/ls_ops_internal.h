@@ -11,10 +11,10 @@
 namespace ls {
 
 // ---- norms around a block (ls_rows.hip) ----------------------------------------------------
-hipError_t launch_norm(const ls_norm_args& a, int n_cu, hipStream_t st);
+hipError_t launch_norm(const ls_norm_args& a, hipStream_t st);
 
 // ---- append to the paged cache (ls_rows.hip) -----------------------------------------------
-hipError_t launch_append(const ls_kv_cache& c, const ls_append_args& a, int n_cu, hipStream_t st);
+hipError_t launch_append(const ls_kv_cache& c, const ls_append_args& a, hipStream_t st);
 
 // ---- 8-bit products (ls_linear.hip) --------------------------------------------------------
 // Workspace that the call needs: the quantised tokens and their scales, where they go through memory.
