@@ -86,22 +86,24 @@ __device__ inline float token_scale(uint32_t m, float* top) {
 
 // round(127 x / max), ties to even.  The product with the rounded inverse is off by less than 1e-4,
 // so away from a tie it rounds to the same integer; near one the quotient decides (for 16-bit x
-// 127 x is exact and the quotient rounded once, so a tie is seen as one).  A division for every
-// element made the kernel twice as slow (2048 x 8192 bfloat16: 17.5 us).
+// 127/128 x is exact, and cannot overflow as 127 x can, and the quotient rounded once, so a tie is
+// seen as one).  A division for every element made the kernel twice as slow.
 __device__ inline int quantise(float x, float top, float inv) {
     const float p = x * inv;
     float r = rintf(p);
-    if (fabsf(p - r) > 0.4999f) r = rintf(x * 127.f / top);
+    if (fabsf(p - r) > 0.4999f) r = rintf(x * 0.9921875f / top * 128.f);
     return (int)r;
 }
 
-// One workgroup per token; 8 elements per thread and step.
-template <typename T>
-__global__ __launch_bounds__(256) void quantise_kernel(const void* x, int64_t x_stride, int k, int8_t* q, float* s) {
-    __shared__ uint32_t part[4];
+// One workgroup of NT threads per token; 8 elements per thread and step, the first kHeld of them kept in
+// registers between the maximum and the division.  2048 x 8192 bfloat16: 16 us; with a thread for every
+// vector 22.2, a workgroup's chain of loads, maximum and barrier being longer than its work.
+template <typename T, int NT, int kHeld>
+__global__ __launch_bounds__(NT) void quantise_kernel(const void* x, int64_t x_stride, int k, int8_t* q, float* s) {
+    __shared__ uint32_t part[NT / 64];
     const int64_t t = blockIdx.x;
     const T* row = static_cast<const T*>(x) + t * x_stride;
-    constexpr int kHeld = 8, kStep = 256 * 8;  // vectors a thread keeps in registers (rows of up to 16384 elements)
+    constexpr int kStep = NT * 8;
     Pack<T, 8> v[kHeld];
     uint32_t m = 0;
 #pragma unroll
@@ -120,7 +122,8 @@ __global__ __launch_bounds__(256) void quantise_kernel(const void* x, int64_t x_
     m = wave_max(m);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
     __syncthreads();
-    m = max(max(part[0], part[1]), max(part[2], part[3]));
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) m = max(m, part[w]);
     float top;
     const float scale = token_scale(m, &top), inv = top > 0.f ? 127.f / top : 0.f;
     if (threadIdx.x == 0) s[t] = scale;
@@ -136,6 +139,20 @@ __global__ __launch_bounds__(256) void quantise_kernel(const void* x, int64_t x_
         if (e < k) write(e, v[c]);
     }
     for (int e = (int)threadIdx.x * 8 + kHeld * kStep; e < k; e += kStep) write(e, load_pack<T, 8>(row, e));
+}
+
+template <typename T>
+hipError_t quantise_rows(const ls_linear_i8_args& a, int8_t* q, float* s, hipStream_t st) {
+    const dim3 grid(a.n_tokens);
+    if (a.k <= 2048)
+        hipLaunchKernelGGL((quantise_kernel<T, 256, 1>), grid, dim3(256), 0, st, a.x, a.x_stride, a.k, q, s);
+    else if (a.k <= 4096)
+        hipLaunchKernelGGL((quantise_kernel<T, 256, 2>), grid, dim3(256), 0, st, a.x, a.x_stride, a.k, q, s);
+    else if (a.k <= 8192)
+        hipLaunchKernelGGL((quantise_kernel<T, 256, 4>), grid, dim3(256), 0, st, a.x, a.x_stride, a.k, q, s);
+    else
+        hipLaunchKernelGGL((quantise_kernel<T, 512, 4>), grid, dim3(512), 0, st, a.x, a.x_stride, a.k, q, s);
+    return hipGetLastError();
 }
 
 // ---- tiles through shared memory -----------------------------------------------------------
@@ -587,14 +604,9 @@ hipError_t linear(const ls_linear_i8_args& a, LinearP p, uint8_t* ws, size_t ws_
         }
         int8_t* q = reinterpret_cast<int8_t*>(ws);
         float* s = reinterpret_cast<float*>(ws + round_up((size_t)a.n_tokens * a.k, 256));
-        const dim3 grid(a.n_tokens), block(256);
-        if (a.x_type == LS_F32)
-            hipLaunchKernelGGL(quantise_kernel<float>, grid, block, 0, st, a.x, a.x_stride, a.k, q, s);
-        else if (a.x_type == LS_F16)
-            hipLaunchKernelGGL(quantise_kernel<_Float16>, grid, block, 0, st, a.x, a.x_stride, a.k, q, s);
-        else
-            hipLaunchKernelGGL(quantise_kernel<__bf16>, grid, block, 0, st, a.x, a.x_stride, a.k, q, s);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = a.x_type == LS_F32   ? quantise_rows<float>(a, q, s, st)
+                             : a.x_type == LS_F16 ? quantise_rows<_Float16>(a, q, s, st)
+                                                  : quantise_rows<__bf16>(a, q, s, st);
         if (e != hipSuccess) return e;
         p.q = q, p.q_stride = a.k, p.s = s;
     }

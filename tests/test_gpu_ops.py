@@ -218,6 +218,28 @@ def test_linear_extreme_sums_and_tokens(ops):
     ops.ls_linear_i8(x[:0], w, ws, out[:0])
 
 
+@pytest.mark.parametrize("k", [2048, 2064, 4096, 4112, 8192, 8208, 16384, 16400, 20000])
+@pytest.mark.parametrize("x_type", ["f32", "f16", "bf16"])
+def test_linear_row_lengths(ops, k, x_type):
+    check_linear(ops, 9, k, 33, x_type, "f32", seed=k)
+
+
+@pytest.mark.parametrize("T", [3, 8])
+@pytest.mark.parametrize("x_type,top", [("f32", 3.3e38), ("bf16", 3.3e38), ("f16", 65504.0), ("f32", 1.6e-36), ("bf16", 1.6e-36)])
+def test_linear_tokens_at_the_ends_of_their_type(ops, T, x_type, top):
+    # every half step of a token whose largest magnitude is about the type's, or about the least that has a scale:
+    # seen through a w with a one a row.  A tie may fall to either side in fp32, nothing may leave the step.
+    dt = TYPES[x_type]
+    k = 256
+    steps = torch.cat([torch.arange(-127, 127, dtype=torch.float64) + 0.5, torch.tensor([127.0, 0.0], dtype=torch.float64)])
+    x = (steps / 127 * top).to(dt).repeat(T, 1).to(DEV)
+    w = torch.eye(k, dtype=torch.int8, device=DEV)
+    out = torch.empty((T, k), device=DEV)
+    ops.ls_linear_i8(x, w, torch.ones(k, device=DEV), out)
+    s = x.double().abs().amax(1, keepdim=True) / 127
+    assert float((out.double() / s - x.double() / s).abs().max()) <= 0.5001
+
+
 # ---- append ----------------------------------------------------------------------------------------
 def make_cache(pages, kv, page, dim, dt, seed, layout="head"):
     shape = (pages, kv, page, dim) if layout == "head" else (pages, page, kv, dim)
