@@ -33,7 +33,7 @@ struct LinearP {
     void* out;
     int64_t out_stride;
     int T, k, n;
-    int slices, splits;  // tiles: 64-byte slices of k per split; splits of k
+    int slices, splits;  // tiles: 128-byte slices of k per split; splits of k
     int32_t* part;       // [splits][T][n] sums of the splits
 };
 
@@ -157,29 +157,32 @@ hipError_t quantise_rows(const ls_linear_i8_args& a, int8_t* q, float* s, hipStr
 
 // ---- tiles through shared memory -----------------------------------------------------------
 // out tile of BM tokens by BN channels; WM x WN waves, each with a (BM / WM) x (BN / WN) part in
-// 32 x 32 matrix tiles.  Both operands come in 64-byte slices of k, copied straight to a ring of
-// four slices in shared memory: a copy takes 1 to 2 us under load and a slice is multiplied in a
-// quarter of that, so three slices are under way while one is used.  (Two slices of 128 bytes, with
-// one under way, took 1.8 us a slice on the 128 x 128 tile, whose products take 0.5.)
-// A row's four 16-byte chunks lie at places permuted by its number, so that the 16 rows a read
+// 32 x 32 matrix tiles.  Both operands come in 128-byte slices of k, copied straight to a ring of S
+// slices in shared memory, S - 1 of them under way while one is used.  (A whole line of memory a row:
+// with slices of 64 bytes, each line asked for twice, the largest tiles' copies alone took 82 us of
+// 2048 x 8192 x 8192 in place of 71, and the product 143 in place of 125.)  A slice is multiplied in
+// four steps; a step's operands are read from shared memory while the products of the step before
+// run.  What is left is the products themselves: without any copies they take 102 us with random
+// operands, 73 with zeros, the clock falling under their load.
+// A row's eight 16-byte chunks lie at places permuted by its number, so that the 16 rows a read
 // touches together lie in different banks.
-constexpr int kSlice = 64;
+constexpr int kSlice = 128;
 
-__device__ inline int place(int row, int chunk) { return chunk ^ ((row >> 2) & 3); }
+__device__ inline int place(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
 
-// A workgroup's copies of ROWS rows, slice by slice: 16 rows an instruction.
+// A workgroup's copies of ROWS rows, slice by slice: 8 rows an instruction.
 template <int ROWS, int WAVES>
 struct Fetch {
-    static constexpr int N = ROWS / (16 * WAVES);
-    static_assert(ROWS % (16 * WAVES) == 0, "whole instructions");
+    static constexpr int N = ROWS / (8 * WAVES);
+    static_assert(ROWS % (8 * WAVES) == 0, "whole instructions");
     const int8_t* src[N];  // this lane's chunk of a slice at 0
 
     __device__ inline void start(const int8_t* base, int64_t stride, int row0, int rows) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int r = (i * WAVES + wave) * 16 + (lane >> 2);
-            src[i] = base + (int64_t)min(row0 + r, rows - 1) * stride + place(r, lane & 3) * 16;
+            const int r = (i * WAVES + wave) * 8 + (lane >> 3);
+            src[i] = base + (int64_t)min(row0 + r, rows - 1) * stride + place(r, lane & 7) * 16;
         }
     }
     // The slice at k0, of which bytes below `last` count.
@@ -187,9 +190,9 @@ struct Fetch {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int r0 = (i * WAVES + wave) * 16;
+            const int r0 = (i * WAVES + wave) * 8;
             const int8_t* from = src[i] + k0;
-            if (k0 + kSlice > last && k0 + place(r0 + (lane >> 2), lane & 3) * 16 >= last) from = reinterpret_cast<const int8_t*>(g_zero_chunk);
+            if (k0 + kSlice > last && k0 + place(r0 + (lane >> 3), lane & 7) * 16 >= last) from = reinterpret_cast<const int8_t*>(g_zero_chunk);
             __builtin_amdgcn_global_load_lds((gptr)from, (lptr)(lds + r0 * kSlice), 16, 0, 0);
         }
     }
@@ -197,27 +200,41 @@ struct Fetch {
 
 template <int BM, int BN, int WM, int WN>
 struct Tile {
-    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32, kAll = TM * TN;
     i32x16 acc[TM][TN];
+    i32x4 x[2][TM], y[2][TN];  // the operands of the present step and of the next
 
-    __device__ inline void multiply(const int8_t* a, const int8_t* b) {
+    // Operands R: step kk (32 bytes of k) of a slice.
+    template <int R>
+    __device__ inline void read(const int8_t* a, const int8_t* b, int kk) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5;
         const int m0 = (wave / WN) * (BM / WM), n0 = (wave % WN) * (BN / WN);
 #pragma unroll
-        for (int kk = 0; kk < kSlice / 32; ++kk) {
-            i32x4 x[TM], y[TN];
+        for (int i = 0; i < TM; ++i)
+            x[R][i] = *reinterpret_cast<const i32x4*>(a + (m0 + i * 32 + r) * kSlice + place(r, kk * 2 + h) * 16);
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-                x[i] = *reinterpret_cast<const i32x4*>(a + (m0 + i * 32 + r) * kSlice + place(r, kk * 2 + h) * 16);
+        for (int j = 0; j < TN; ++j)
+            y[R][j] = *reinterpret_cast<const i32x4*>(b + (n0 + j * 32 + r) * kSlice + place(r, kk * 2 + h) * 16);
+    }
+    // The products of operands R from the FROM-th on, below the TO-th.
+    template <int R, int FROM, int TO>
+    __device__ inline void multiply() {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
-                y[j] = *reinterpret_cast<const i32x4*>(b + (n0 + j * 32 + r) * kSlice + place(r, kk * 2 + h) * 16);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[i], y[j], acc[i][j], 0, 0, 0);
-        }
+                if (i * TN + j >= FROM && i * TN + j < TO)
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[R][i], y[R][j], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // The products of operands R; once the first has them (the wait for a read is for all reads), `next`
+    // asks for those of the next step.
+    template <int R, typename F>
+    __device__ inline void step(F&& next) {
+        multiply<R, 0, 1>();
+        next();
+        __builtin_amdgcn_sched_barrier(0);
+        multiply<R, 1, kAll>();
     }
 };
 
@@ -234,11 +251,14 @@ __device__ inline void arrive() {
 
 // k in p.splits parts, one workgroup each (blockIdx.y): where the tiles alone would leave compute
 // units idle.  Their sums meet in finish_kernel.
-template <typename O, int BM, int BN, int WM, int WN>
+template <typename O, int BM, int BN, int WM, int WN, int S>
 __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void tile_kernel(const LinearP p, int tiles_n) {
-    // eight arrays, not one: a read of one slice must not wait for the copies into the others
-    __shared__ __attribute__((aligned(16))) int8_t a0[BM * kSlice], a1[BM * kSlice], a2[BM * kSlice], a3[BM * kSlice];
-    __shared__ __attribute__((aligned(16))) int8_t b0[BN * kSlice], b1[BN * kSlice], b2[BN * kSlice], b3[BN * kSlice];
+    static_assert(S >= 2 && S <= 4, "the ring");
+    // an array for each slice, not one: a read of one must not wait for the copies into the others
+    constexpr int kA = BM * kSlice, kB = BN * kSlice;
+    __shared__ __attribute__((aligned(16))) int8_t a0[kA], a1[kA], a2[S > 2 ? kA : 16], a3[S > 3 ? kA : 16];
+    __shared__ __attribute__((aligned(16))) int8_t b0[kB], b1[kB], b2[S > 2 ? kB : 16], b3[S > 3 ? kB : 16];
+    __shared__ float scale[BM];  // of the tokens
     const int t0 = (blockIdx.x / tiles_n) * BM, n0 = (blockIdx.x % tiles_n) * BN;
     const int first = blockIdx.y * p.slices * kSlice, last = min(p.k, first + p.slices * kSlice);
     Tile<BM, BN, WM, WN> tile;
@@ -253,10 +273,10 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void tile_kernel(const L
     constexpr int kCopies = fa.N + fb.N;  // of a slice, by each wave
     // Slices are taken in turn from one that depends on the workgroup (rows a power of two apart would
     // all ask the same memory channel at once: 2048 x 8192 x 10240 241 -> 223 us), and past the end
-    // slices of zeros: the count under way stays the same, and the ring's four steps are one loop
+    // slices of zeros: the count under way stays the same, and the ring's S steps are one loop
     // without exits (whose copies of the sums cost more than the products).
     const int n_slices = (last - first + kSlice - 1) / kSlice;
-    const int turn = (int)(blockIdx.x % tiles_n / 8 % 4) * 4 % n_slices;
+    const int turn = (int)(blockIdx.x % tiles_n / 8 % 4) * 2 % n_slices;
     auto copy = [&](int i, int8_t* a, int8_t* b) {
         int at = i + turn;
         at -= at >= n_slices ? n_slices : 0;
@@ -264,38 +284,72 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void tile_kernel(const L
         fa.copy(k0, last, a);
         fb.copy(k0, last, b);
     };
+    const float own = p.s[min(t0 + (int)threadIdx.x % BM, p.T - 1)];
     copy(0, a0, b0);
     copy(1, a1, b1);
-    copy(2, a2, b2);
-    auto step = [&](int i, const int8_t* a, const int8_t* b, int8_t* a_next, int8_t* b_next) {
-        arrive<2 * kCopies>();
-        copy(i + 3, a_next, b_next);
-        tile.multiply(a, b);
+    if constexpr (S > 2) copy(2, a2, b2);
+    if constexpr (S > 3) copy(3, a3, b3);
+    scale[threadIdx.x % BM] = own;
+    arrive<(S - 1) * kCopies>();
+    tile.template read<0>(a0, b0, 0);
+    // Slice i, the operands of whose first step are on their way.  Before its last step everything of it
+    // has been read, so its place is free for slice i + S, and slice i + 1 has landed.
+    auto slice = [&](int i, int8_t* a, int8_t* b, const int8_t* a_next, const int8_t* b_next) {
+        tile.template step<0>([&] { tile.template read<1>(a, b, 1); });
+        tile.template step<1>([&] { tile.template read<0>(a, b, 2); });
+        tile.template step<0>([&] { tile.template read<1>(a, b, 3); });
+        arrive<(S - 2) * kCopies>();
+        tile.template step<1>([&] {
+            tile.template read<0>(a_next, b_next, 0);
+            copy(i + S, a, b);
+        });
     };
-    for (int i = 0; i < n_slices; i += 4) {
-        step(i, a0, b0, a3, b3);
-        step(i + 1, a1, b1, a0, b0);
-        step(i + 2, a2, b2, a1, b1);
-        step(i + 3, a3, b3, a2, b2);
+    for (int i = 0; i < n_slices; i += S) {
+        slice(i, a0, b0, a1, b1);
+        if constexpr (S == 2) slice(i + 1, a1, b1, a0, b0);
+        if constexpr (S > 2) slice(i + 1, a1, b1, a2, b2);
+        if constexpr (S == 3) slice(i + 2, a2, b2, a0, b0);
+        if constexpr (S > 3) {
+            slice(i + 2, a2, b2, a3, b3);
+            slice(i + 3, a3, b3, a0, b0);
+        }
     }
     __builtin_amdgcn_s_waitcnt(0x0070);  // no copy into shared memory outlives the workgroup
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int m0 = t0 + (wave / WN) * (BM / WM), c0 = n0 + (wave % WN) * (BN / WN) + (lane & 31);
+    auto token = [&](int i, int g) { return m0 + i * 32 + 8 * (g / 4) + 4 * (lane >> 5) + g % 4; };
+    if (p.splits > 1) {
+#pragma unroll
+        for (int i = 0; i < tile.TM; ++i)
+#pragma unroll
+            for (int g = 0; g < 16; ++g)
+#pragma unroll
+                for (int j = 0; j < tile.TN; ++j) {
+                    const int t = token(i, g), n = c0 + j * 32;
+                    if (t < p.T && n < p.n) p.part[((int64_t)blockIdx.y * p.T + t) * p.n + n] = tile.acc[i][j][g];
+                }
+        return;
+    }
+    // The scales before the first store (a load after a store waits for it), those of the tokens from
+    // shared memory: with loads in between, the 256 x 256 tiles of 2048 x 8192 x 8192 took 152 us, not 137.
+    float ws[tile.TN], bias[tile.TN];
+#pragma unroll
+    for (int j = 0; j < tile.TN; ++j) {
+        const int n = min(c0 + j * 32, p.n - 1);
+        ws[j] = p.w_scale[n], bias[j] = p.bias ? p.bias[n] : 0.f;
+    }
 #pragma unroll
     for (int i = 0; i < tile.TM; ++i)
 #pragma unroll
         for (int g = 0; g < 16; ++g) {
-            const int t = m0 + i * 32 + 8 * (g / 4) + 4 * (lane >> 5) + g % 4;
-            if (t >= p.T) continue;
-            const float s = p.splits > 1 ? 0.f : p.s[t];
+            const int t = token(i, g);
+            const float s = scale[t - t0];
+            O* out = static_cast<O*>(p.out) + (int64_t)t * p.out_stride;
 #pragma unroll
             for (int j = 0; j < tile.TN; ++j) {
                 const int n = c0 + j * 32;
-                if (n >= p.n) continue;
-                if (p.splits > 1)
-                    p.part[((int64_t)blockIdx.y * p.T + t) * p.n + n] = tile.acc[i][j][g];
-                else
-                    put<O>(p, t, n, tile.acc[i][j][g], s);
+                const float v = (float)tile.acc[i][j][g] * s * ws[j];
+                if (t < p.T && n < p.n) out[n] = (O)(p.bias ? v + bias[j] : v);
             }
         }
 }
@@ -510,15 +564,16 @@ hipError_t slices(const LinearP& p, hipStream_t st) {
 }
 
 // ---- choice of tiles -----------------------------------------------------------------------
-// The tile shapes, by tokens and channels: workgroups that run at once on a compute unit, and the
-// time of a 64-byte slice of k with the unit full and with one workgroup on it, as measured on
-// 512 and 2048 tokens of k = 8192 (us).
+// The tile shapes, by tokens and channels: slices in the ring, workgroups that run at once on a
+// compute unit, and the time of a 128-byte slice of k with all of them running, as measured on 64 to
+// 2048 tokens of k = 8192 (us).  Where a workgroup has its compute unit to itself, a longer ring
+// hides the copies' way (2048 x 8192 x 2048 in 128 x 128 tiles: 47 us with two slices, 40 with four).
 struct TileShape {
-    int bm, bn, per_cu;
-    double full_us, lone_us;
+    int bm, bn, ring, per_cu;
+    double slice_us;
 };
-constexpr TileShape kTiles[] = {{64, 128, 3, 0.75, 0.45}, {128, 128, 2, 0.75, 0.53}, {256, 256, 1, 1.20, 1.20}};
-constexpr int kMaxSplits = 8;
+constexpr TileShape kTiles[] = {{64, 128, 4, 1, 0.48}, {64, 128, 3, 2, 0.67}, {128, 128, 4, 1, 0.62}, {128, 128, 2, 2, 1.17}, {256, 256, 2, 1, 1.95}};
+constexpr int kShapes = 5, kLargest = 4, kMaxSplits = 8;
 
 // Shape and splits of k with the least estimated time for T x n: rounds of workgroups x (slices +
 // start), and for a split the traffic of its sums.
@@ -529,22 +584,24 @@ struct TilePlan {
 TilePlan plan_tiles(int64_t T, int64_t k, int64_t n, int n_cu, size_t room) {
     const int64_t slices = ceil_div(k, kSlice);
     TilePlan best{0, 1, (int)slices, 0};
-    for (int i = 0; i < 3; ++i)
+    for (int i = 0; i < kShapes; ++i)
         for (int s = 1; s <= kMaxSplits; ++s) {
-            const int64_t per = round_up(ceil_div(slices, s), 4);
+            const TileShape& t = kTiles[i];
+            const int64_t per = round_up(ceil_div(slices, s), t.ring);
             if (s > 1 && ((uint64_t)s * T * n * 4 > room || ceil_div(slices, per) != s)) continue;
-            const int64_t wgs = ceil_div(T, kTiles[i].bm) * ceil_div(n, kTiles[i].bn) * s, slots = (int64_t)n_cu * kTiles[i].per_cu;
-            const double slice_us = wgs <= n_cu ? kTiles[i].lone_us : kTiles[i].full_us;
-            const double us = ceil_div(wgs, slots) * (per * slice_us + 3.0) + (s > 1 ? 4.0 + (double)s * T * n * 8 / 4e6 : 0.0);
+            const int64_t wgs = ceil_div(T, t.bm) * ceil_div(n, t.bn) * s, slots = (int64_t)n_cu * t.per_cu;
+            const double us = ceil_div(wgs, slots) * (per * t.slice_us + 3.0) + (s > 1 ? 4.0 + (double)s * T * n * 8 / 4e6 : 0.0);
             if (best.us == 0 || us < best.us) best = {i, s, (int)per, us};
         }
     return best;
 }
 
-template <typename O, int BM, int BN, int WM, int WN>
+template <typename O, int SHAPE, int WM, int WN>
 hipError_t tiles(const LinearP& p, hipStream_t st) {
-    const int tn = (int)ceil_div(p.n, BN);
-    hipLaunchKernelGGL((tile_kernel<O, BM, BN, WM, WN>), dim3((unsigned)(ceil_div(p.T, BM) * tn), p.splits), dim3(WM * WN * 64), 0, st, p, tn);
+    constexpr TileShape t = kTiles[SHAPE];
+    const int tn = (int)ceil_div(p.n, t.bn);
+    hipLaunchKernelGGL((tile_kernel<O, t.bm, t.bn, WM, WN, t.ring>), dim3((unsigned)(ceil_div(p.T, t.bm) * tn), p.splits),
+                       dim3(WM * WN * 64), 0, st, p, tn);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     hipLaunchKernelGGL(finish_kernel<O>, dim3((unsigned)ceil_div(p.n, 256), (unsigned)std::min(p.T, 65535)), dim3(256), 0, st, p);
@@ -555,9 +612,11 @@ template <typename O>
 hipError_t tiles_of(LinearP p, const TilePlan& plan, int32_t* part, hipStream_t st) {
     p.splits = plan.splits, p.slices = plan.slices, p.part = part;
     switch (plan.shape) {
-        case 0: return tiles<O, 64, 128, 2, 2>(p, st);
-        case 1: return tiles<O, 128, 128, 2, 2>(p, st);
-        default: return tiles<O, 256, 256, 2, 4>(p, st);
+        case 0: return tiles<O, 0, 2, 2>(p, st);
+        case 1: return tiles<O, 1, 2, 2>(p, st);
+        case 2: return tiles<O, 2, 2, 2>(p, st);
+        case 3: return tiles<O, 3, 2, 2>(p, st);
+        default: return tiles<O, kLargest, 2, 4>(p, st);
     }
 }
 
@@ -577,10 +636,10 @@ hipError_t product(const LinearP& p, int32_t* part, size_t room, int n_cu, hipSt
     if (first > 0 && first < columns) {
         const int64_t slices = ceil_div(p.k, kSlice), n1 = first * 256;
         const TilePlan rest = plan_tiles(p.T, p.k, p.n - n1, n_cu, room);
-        if (rounds * (round_up(slices, 4) * kTiles[2].full_us + 3.0) + rest.us + 2.0 < whole.us) {
+        if (rounds * (round_up(slices, 2) * kTiles[kLargest].slice_us + 3.0) + rest.us + 2.0 < whole.us) {
             LinearP a = p, b = p;
             a.n = (int)n1;
-            hipError_t e = tiles_of<O>(a, {2, 1, (int)round_up(slices, 4), 0}, part, st);
+            hipError_t e = tiles_of<O>(a, {kLargest, 1, (int)round_up(slices, 2), 0}, part, st);
             if (e != hipSuccess) return e;
             b.n = p.n - a.n;
             b.w += n1 * p.w_stride;
