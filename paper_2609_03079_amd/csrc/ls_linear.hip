@@ -484,7 +484,8 @@ hipError_t vec(const LinearP& p, const void* x, int64_t x_stride, int n_cu, hipS
 // slices of 16 NR rows of w and of the tokens to shared memory of its own, every W-th slice, without
 // barriers, one slice ahead, and the waves' sums are added at the end.  8 tokens x 5120 x 5120 6.4 us,
 // x 8192 x 28672 46 us (with both operands read straight into the matrix operands, 16 rows x 64 bytes
-// an instruction, 14.3 and 53.7); 37 tokens x 5120 x 5120 10.0 us (by tiles with k split 15.7).
+// an instruction, 14.3 and 53.7).  From 17 tokens on only while each workgroup has a compute unit at
+// once: 48 tokens x 5120 x 5120 10.2 us (in tiles with k split 14.4), but x 8192 x 10240 36.4 (22.8).
 template <typename O, int MT, int NR, int W>
 __global__ __launch_bounds__(W * 64) void slice_kernel(const LinearP p) {
     constexpr int RW = 16 * NR, RX = 16 * MT, kBytes = 256;
@@ -623,11 +624,9 @@ hipError_t tiles_of(LinearP p, const TilePlan& plan, int32_t* part, hipStream_t 
 template <typename O>
 hipError_t product(const LinearP& p, int32_t* part, size_t room, int n_cu, hipStream_t st) {
     if (vec_takes(p.T, p.k)) return vec<O, int8_t>(p, nullptr, 0, n_cu, st);
-    if (p.T <= 48) {
-        if (p.T <= 16) return slices<O, 1, 1, 4>(p, st);
-        if (p.T <= 32) return slices<O, 2, 2, 4>(p, st);
-        return slices<O, 3, 2, 4>(p, st);
-    }
+    if (p.T <= 16) return slices<O, 1, 1, 4>(p, st);
+    if (p.T <= 48 && ceil_div(p.n, 32) <= n_cu)
+        return p.T <= 32 ? slices<O, 2, 2, 4>(p, st) : slices<O, 3, 2, 4>(p, st);
     const TilePlan whole = plan_tiles(p.T, p.k, p.n, n_cu, room);
     // The largest tiles in whole rounds, the channels left over by the best shape for them, where
     // that is faster: 2048 x 8192 x 10240 is 1.25 rounds of 256 x 256 tiles.
