@@ -218,6 +218,14 @@ def test_linear_extreme_sums_and_tokens(ops):
     ops.ls_linear_i8(x[:0], w, ws, out[:0])
 
 
+# Tiles of every shape, k split and whole, channels in whole rounds of the largest tiles and a rest.
+@pytest.mark.parametrize("T,k,n", [(17, 272, 8300), (48, 656, 8201), (49, 5120, 515), (64, 1040, 65601), (128, 1168, 65601), (256, 528, 32900),
+                                   (300, 400, 4097), (2050, 1040, 8969), (2050, 400, 9001)])
+def test_linear_tiles(ops, T, k, n):
+    check_linear(ops, T, k, n, "bf16", "bf16", bias=True, pad=1, seed=n)
+    check_linear(ops, T, k, n, "i8", "f16", seed=k)
+
+
 @pytest.mark.parametrize("k", [2048, 2064, 4096, 4112, 8192, 8208, 16384, 16400, 20000])
 @pytest.mark.parametrize("x_type", ["f32", "f16", "bf16"])
 def test_linear_row_lengths(ops, k, x_type):
