@@ -99,7 +99,7 @@ ls_status ls_norm_residual(ls_ops* ctx, const ls_norm_args* a);
  * w: int8 [n, k] (nn.Linear layout, quantised by row).  k: a multiple of 16, at most 131056;
  * rows of x and w 16-byte aligned.  n >= 1; n_tokens 0 does nothing.
  * LS_E_CAPACITY if the quantised tokens (n_tokens (k + 4) bytes, each part rounded up to 256)
- * exceed the workspace. */
+ * exceed the workspace; one to four tokens of up to 16384 elements need none. */
 typedef struct {
     int32_t n_tokens, k, n;
     ls_dtype x_type, out_type;

@@ -14,10 +14,17 @@
 // same, and the values are read from shared memory (transposed on the way) in the order in which
 // the scores lie.
 //
-// Two shapes of workgroup (128 x 64 keys at a time is compute-bound, 32 rows are memory-bound):
-//  - wide: four waves of 32 rows share 64 keys in shared memory;
-//  - narrow (up to 32 rows): each wave takes every fourth 32 keys through its own share of
-//    shared memory, without barriers, and the waves' results are joined at the end.
+// Two shapes of workgroup:
+//  - wide: four waves of 32 rows share 64 keys in shared memory, the scores of the next 64 computed
+//    while the exponentials of these are: bound by the vector and matrix units together (64
+//    sequences, 64 query and 8 key heads of 128 bfloat16, 32768 prefix keys: 91 to 104 us, 68.7
+//    GFLOP, the matrix units busy for two fifths of it; 79 without any copies);
+//  - narrow (up to 32 rows): two waves, each taking every second 32 keys through its own share of
+//    shared memory, without barriers, the waves' results joined at the end: bound by each wave's
+//    chain of copy, products, exponentials and products (the same 64 sequences' own keys, 512 to
+//    1024 each: 44 us, 200 MB at 4.6 TB/s) and, for few keys, by its start: table, page, keys and
+//    the first products wait for each other, about 5.5 us.  Asking for keys and values two tiles
+//    ahead in place of one changed nothing there.
 // In both the next keys are copied straight to shared memory while the present ones are used.
 #include <algorithm>
 #include <type_traits>
@@ -735,7 +742,6 @@ bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes,
     // from the prefix more than running beside it gives (64 sequences behind 32768 keys 149 -> 184 us).
     plan->together = plan->pre_parts && plan->suf_parts && plan->pre_wide && !plan->suf_wide && c.head_dim <= 128 &&
                      n_pre * plan->pre_parts + 8 * plan->pre_tiles + n_suf * plan->suf_parts <= 2 * n_cu;
-    plan->bytes = (size_t)((plan->pre_parts + plan->suf_parts) * part_bytes);
     return true;
 }
 

@@ -29,7 +29,6 @@ struct AttendPlan {
     int suf_chunk, suf_parts, suf_tiles;
     bool pre_wide, suf_wide;              // 128-row tiles instead of 32-row tiles
     bool together;                        // a wide prefix and narrow sequences in one launch
-    size_t bytes;                         // workspace
 };
 // False where no split fits the workspace.
 bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan);
