@@ -258,7 +258,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void tile_kernel(const L
     constexpr int kA = BM * kSlice, kB = BN * kSlice;
     __shared__ __attribute__((aligned(16))) int8_t a0[kA], a1[kA], a2[S > 2 ? kA : 16], a3[S > 3 ? kA : 16];
     __shared__ __attribute__((aligned(16))) int8_t b0[kB], b1[kB], b2[S > 2 ? kB : 16], b3[S > 3 ? kB : 16];
-    __shared__ float scale[BM];  // of the tokens
+    __shared__ __attribute__((aligned(16))) float scale[BM];  // of the tokens
     const int t0 = (blockIdx.x / tiles_n) * BM, n0 = (blockIdx.x % tiles_n) * BN;
     const int first = blockIdx.y * p.slices * kSlice, last = min(p.k, first + p.slices * kSlice);
     Tile<BM, BN, WM, WN> tile;
@@ -317,17 +317,18 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void tile_kernel(const L
     }
     __builtin_amdgcn_s_waitcnt(0x0070);  // no copy into shared memory outlives the workgroup
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int m0 = t0 + (wave / WN) * (BM / WM), c0 = n0 + (wave % WN) * (BN / WN) + (lane & 31);
-    auto token = [&](int i, int g) { return m0 + i * 32 + 8 * (g / 4) + 4 * (lane >> 5) + g % 4; };
+    // Element g of a lane's sums belongs to row 8 (g / 4) + g % 4 of its rows, which begin at r0 of the tile.
+    const int r0 = (wave / WN) * (BM / WM) + 4 * (lane >> 5), c0 = n0 + (wave % WN) * (BN / WN) + (lane & 31);
     if (p.splits > 1) {
+        int32_t* to = p.part + ((int64_t)blockIdx.y * p.T + t0 + r0) * p.n + c0;
 #pragma unroll
         for (int i = 0; i < tile.TM; ++i)
 #pragma unroll
             for (int g = 0; g < 16; ++g)
 #pragma unroll
                 for (int j = 0; j < tile.TN; ++j) {
-                    const int t = token(i, g), n = c0 + j * 32;
-                    if (t < p.T && n < p.n) p.part[((int64_t)blockIdx.y * p.T + t) * p.n + n] = tile.acc[i][j][g];
+                    const int row = i * 32 + 8 * (g / 4) + g % 4;
+                    if (t0 + r0 + row < p.T && c0 + j * 32 < p.n) to[(int64_t)row * p.n + j * 32] = tile.acc[i][j][g];
                 }
         return;
     }
@@ -339,20 +340,28 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void tile_kernel(const L
         const int n = min(c0 + j * 32, p.n - 1);
         ws[j] = p.w_scale[n], bias[j] = p.bias ? p.bias[n] : 0.f;
     }
+    O* to = static_cast<O*>(p.out) + (int64_t)(t0 + r0) * p.out_stride + c0;
+    auto write = [&](auto whole) {  // whole: nothing of the tile lies outside the product
 #pragma unroll
-    for (int i = 0; i < tile.TM; ++i)
+        for (int i = 0; i < tile.TM; ++i)
 #pragma unroll
-        for (int g = 0; g < 16; ++g) {
-            const int t = token(i, g);
-            const float s = scale[t - t0];
-            O* out = static_cast<O*>(p.out) + (int64_t)t * p.out_stride;
+            for (int g = 0; g < 16; g += 4) {
+                const f32x4 s = *reinterpret_cast<const f32x4*>(scale + r0 + i * 32 + 2 * g);
 #pragma unroll
-            for (int j = 0; j < tile.TN; ++j) {
-                const int n = c0 + j * 32;
-                const float v = (float)tile.acc[i][j][g] * s * ws[j];
-                if (t < p.T && n < p.n) out[n] = (O)(p.bias ? v + bias[j] : v);
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int j = 0; j < tile.TN; ++j) {
+                        const int row = i * 32 + 2 * g + e;
+                        const float v = (float)tile.acc[i][j][g + e] * s[e] * ws[j];
+                        if (whole.value || (t0 + r0 + row < p.T && c0 + j * 32 < p.n))
+                            to[row * p.out_stride + j * 32] = (O)(p.bias ? v + bias[j] : v);
+                    }
             }
-        }
+    };
+    if (t0 + BM <= p.T && n0 + BN <= p.n)
+        write(std::true_type{});
+    else
+        write(std::false_type{});
 }
 
 template <typename O>
