@@ -564,11 +564,10 @@ __device__ inline float wave_max(float v) {
 // parts are all asked for at once, parts that turn out never to have been written among them (their
 // weight is zero, and they are not looked at).
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void join_kernel(const AttendP p) {
-    constexpr int L = DP / 4, GR = 64 / L, U = 4;
+__global__ __launch_bounds__(64) void join_kernel(const AttendP p) {
+    constexpr int L = DP / 4, GR = 64 / L, U = 16 / GR;  // 16 parts at a time
     const int lane = threadIdx.x & 63;
-    const int rows = p.S * p.n_q * p.H, r = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (r >= rows) return;
+    const int r = blockIdx.x;
     const int token = p.by_H.of(r), seq = p.by_n_q.of(token);
     const float* ml = p.ml + (int64_t)r * p.parts * 2;
     const float* part = p.part + (int64_t)r * p.parts * p.D;
@@ -679,7 +678,7 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_attend_args& a, const Atte
         if (e == hipSuccess) e = go(suf_role, 0, suf);
     }
     if (e != hipSuccess || p.direct) return e;
-    hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)rows), dim3(64), 0, st, p);
     return hipGetLastError();
 }
 
