@@ -517,8 +517,8 @@ enum Roles { NARROW, WIDE_ROWS, BOTH };
 
 template <typename T, int DP, Roles ROLES, bool MULTI>
 __global__ __launch_bounds__((Shape<T, DP, ROLES != NARROW>::NW * 64), (ROLES != NARROW && DP <= 128 && (ROLES == BOTH || !MULTI) ? 2 : 1)) void attend_kernel(const AttendP p) {
-    constexpr int kBuf = Shape<T, DP, ROLES != NARROW>::kBuf;
-    static_assert(ROLES != BOTH || kBuf == Shape<T, DP, false>::kBuf, "one size serves both shapes");
+    constexpr int kBuf = ROLES == WIDE_ROWS ? Shape<T, DP, true>::kBuf : Shape<T, DP, false>::kBuf;
+    static_assert(Shape<T, DP, false>::kBuf >= Shape<T, DP, true>::kBuf, "room for either shape");
     __shared__ __attribute__((aligned(16))) T k0[kBuf], k1[kBuf], v0[kBuf], v1[kBuf];
     __shared__ float wave_ml[Shape<T, DP, false>::NW][2][32], row_sum[32];
     int b = blockIdx.x;
@@ -559,19 +559,19 @@ __device__ inline float wave_max(float v) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// Joins the parts of a row: a wave per row, DP / 4 lanes across its elements and the other
-// lanes on other parts.  Bound by latency: the sequence's length, the maxima and sums and the first
-// parts are all asked for at once, parts that turn out never to have been written among them (their
-// weight is zero, and they are not looked at).
+// Joins the parts of a row: a wave for 64 of its elements, 16 lanes across them and the other lanes on
+// other parts (a wave for a whole row took 9.2 us, not 4.0, for 48 rows of 65 parts of 256 elements).
+// Bound by latency: the sequence's length, the maxima and sums and the first parts are all asked for
+// at once, parts that turn out never to have been written among them (their weight is zero, and they
+// are not looked at).
 template <typename T, int DP>
 __global__ __launch_bounds__(64) void join_kernel(const AttendP p) {
-    constexpr int L = DP / 4, GR = 64 / L, U = 16 / GR;  // 16 parts at a time
-    const int lane = threadIdx.x & 63;
-    const int r = blockIdx.x;
+    constexpr int L = 16, GR = 64 / L, U = 16 / GR;  // 16 parts at a time
+    const int lane = threadIdx.x & 63, r = blockIdx.x;
     const int token = p.by_H.of(r), seq = p.by_n_q.of(token);
     const float* ml = p.ml + (int64_t)r * p.parts * 2;
     const float* part = p.part + (int64_t)r * p.parts * p.D;
-    const int d = (lane % L) * 4, g = lane / L, dd = min(d, p.D - 4);
+    const int d = blockIdx.y * 64 + (lane % L) * 4, g = lane / L, dd = min(d, p.D - 4);
     float m[2], l[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -659,7 +659,7 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_attend_args& a, const Atte
                 hipLaunchKernelGGL((attend_kernel<T, DP, WIDE_ROWS, true>), grid, wide_wg, 0, st, p);
             else
                 hipLaunchKernelGGL((attend_kernel<T, DP, WIDE_ROWS, false>), grid, wide_wg, 0, st, p);
-        } else if constexpr (DP <= 128) {
+        } else {
             if (multi)
                 hipLaunchKernelGGL((attend_kernel<T, DP, BOTH, true>), grid, wide_wg, 0, st, p);
             else
@@ -678,7 +678,7 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_attend_args& a, const Atte
         if (e == hipSuccess) e = go(suf_role, 0, suf);
     }
     if (e != hipSuccess || p.direct) return e;
-    hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)rows), dim3(64), 0, st, p);
+    hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)rows, (unsigned)ceil_div(p.D, 64)), dim3(64), 0, st, p);
     return hipGetLastError();
 }
 
@@ -739,8 +739,8 @@ bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes,
     // A wide prefix and narrow sequences in one launch where all their workgroups run at once (5 x 4 tokens
     // behind 333 keys 20.4 -> 16.3 us).  Larger ones apart: the sequences' stream through the caches takes
     // from the prefix more than running beside it gives (64 sequences behind 32768 keys 149 -> 184 us).
-    plan->together = plan->pre_parts && plan->suf_parts && plan->pre_wide && !plan->suf_wide && c.head_dim <= 128 &&
-                     n_pre * plan->pre_parts + 8 * plan->pre_tiles + n_suf * plan->suf_parts <= 2 * n_cu;
+    plan->together = plan->pre_parts && plan->suf_parts && plan->pre_wide && !plan->suf_wide &&
+                     n_pre * plan->pre_parts + 8 * plan->pre_tiles + n_suf * plan->suf_parts <= wide_cu * n_cu;
     return true;
 }
 

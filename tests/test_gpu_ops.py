@@ -510,6 +510,20 @@ def test_attend_strides(ops):
     check_attend(ops, lens=[50, 90], prefix=20, stride_pad=3, layout="token")
 
 
+@pytest.mark.parametrize("dim", [40, 64, 80, 128, 136, 192, 256])
+@pytest.mark.parametrize("n_q", [1, 3, 4])
+def test_attend_wide_prefix_beside_narrow_sequences(ops, dim, n_q):
+    # more than 32 rows share the prefix, at most 32 a sequence
+    for dt in BOTH:
+        check_attend(ops, lens=[0, 1, 33, 300, -1, 64, 517], prefix=333, heads=8, kv=1, n_q=n_q, dim=dim, dt=dt, page=16, seed=dim + n_q)
+
+
+@pytest.mark.parametrize("dim", [64, 80, 136, 256])
+def test_attend_many_parts(ops, dim):
+    check_attend(ops, lens=[7000, 20], prefix=9000, heads=4, kv=1, dim=dim, page=64, seed=dim)
+    check_attend(ops, lens=[2000] * 5, prefix=9000, heads=8, kv=1, n_q=2, dim=dim, page=64, seed=dim)
+
+
 @pytest.mark.parametrize("lens,prefix,heads,kv,n_q", [([3000] * 2, 9000, 8, 8, 1), ([200 * s for s in range(20)], 5000, 32, 4, 2)])
 def test_attend_longer(ops, lens, prefix, heads, kv, n_q):
     check_attend(ops, lens=lens, prefix=prefix, heads=heads, kv=kv, n_q=n_q, dim=128, dt=torch.bfloat16, page=64, poison=False)
