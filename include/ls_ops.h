@@ -97,7 +97,8 @@ ls_status ls_norm_residual(ls_ops* ctx, const ls_norm_args* a);
  * The sums are exact in 32-bit integers; scales and bias (fp32 [n] or NULL) are applied in fp32
  * and rounded once to out_type (LS_F32, LS_F16 or LS_BF16).
  * w: int8 [n, k] (nn.Linear layout, quantised by row).  k: a multiple of 16, at most 131056;
- * rows of x and w 16-byte aligned.  n >= 1; n_tokens 0 does nothing.
+ * rows of x and w 16-byte aligned.  n >= 1; n_tokens 0 does nothing; n_tokens < 2^23 where x is
+ * quantised on the way.
  * LS_E_CAPACITY if the quantised tokens (n_tokens (k + 4) bytes, each part rounded up to 256)
  * exceed the workspace; one to four tokens of up to 16384 elements need none. */
 typedef struct {

@@ -715,7 +715,7 @@ bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes,
         for (int64_t chunk = 128;; chunk = std::min(most, chunk + std::max<int64_t>(128, chunk / 8 / 128 * 128))) {
             const int64_t pp = ceil_div(pre_keys, chunk), sp = ceil_div(suf_keys, chunk), items = n_pre * pp + n_suf * sp;
             const bool fits = pp <= kMaxParts / 2 && sp <= kMaxParts / 2 && std::max(pp, sp) * part_bytes <= (int64_t)ws_bytes / 2 &&
-                              (n_pre + 8) * (pp + 8) + n_suf * sp < (int64_t)1 << 30;
+                              (n_pre + 8) * (pp + 8) + n_suf * sp < (int64_t)1 << 24;  // 2^32 threads of a launch
             if (fits) {
                 const double t = item_us(wide, chunk) * ceil_div(items, slots) + (pp + sp) * part_us;
                 if (!best || t < least) best = chunk, least = t;

@@ -164,6 +164,7 @@ ls_status ls_linear_i8(ls_ops* c, const ls_linear_i8_args* a) {
                "a pointer is not aligned to its type");
     // one workgroup per 16 channels and 128 tokens at the finest
     LS_REQUIRE(ls::ceil_div(a->n_tokens, 64) * ls::ceil_div(a->n, 16) < (int64_t)1 << 31, "n_tokens and n are too large for one call");
+    LS_REQUIRE(a->x_type == LS_I8 || a->n_tokens < 1 << 23, "n_tokens must be below 2^23 where x is quantised on the way");
     const size_t need = ls::linear_workspace(*a);
     if (need > c->ws_bytes)
         return fail(c, LS_E_CAPACITY, "the quantised tokens take %zu bytes, the workspace has %zu", need, c->ws_bytes);

@@ -274,20 +274,47 @@ hipError_t append_type(const ls_kv_cache& c, const ls_append_args& a, hipStream_
 
 }  // namespace
 
+// A launch holds fewer than 2^32 threads along x: calls with a workgroup of up to 1024 for each of
+// more tokens than this are cut.
+constexpr int kTokensPerLaunch = 1 << 21;
+
 hipError_t launch_norm(const ls_norm_args& a, hipStream_t st) {
-    switch (a.dtype) {
-        case LS_F32: return norm_type<float>(a, st);
-        case LS_F16: return norm_type<_Float16>(a, st);
-        default: return norm_type<__bf16>(a, st);
+    for (int64_t t = 0; t < a.n_tokens; t += kTokensPerLaunch) {
+        ls_norm_args b = a;
+        const int64_t es = (int64_t)type_size(a.dtype);
+        auto skip = [&](const void* p, int64_t stride) { return p ? static_cast<const char*>(p) + t * stride * es : nullptr; };
+        b.n_tokens = (int32_t)std::min<int64_t>(kTokensPerLaunch, a.n_tokens - t);
+        b.x += t * a.x_stride;
+        if (b.x_out) b.x_out += t * a.x_out_stride;
+        b.y = skip(a.y, a.y_stride);
+        b.gate = skip(a.gate, a.gate_stride);
+        b.h = const_cast<char*>(skip(a.h, a.h_stride));
+        const hipError_t e = a.dtype == LS_F32   ? norm_type<float>(b, st)
+                             : a.dtype == LS_F16 ? norm_type<_Float16>(b, st)
+                                                 : norm_type<__bf16>(b, st);
+        if (e != hipSuccess) return e;
     }
+    return hipSuccess;
 }
 
 hipError_t launch_append(const ls_kv_cache& c, const ls_append_args& a, hipStream_t st) {
-    switch (c.dtype) {
-        case LS_F32: return append_type<float>(c, a, st);
-        case LS_F16: return append_type<_Float16>(c, a, st);
-        default: return append_type<__bf16>(c, a, st);
+    for (int64_t t = 0; t < a.n_tokens; t += kTokensPerLaunch) {
+        ls_append_args b = a;
+        const int64_t es = (int64_t)type_size(c.dtype);
+        auto skip = [&](const void* p, int64_t stride) { return p ? static_cast<const char*>(p) + t * stride * es : nullptr; };
+        b.n_tokens = (int32_t)std::min<int64_t>(kTokensPerLaunch, a.n_tokens - t);
+        b.k = skip(a.k, a.k_token_stride);
+        b.v = skip(a.v, a.v_token_stride);
+        b.q = skip(a.q, a.q_token_stride);
+        b.q_out = const_cast<char*>(skip(a.q_out, a.q_out_token_stride));
+        if (b.positions) b.positions += t;
+        b.slots += t;
+        const hipError_t e = c.dtype == LS_F32   ? append_type<float>(c, b, st)
+                             : c.dtype == LS_F16 ? append_type<_Float16>(c, b, st)
+                                                 : append_type<__bf16>(c, b, st);
+        if (e != hipSuccess) return e;
     }
+    return hipSuccess;
 }
 
 }  // namespace ls

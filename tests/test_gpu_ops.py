@@ -706,3 +706,38 @@ def test_context_refusals():
     o.close()
     o.close()  # a second time does nothing
     refused(lambda: o.ls_norm_residual(torch.zeros((1, 8), device=DEV), x_out=torch.zeros((1, 8), device=DEV)))
+
+
+# ---- more tokens than one launch holds ---------------------------------------------------------------
+def test_norm_of_millions_of_tokens(ops):
+    check_norm(ops, 2 ** 21 + 3, 9, torch.float16, gate="token", pad=1)
+    check_norm(ops, 2 ** 21 + 3, 8, torch.bfloat16, in_place=True)
+
+
+def test_append_of_millions_of_tokens(ops):
+    T, dim = 2 ** 21 + 3, 8
+    kc, vc = (torch.zeros((T // 4096 + 1, 1, 4096, dim), dtype=torch.float16, device=DEV) for _ in range(2))
+    k, v, q = (rand((T, 1, dim), s, torch.float16) for s in (1, 2, 3))
+    q_out, cs = torch.empty_like(q), table(5, dim)
+    at = torch.arange(T, dtype=torch.int32, device=DEV)
+    slots = T - 1 - at
+    slots[T - 2] = -1   # padding, in the second launch
+    positions = at % 5
+    ops.ls_kv_append(kc, vc, k, v, positions, slots, cs, q=q, q_out=q_out, style=lsffn.LS_ROPE_HALF)
+    # two products and a sum in fp32, then one rounding
+    c, s = cs[positions.long()].double().split(dim // 2, -1)
+    for x, got in ((k, kc.view(-1, dim)[:T].flip(0)), (q, q_out[:, 0])):
+        a, b = x[:, 0].double().split(dim // 2, -1)
+        ref = torch.cat([a * c - b * s, b * c + a * s], -1)
+        mag = torch.cat([(a * c).abs() + (b * s).abs(), (b * c).abs() + (a * s).abs()], -1)
+        if x is k:
+            ref[T - 2] = 0
+        within(got, ref, 3 * E * mag + U[torch.float16] * (ref.abs() + 3 * E * mag) + TINY[torch.float16])
+    kept = vc.view(-1, dim)[:T].flip(0)
+    assert torch.equal(kept[:T - 2], v[:T - 2, 0]) and torch.equal(kept[T - 1], v[T - 1, 0]) and not kept[T - 2].any()
+
+
+def test_linear_refuses_more_tokens_than_are_quantised_at_once(ops):
+    x = torch.zeros((1, 16), dtype=torch.float16, device=DEV).expand(2 ** 23, 16)
+    w, s = torch.zeros((1, 16), dtype=torch.int8, device=DEV), torch.ones(1, device=DEV)
+    refused(lambda: ops.ls_linear_i8(x, w, s, torch.empty((2 ** 23, 1), device=DEV)), text="2^23")
