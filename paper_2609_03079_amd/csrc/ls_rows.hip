@@ -47,7 +47,7 @@ __device__ inline float row_sum(float v, float* part) {
 // row.  All loads are issued before the first sum, so a single token costs one memory round trip
 // and two sums.  Rows of up to 8192 elements have a thread for every vector: 8191 x 8192 bfloat16
 // with a gate for each token 171 us, with four vectors a thread 230; outputs larger than the caches
-// are stored past them: 163 us (939 MB at 5.7 TB/s; a copy of 1 GiB moves 5.2).
+// are stored past them: 163 to 173 us (939 MB at 5.4 to 5.7 TB/s; a copy of 1 GiB moves 5.2).
 template <typename T, int V, int C, int NT>
 __global__ __launch_bounds__(NT) void norm_kernel(const ls_norm_args p, bool past_caches) {
     __shared__ float part[2][NT / 64];
@@ -158,7 +158,7 @@ struct AppendP {
 // A thread moves one vector of one head at a time: V pairs that turn (or V / 2 of neighbours), or
 // V elements that are copied.  The vectors of a token's query, key and value heads follow each
 // other; blockIdx.x is the token, blockIdx.y 256 of its vectors.  8192 tokens of 64 query and 8 key
-// heads of 128 bfloat16: 58 us (340 MB at 5.8 TB/s), 73 with the stores kept in the caches, 78 with
+// heads of 128 bfloat16: 58 to 65 us (340 MB at 5.2 to 5.8 TB/s), 73 with the stores kept in the caches, 78 with
 // one workgroup for all of a token's vectors.
 template <typename T, int V, bool PAIR>
 __global__ __launch_bounds__(256) void append_kernel(const AppendP p, bool past_caches) {
