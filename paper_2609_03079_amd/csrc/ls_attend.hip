@@ -4,8 +4,10 @@
 //
 // The prefix's keys serve the rows of every sequence at once (n_seqs n_q G rows per key/value head,
 // G query heads sharing it), a sequence's own keys its n_q G rows.  Both are cut along the keys
-// into parts; each part keeps the running maximum m, sum l and sum of weighted values of its rows
-// (one pass over the keys), and a second kernel joins the parts of a row.
+// into parts; each part keeps the running maximum, sum l and sum of weighted values of its rows
+// (one pass over the keys), and a second kernel joins the parts of a row.  What is kept of the
+// maximum is m = max scale log2(e) q k, rounded: the number that the weights are taken relative to, so
+// that a maximum that stays rescales by exactly one, whatever the rows beside it do.
 //
 // The products run transposed, S^T = K Q^T and O^T = V^T P^T, on the 32 x 32 x 16 matrix
 // instructions: a lane then holds one query row's scores, 16 of each 32 keys, so the softmax
@@ -313,9 +315,9 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
             largest(s);
         }
         const float top = fmaxf(s.top, other_half(s.top));
-        const float next = fmaxf(m, top), base = next == -INFINITY ? 0.f : next * p.c;
+        const float next = fmaxf(m, top * p.c), base = next == -INFINITY ? 0.f : next;
         if (__any(next > m)) {
-            const float scale = __builtin_amdgcn_exp2f(fmaf(m, p.c, -base));  // m = -inf: 0
+            const float scale = __builtin_amdgcn_exp2f(m - base);  // m = -inf: 0
             l *= scale;
 #pragma unroll
             for (auto& x : o) x *= scale;
@@ -470,11 +472,11 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     float top = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) top = fmaxf(top, wave_ml[w][0][n]);
-    const float base = top == -INFINITY ? 0.f : top * p.c;
+    const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
         const float wl = wave_ml[w][1][n];
-        if (wl != 0.f) sum += wl * __builtin_amdgcn_exp2f(fmaf(wave_ml[w][0][n], p.c, -base));
+        if (wl != 0.f) sum += wl * __builtin_amdgcn_exp2f(wave_ml[w][0][n] - base);
     }
     // [wave][row][DP], 16-byte chunks permuted by the row: half of each row in the keys' array, half in the values'
     static_assert(WIDE || Sh::kBuf * sizeof(T) >= NW * 32 * DP / 2 * 4, "room for the waves' sums");
@@ -483,7 +485,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         return reinterpret_cast<f32x4*>(c < half ? k0 : v0) + (w * 32 + r) * half + c % half;
     };
     if (row_ok) {
-        const float scale = __builtin_amdgcn_exp2f(fmaf(m, p.c, -base));
+        const float scale = __builtin_amdgcn_exp2f(m - base);
 #pragma unroll
         for (int t = 0; t < ND; ++t)
 #pragma unroll
@@ -596,9 +598,9 @@ __global__ __launch_bounds__(64) void join_kernel(const AttendP p) {
         m[i] = in ? m[i] : -INFINITY;
         l[i] = in ? l[i] : 0.f;
     }
-    const float top = wave_max(fmaxf(m[0], m[1])), base = top == -INFINITY ? 0.f : top * p.c;
+    const float top = wave_max(fmaxf(m[0], m[1])), base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) m[i] = l[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(fmaf(m[i], p.c, -base));  // now its weight
+    for (int i = 0; i < 2; ++i) m[i] = l[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(m[i] - base);  // now its weight
     const float sum = wave_sum_dpp(l[0] * m[0] + l[1] * m[1]);
     f32x4 acc{};
     for (int j0 = 0; j0 < last; j0 += U * GR) {
