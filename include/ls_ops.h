@@ -177,7 +177,8 @@ ls_status ls_kv_append(ls_ops* ctx, const ls_kv_cache* cache, const ls_append_ar
  * for LS_F32).  head_dim: a multiple of 8, at most 256; pointers and strides of q, out, k and v
  * 16-byte aligned.  1 <= n_q <= 16; prefix_len, max_len < 2^22; scale > 0.
  * Scores, the softmax's maxima and sums and the outputs are fp32; probabilities are rounded to
- * the cache's type for the product with the values.
+ * the cache's type for the product with the values (to a step of 2^-31 of the row's largest, at
+ * the finest, in f16).
  * LS_E_CAPACITY if the workspace cannot hold the parts of one split
  * (n_seqs n_q n_heads 2 (head_dim + 2) floats). */
 typedef struct {

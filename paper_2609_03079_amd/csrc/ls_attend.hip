@@ -6,8 +6,8 @@
 // G query heads sharing it), a sequence's own keys its n_q G rows.  Both are cut along the keys
 // into parts; each part keeps the running maximum, sum l and sum of weighted values of its rows
 // (one pass over the keys), and a second kernel joins the parts of a row.  What is kept of the
-// maximum is m = max scale log2(e) q k, rounded: the number that the weights are taken relative to, so
-// that a maximum that stays rescales by exactly one, whatever the rows beside it do.
+// maximum is m = max scale log2(e) q k - kLift, rounded: the number that the weights are taken relative
+// to, so that a maximum that stays rescales by exactly one, whatever the rows beside it do.
 //
 // The products run transposed, S^T = K Q^T and O^T = V^T P^T, on the 32 x 32 x 16 matrix
 // instructions: a lane then holds one query row's scores, 16 of each 32 keys, so the softmax
@@ -105,6 +105,12 @@ __device__ inline int swz(int row) {
 
 template <typename T, int DP, bool WIDE>
 struct Shape {
+    // The largest weight is 2^kLift.  Weights enter the second product in 16 bits (in 32 the product
+    // would run at a sixteenth of the rate), and with a largest of one float16 would drop those below 2^-25,
+    // which the sum counts: 30000 keys that far below one that dominates are a thousandth of the
+    // result.  With 2^7 those below 2^-32 are dropped, a part's 65536 at most a 2^-16th; what is left
+    // of the type's range is for a maximum that was rounded (by 2^8 at most while |m| < 2^28).
+    static constexpr float kLift = std::is_same_v<T, _Float16> ? 7.f : 0.f;
     static constexpr int NW = WIDE ? 4 : 2;                     // waves
     static constexpr int KT = WIDE && DP < 256 ? 64 : 32;       // keys at a time
     static constexpr int CPR = DP / 8;                          // chunks per row
@@ -315,7 +321,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
             largest(s);
         }
         const float top = fmaxf(s.top, other_half(s.top));
-        const float next = fmaxf(m, top * p.c), base = next == -INFINITY ? 0.f : next;
+        const float next = fmaxf(m, top * p.c - Sh::kLift), base = next == -INFINITY ? 0.f : next;
         if (__any(next > m)) {
             const float scale = __builtin_amdgcn_exp2f(m - base);  // m = -inf: 0
             l *= scale;

@@ -44,3 +44,37 @@ def test_a_row_does_not_depend_on_the_rows_of_its_wave(ops, dt, dim, shared):
     mean, size = (f(vc.double()).transpose(1, 2).flatten(0, 1).mean(0)[:, None] for f in (lambda v: v, torch.abs))
     assert torch.all((outs[1][:, :, :4].double() - mean).abs() <= u * mean.abs() + 2 * u * size)
     assert math.isfinite(float(outs[1].double().sum()))
+
+
+@pytest.mark.parametrize("dt", BOTH, ids=["f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 80, 256])
+@pytest.mark.parametrize("form", ["own", "prefix", "tokens"])
+@pytest.mark.parametrize("gap", [14.0, 17.5, 19.0])
+def test_many_keys_far_below_the_largest_count(ops, dt, dim, form, gap):
+    """One key's score is `gap` above all others' and its value is zero: the result is what the others add."""
+    S, G, page, n_q, n = 12, 4, 16, 3 if form == "tokens" else 1, 640
+    kc, vc = (torch.zeros((n // page, 1, page, dim), dtype=dt, device=DEV) for _ in range(2))
+    kc[0, 0, 5, 0] = 1
+    vc.uniform_(500, 1500, generator=torch.Generator(DEV).manual_seed(int(gap)))
+    vc[0, 0, 5] = 0
+    pages = torch.arange(n // page, dtype=torch.int32, device=DEV)
+    q = torch.zeros((S * n_q, G, dim), dtype=dt, device=DEV)
+    q[..., 0] = gap
+    out = torch.empty_like(q)
+    if form == "prefix":
+        args = dict(max_len=0, prefix_pages=pages, prefix_len=n)
+    else:
+        args = dict(max_len=n)
+    lens = torch.full((S,), 0 if form == "prefix" else n, dtype=torch.int32, device=DEV)
+    ops.ls_attend(q, kc, vc, None if form == "prefix" else pages.repeat(S, 1), lens, out, n_q=n_q, scale=1.0, **args)
+    v = vc.double().view(n, dim)
+    u = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dt]
+    # a weight is rounded to u of itself or half a step of 2^-31 of the largest, its exponent (below 64, rounded twice)
+    # to 2^-18 and the exponential to a few of fp32's; so is the sum; the result is rounded once, to u or half a subnormal step
+    for i in range(n_q):
+        seen = v[:n - n_q + 1 + i]
+        w = math.exp(-gap)
+        total = 1 + (len(seen) - 1) * w
+        ref, size = w * seen.sum(0) / total, seen.sum(0) / total
+        tol = (2 * u + 2.0 ** -17) * ref + (2.0 ** -32 * size if dt == torch.float16 else 0) + 2.0 ** -25
+        assert torch.all((out[i::n_q].double() - ref).abs() <= tol)
