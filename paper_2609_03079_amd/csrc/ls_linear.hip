@@ -44,6 +44,38 @@ __device__ inline void put(const LinearP& p, int t, int n, int acc, float s) {
     static_cast<O*>(p.out)[(int64_t)t * p.out_stride + n] = (O)v;
 }
 
+// Channels n0 .. n0 + n - 1 of the product, and tokens t0 .. t0 + T - 1.
+template <typename O>
+LinearP channels(LinearP p, int64_t n0, int64_t n) {
+    p.n = (int)n;
+    p.w += n0 * p.w_stride;
+    p.w_scale += n0;
+    if (p.bias) p.bias += n0;
+    p.out = static_cast<O*>(p.out) + n0;
+    return p;
+}
+template <typename O>
+LinearP tokens(LinearP p, int64_t t0, int64_t T) {
+    p.T = (int)T;
+    p.q += t0 * p.q_stride;
+    p.s += t0;
+    p.out = static_cast<O*>(p.out) + t0 * p.out_stride;
+    return p;
+}
+
+// A launch holds fewer than 2^32 threads along x, and the kernels count channels and tokens in 31 bits
+// with room for a grid's stride: larger products are cut into pieces of at most this (2^23 of the smallest tiles).
+constexpr int64_t kChannelsPerLaunch = 1 << 20, kTokensPerLaunch = 1 << 16;
+
+template <typename O, typename F>
+hipError_t by_channels(const LinearP& p, F&& launch) {
+    for (int64_t n = 0; n < p.n; n += kChannelsPerLaunch) {
+        const hipError_t e = launch(channels<O>(p, n, std::min(kChannelsPerLaunch, p.n - n)));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // ---- quantisation --------------------------------------------------------------------------
 // |x| as ordered integers: an infinity is 0x7f800000, a NaN above it.
 __device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
@@ -647,16 +679,9 @@ hipError_t product(const LinearP& p, int32_t* part, size_t room, int n_cu, hipSt
         const int64_t slices = ceil_div(p.k, kSlice), n1 = first * 256;
         const TilePlan rest = plan_tiles(p.T, p.k, p.n - n1, n_cu, room);
         if (rounds * (round_up(slices, 2) * kTiles[kLargest].slice_us + 3.0) + rest.us + 2.0 < whole.us) {
-            LinearP a = p, b = p;
-            a.n = (int)n1;
-            hipError_t e = tiles_of<O>(a, {kLargest, 1, (int)round_up(slices, 2), 0}, part, st);
+            hipError_t e = tiles_of<O>(channels<O>(p, 0, n1), {kLargest, 1, (int)round_up(slices, 2), 0}, part, st);
             if (e != hipSuccess) return e;
-            b.n = p.n - a.n;
-            b.w += n1 * p.w_stride;
-            b.w_scale += n1;
-            if (b.bias) b.bias += n1;
-            b.out = static_cast<O*>(p.out) + n1;
-            return tiles_of<O>(b, rest, part, st);
+            return tiles_of<O>(channels<O>(p, n1, p.n - n1), rest, part, st);
         }
     }
     return tiles_of<O>(p, whole, part, st);
@@ -667,9 +692,11 @@ hipError_t linear(const ls_linear_i8_args& a, LinearP p, uint8_t* ws, size_t ws_
     const size_t used = linear_workspace(a);
     if (a.x_type != LS_I8) {
         if (vec_takes(p.T, p.k)) {
-            if (a.x_type == LS_F32) return vec<O, float>(p, a.x, a.x_stride, n_cu, st);
-            if (a.x_type == LS_F16) return vec<O, _Float16>(p, a.x, a.x_stride, n_cu, st);
-            return vec<O, __bf16>(p, a.x, a.x_stride, n_cu, st);
+            return by_channels<O>(p, [&](const LinearP& b) {
+                return a.x_type == LS_F32   ? vec<O, float>(b, a.x, a.x_stride, n_cu, st)
+                       : a.x_type == LS_F16 ? vec<O, _Float16>(b, a.x, a.x_stride, n_cu, st)
+                                            : vec<O, __bf16>(b, a.x, a.x_stride, n_cu, st);
+            });
         }
         int8_t* q = reinterpret_cast<int8_t*>(ws);
         float* s = reinterpret_cast<float*>(ws + round_up((size_t)a.n_tokens * a.k, 256));
@@ -679,7 +706,13 @@ hipError_t linear(const ls_linear_i8_args& a, LinearP p, uint8_t* ws, size_t ws_
         if (e != hipSuccess) return e;
         p.q = q, p.q_stride = a.k, p.s = s;
     }
-    return product<O>(p, reinterpret_cast<int32_t*>(ws + used), ws_bytes - used, n_cu, st);
+    for (int64_t t = 0; t < p.T; t += kTokensPerLaunch) {
+        const hipError_t e = by_channels<O>(tokens<O>(p, t, std::min(kTokensPerLaunch, p.T - t)), [&](const LinearP& b) {
+            return product<O>(b, reinterpret_cast<int32_t*>(ws + used), ws_bytes - used, n_cu, st);
+        });
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

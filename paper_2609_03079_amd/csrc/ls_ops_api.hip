@@ -162,8 +162,6 @@ ls_status ls_linear_i8(ls_ops* c, const ls_linear_i8_args* a) {
     LS_REQUIRE(ls::aligned(a->w, 16) && a->w_stride % 16 == 0, "rows of w must be 16-byte aligned");
     LS_REQUIRE(ls::aligned(a->w_scale, 4) && ls::aligned(a->x_scale, 4) && ls::aligned(a->bias, 4) && element_aligned(a->out, a->out_type),
                "a pointer is not aligned to its type");
-    // one workgroup per 16 channels and 128 tokens at the finest
-    LS_REQUIRE(ls::ceil_div(a->n_tokens, 64) * ls::ceil_div(a->n, 16) < (int64_t)1 << 31, "n_tokens and n are too large for one call");
     LS_REQUIRE(a->x_type == LS_I8 || a->n_tokens < 1 << 23, "n_tokens must be below 2^23 where x is quantised on the way");
     const size_t need = ls::linear_workspace(*a);
     if (need > c->ws_bytes)
