@@ -4,7 +4,7 @@
 // Both operands are contiguous in k, which is what the integer matrix instructions take: a lane
 // holds 16 consecutive bytes of a row of w and of a row of q.  Sums are exact (32-bit integers,
 // |sum| < 2^31 for k < 2^17), so neither the order of the sum nor the kernel chosen changes a bit
-// of the result; the two scales and the bias are applied once, in fp32.
+// of the result; the two scales and the bias are applied once, in fp32 and in the same order everywhere.
 #include <algorithm>
 #include <type_traits>
 
@@ -37,11 +37,19 @@ struct LinearP {
     int32_t* part;       // [splits][T][n] sums of the splits
 };
 
+// A sum with its scales and bias, the same three roundings in every kernel: left to the compiler, some
+// added the bias in one step with the product and some after it, and some rounded to float16 in that step
+// too, which the empty statement keeps apart.  Without a bias: adds -0, which changes nothing.
+__device__ inline float scaled(int acc, float s, float w_scale, float bias) {
+    float v = fmaf((float)acc * s, w_scale, bias);
+    asm("" : "+v"(v));
+    return v;
+}
+__device__ inline float bias_of(const LinearP& p, int n) { return p.bias ? p.bias[n] : -0.f; }
+
 template <typename O>
 __device__ inline void put(const LinearP& p, int t, int n, int acc, float s) {
-    float v = (float)acc * s * p.w_scale[n];
-    if (p.bias) v += p.bias[n];
-    static_cast<O*>(p.out)[(int64_t)t * p.out_stride + n] = (O)v;
+    static_cast<O*>(p.out)[(int64_t)t * p.out_stride + n] = (O)scaled(acc, s, p.w_scale[n], bias_of(p, n));
 }
 
 // Channels n0 .. n0 + n - 1 of the product, and tokens t0 .. t0 + T - 1.
@@ -370,7 +378,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void tile_kernel(const L
 #pragma unroll
     for (int j = 0; j < tile.TN; ++j) {
         const int n = min(c0 + j * 32, p.n - 1);
-        ws[j] = p.w_scale[n], bias[j] = p.bias ? p.bias[n] : 0.f;
+        ws[j] = p.w_scale[n], bias[j] = bias_of(p, n);
     }
     O* to = static_cast<O*>(p.out) + (int64_t)(t0 + r0) * p.out_stride + c0;
     auto write = [&](auto whole) {  // whole: nothing of the tile lies outside the product
@@ -384,9 +392,8 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void tile_kernel(const L
 #pragma unroll
                     for (int j = 0; j < tile.TN; ++j) {
                         const int row = i * 32 + 2 * g + e;
-                        const float v = (float)tile.acc[i][j][g + e] * s[e] * ws[j];
                         if (whole.value || (t0 + r0 + row < p.T && c0 + j * 32 < p.n))
-                            to[row * p.out_stride + j * 32] = (O)(p.bias ? v + bias[j] : v);
+                            to[row * p.out_stride + j * 32] = (O)scaled(tile.acc[i][j][g + e], s[e], ws[j], bias[j]);
                     }
             }
     };
