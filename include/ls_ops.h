@@ -180,7 +180,8 @@ ls_status ls_kv_append(ls_ops* ctx, const ls_kv_cache* cache, const ls_append_ar
  * the cache's type for the product with the values (to a step of 2^-31 of the row's largest, at
  * the finest, in f16).
  * LS_E_CAPACITY if the workspace cannot hold the parts of one split
- * (n_seqs n_q n_heads 2 (head_dim + 2) floats). */
+ * (n_seqs n_q n_heads 2 (head_dim + 2) floats; of more than 2^20 rows n_seqs n_q n_heads as many
+ * whole sequences as 2^20 hold are taken at a time). */
 typedef struct {
     int32_t n_seqs, n_q, n_heads;
     int32_t prefix_len, max_len;

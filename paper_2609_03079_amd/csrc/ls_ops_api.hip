@@ -1,4 +1,5 @@
 // ls_ops_api.hip - the C entry points of include/ls_ops.h: context, checks of arguments, launches.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -206,7 +207,6 @@ ls_status ls_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a) {
                "prefix_len and max_len must be in 0..2^22 - 1");
     LS_REQUIRE(std::isfinite(a->scale) && a->scale > 0.f, "scale must be finite and > 0");
     if (a->n_seqs == 0) return LS_OK;
-    LS_REQUIRE((int64_t)a->n_seqs * a->n_q * a->n_heads < (int64_t)1 << 26, "n_seqs * n_q * n_heads must be below 2^26");
     LS_REQUIRE(a->q && a->out && a->lens, "q, out or lens is NULL");
     LS_REQUIRE(a->prefix_len == 0 || a->prefix_pages, "prefix_pages is NULL");
     LS_REQUIRE(a->max_len == 0 || a->pages, "pages is NULL");
@@ -218,10 +218,21 @@ ls_status ls_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a) {
     LS_REQUIRE(ls::aligned(a->q, 16) && ls::aligned(a->out, 16) && ls::aligned(kv->k, 16) && ls::aligned(kv->v, 16),
                "q, out, k and v must be 16-byte aligned");
     LS_REQUIRE(ls::aligned(a->prefix_pages, 4) && ls::aligned(a->pages, 4) && ls::aligned(a->lens, 4), "a pointer is not aligned to its type");
-    ls::AttendPlan plan;
-    if (!ls::plan_attend(*kv, *a, c->ws_bytes, c->n_cu, &plan))
-        return fail(c, LS_E_CAPACITY, "the partial results do not fit the workspace of %zu bytes", c->ws_bytes);
-    return launched(c, ls::launch_attend(*kv, *a, plan, c->ws, c->stream), "ls_attend");
+    // A launch holds fewer than 2^32 threads: more rows than 2^20 (at most 2^21 workgroups for a part) are taken in pieces.
+    const int64_t piece = std::max<int64_t>(1, (1 << 20) / ((int64_t)a->n_q * a->n_heads)), es = (int64_t)ls::type_size(kv->dtype);
+    for (int64_t s = 0; s < a->n_seqs; s += piece) {
+        ls_attend_args b = *a;
+        b.n_seqs = (int32_t)std::min<int64_t>(piece, a->n_seqs - s);
+        b.q = static_cast<const char*>(a->q) + s * a->n_q * a->q_token_stride * es;
+        b.out = static_cast<char*>(a->out) + s * a->n_q * a->out_token_stride * es;
+        if (b.pages) b.pages += s * a->pages_stride;
+        b.lens += s;
+        ls::AttendPlan plan;
+        if (!ls::plan_attend(*kv, b, c->ws_bytes, c->n_cu, &plan))
+            return fail(c, LS_E_CAPACITY, "the partial results do not fit the workspace of %zu bytes", c->ws_bytes);
+        if ((st = launched(c, ls::launch_attend(*kv, b, plan, c->ws, c->stream), "ls_attend")) != LS_OK) return st;
+    }
+    return LS_OK;
 }
 
 }  // extern "C"

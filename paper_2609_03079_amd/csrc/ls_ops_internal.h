@@ -30,7 +30,7 @@ struct AttendPlan {
     bool pre_wide, suf_wide;              // 128-row tiles instead of 32-row tiles
     bool together;                        // a wide prefix and narrow sequences in one launch
 };
-// False where no split fits the workspace.
+// For at most 2^20 rows n_seqs n_q n_heads, or one sequence.  False where no split fits the workspace.
 bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan);
 hipError_t launch_attend(const ls_kv_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws,
                          hipStream_t st);
