@@ -354,12 +354,15 @@ def Ops(*, workspace_bytes=0, stream=None):
     """The decoder layer's operators around the FFN (``ls_ops.h``) on one stream: an object whose
     methods mirror the C entry points (``ls_norm_residual``, ``ls_linear_i8``, ``ls_kv_append``,
     ``ls_attend``, ``ls_ops_sync``; ``close`` releases it).  Sizes, strides and types are those of
-    the tensors they are given; a tensor that does not fit raises ``ValueError``, a call that the
-    library refuses ``LsError``."""
+    the tensors they are given; a tensor that does not fit or is on another GPU than the context (the
+    one that is current here) raises ``ValueError``, a call that the library refuses ``LsError``."""
     import torch
     if stream is None:
         stream = torch.cuda.current_stream()
-    o = _load_native().Ops(workspace_bytes, stream.cuda_stream)
+    device = torch.cuda.current_device()
+    if stream.device.index != device:
+        raise ValueError(f"the stream belongs to device {stream.device.index}, the current device is {device}")
+    o = _load_native().Ops(workspace_bytes, stream.cuda_stream, device)
     o.torch_stream = stream   # lives as long as the context that borrows it
     _live.add(o)
     return o

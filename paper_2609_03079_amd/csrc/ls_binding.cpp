@@ -36,13 +36,6 @@ void expect(const Tensor& t, at::ScalarType type, const char* what) {
     if (t.scalar_type() != type) bad(std::string(what) + " has the wrong type");
 }
 
-// A GPU tensor of the given sizes whose last dimension is contiguous.
-void shaped(const Tensor& t, at::IntArrayRef sizes, const char* what) {
-    if (!t.is_cuda()) bad(std::string(what) + " is not on the GPU");
-    if (t.sizes() != sizes) bad(std::string(what) + " has the wrong shape");
-    if (t.size(-1) > 1 && t.stride(-1) != 1) bad(std::string(what) + " is not contiguous in its last dimension");
-}
-
 // Stride of a dimension in elements, 0 where it has one entry.
 int64_t step(const Tensor& t, int dim) { return t.size(dim) > 1 ? t.stride(dim) : 0; }
 
@@ -55,7 +48,8 @@ const void* data(const Maybe& t) { return t ? t->const_data_ptr() : nullptr; }
 
 class Ops {
 public:
-    Ops(uint64_t workspace_bytes, uintptr_t stream) {
+    // device: the current one, which the library makes the context on
+    Ops(uint64_t workspace_bytes, uintptr_t stream, int device) : device_(device) {
         ls_ops_desc d{};
         d.workspace_bytes = workspace_bytes;
         d.stream = reinterpret_cast<void*>(stream);
@@ -170,7 +164,8 @@ public:
         if (cos_sin) {
             if (cos_sin->dim() != 2) bad("cos_sin has the wrong shape");
             expect(*cos_sin, at::kFloat, "cos_sin");
-            if (!cos_sin->is_cuda() || !cos_sin->is_contiguous()) bad("cos_sin is not contiguous on the GPU");
+            on_device(*cos_sin, "cos_sin");
+            if (!cos_sin->is_contiguous()) bad("cos_sin is not contiguous");
             a.n_pos = count(cos_sin->size(0), "cos_sin"), a.rot_dim = count(cos_sin->size(1), "cos_sin");
             a.cos_sin = static_cast<const float*>(cos_sin->const_data_ptr());
         }
@@ -212,6 +207,19 @@ public:
 
 private:
     ls_ops* ctx_ = nullptr;
+    int device_;
+
+    void on_device(const Tensor& t, const char* what) const {
+        if (!t.is_cuda()) bad(std::string(what) + " is not on the GPU");
+        if (t.device().index() != device_) bad(std::string(what) + " is on another GPU than the context");
+    }
+
+    // A tensor of the context's GPU, of the given sizes, whose last dimension is contiguous.
+    void shaped(const Tensor& t, at::IntArrayRef sizes, const char* what) const {
+        on_device(t, what);
+        if (t.sizes() != sizes) bad(std::string(what) + " has the wrong shape");
+        if (t.size(-1) > 1 && t.stride(-1) != 1) bad(std::string(what) + " is not contiguous in its last dimension");
+    }
 
     void check(ls_status st) const {
         if (st == LS_OK) return;
@@ -221,14 +229,14 @@ private:
         throw py::error_already_set();
     }
 
-    static const int32_t* indices(const Tensor& t, at::IntArrayRef sizes, const char* what) {
+    const int32_t* indices(const Tensor& t, at::IntArrayRef sizes, const char* what) const {
         expect(t, at::kInt, what);
         shaped(t, sizes, what);
         return static_cast<const int32_t*>(t.const_data_ptr());
     }
 
     // [n_pages, n_kv_heads, page_size, head_dim], both of the same strides in any order
-    static ls_kv_cache cache(const Tensor& k, const Tensor& v) {
+    ls_kv_cache cache(const Tensor& k, const Tensor& v) const {
         if (k.dim() != 4) bad("k_cache has the wrong shape");
         ls_kv_cache c{};
         c.dtype = type_of(k, "k_cache");
@@ -250,7 +258,7 @@ private:
 PYBIND11_MODULE(_lsops, m) {
     m.attr("digest") = LS_BUILD_DIGEST;
     py::class_<Ops>(m, "Ops", py::dynamic_attr())
-        .def(py::init<uint64_t, uintptr_t>())
+        .def(py::init<uint64_t, uintptr_t, int>())
         .def("close", &Ops::close)
         .def_property_readonly("ctx", &Ops::ctx)
         .def("ls_ops_sync", &Ops::sync)
