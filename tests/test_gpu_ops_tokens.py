@@ -46,3 +46,38 @@ def test_a_later_tokens_key_or_value_stays_out(ops, dt, dim, heads, n_q, bad):
                 assert not torch.any(torch.isfinite(out[first:n_q, :, 3]))
             elif math.isnan(bad):
                 assert torch.all(torch.isnan(out[first:n_q]))
+
+
+def attend_us(ops, S, n_q, heads, kv, dim, own, prefix):
+    """Microseconds of a call among others, the least of several rounds."""
+    page, dt, dev = 64, torch.bfloat16, "cuda:0"
+    n, pre = -(-own // page), -(-prefix // page)
+    g = torch.Generator(dev).manual_seed(1)
+    kc, vc = (torch.randn((n * S + pre, kv, page, dim), device=dev, generator=g).to(dt) for _ in range(2))
+    pages = torch.arange(n * S, dtype=torch.int32, device=dev).view(S, n)
+    prefix_pages = torch.arange(n * S, n * S + pre, dtype=torch.int32, device=dev)
+    lens = torch.full((S,), own, dtype=torch.int32, device=dev)
+    q = torch.randn((S * n_q, heads, dim), device=dev, generator=g).to(dt)
+    out, best = torch.empty_like(q), math.inf
+    for _ in range(8):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        torch.cuda.synchronize()
+        a.record()
+        for _ in range(10):
+            ops.ls_attend(q, kc, vc, pages, lens, out, max_len=own, n_q=n_q, scale=dim ** -0.5, prefix_pages=prefix_pages, prefix_len=prefix)
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b) * 100)
+    return best
+
+
+@pytest.mark.parametrize("S,n_q,heads,kv,dim,own,prefix", [(16, 8, 64, 8, 128, 512, 8192), (64, 16, 32, 8, 128, 200, 16384),
+                                                           (16, 8, 64, 8, 64, 512, 8192)])
+def test_tokens_cost_little_more_than_as_many_heads(ops, S, n_q, heads, kv, dim, own, prefix):
+    """The same rows and keys, once as tokens of a sequence and once as heads of one token: what the masks of a
+    sequence's last keys cost must not be paid along the prefix, nor a second round of workgroups by a
+    plan that counts more of them at once than run."""
+    tokens = attend_us(ops, S, n_q, heads, kv, dim, own, prefix)
+    one = attend_us(ops, S, 1, heads * n_q, kv, dim, own, prefix)
+    print(f"{tokens:.1f} us, as heads {one:.1f}")
+    assert tokens <= 1.6 * one
