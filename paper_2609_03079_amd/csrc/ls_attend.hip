@@ -608,6 +608,10 @@ __global__ __launch_bounds__(64) void join_kernel(const AttendP p) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) m[i] = l[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(m[i] - base);  // now its weight
     const float sum = wave_sum_dpp(l[0] * m[0] + l[1] * m[1]);
+    // parts without a key must not count, whatever lies in their place; the others must, even with a weight
+    // that is zero in fp32: a value that is no number makes the row none
+#pragma unroll
+    for (int i = 0; i < 2; ++i) m[i] = l[i] == 0.f ? -1.f : m[i];
     f32x4 acc{};
     for (int j0 = 0; j0 < last; j0 += U * GR) {
         if (j0) ask(j0);
@@ -615,7 +619,7 @@ __global__ __launch_bounds__(64) void join_kernel(const AttendP p) {
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u * GR + g;
             const float w = __shfl(j < 64 ? m[0] : m[1], j & 63, 64);
-            if (j < last && w != 0.f) acc += v[u] * w;
+            if (j < last && !(w < 0.f)) acc += v[u] * w;
         }
     }
 #pragma unroll

@@ -78,3 +78,26 @@ def test_many_keys_far_below_the_largest_count(ops, dt, dim, form, gap):
         ref, size = w * seen.sum(0) / total, seen.sum(0) / total
         tol = (2 * u + 2.0 ** -17) * ref + (2.0 ** -32 * size if dt == torch.float16 else 0) + 2.0 ** -25
         assert torch.all((out[i::n_q].double() - ref).abs() <= tol)
+
+
+@pytest.mark.parametrize("dt", BOTH, ids=["f16", "bf16"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("shared", [False, True], ids=["own", "prefix"])
+@pytest.mark.parametrize("at", [0, 77, 2000, 4095])
+def test_a_visible_value_that_is_no_number_counts_at_any_weight(ops, dt, bad, shared, at):
+    """A key 200 below the largest, the value of whose element 3 is no number: so is the row's element 3, and no other."""
+    n, G, page, dim = 4096, 4, 64, 64
+    kc, vc = (torch.zeros((n // page, 1, page, dim), dtype=dt, device=DEV) for _ in range(2))
+    vc.normal_(generator=torch.Generator(DEV).manual_seed(at))
+    top = 1000
+    kc[top // page, 0, top % page, 0] = 1
+    vc[at // page, 0, at % page, 3] = bad
+    pages = torch.arange(n // page, dtype=torch.int32, device=DEV)
+    q = torch.zeros((1, G, dim), dtype=dt, device=DEV)
+    q[..., 0] = 200
+    out = torch.empty_like(q)
+    args = dict(max_len=0, prefix_pages=pages, prefix_len=n) if shared else dict(max_len=n)
+    lens = torch.full((1,), 0 if shared else n, dtype=torch.int32, device=DEV)
+    ops.ls_attend(q, kc, vc, None if shared else pages[None], lens, out, scale=1.0, **args)
+    fine = torch.isfinite(out)
+    assert not fine[..., 3].any() and fine[..., :3].all() and fine[..., 4:].all()
