@@ -94,8 +94,9 @@ ls_status ls_norm_residual(ls_ops* ctx, const ls_norm_args* a);
  * the way, s_t = max_k |x_tk| / 127 and q_tk = round(127 x_tk / max_k |x_tk|), to nearest, ties to
  * even, in fp32 (x_scale must be NULL).  A token of zeros (or whose s_t is below the smallest
  * normal fp32 number) has s_t = 0; one that holds an infinity or NaN gives NaN in its whole row.
- * The sums are exact in 32-bit integers; scales and bias (fp32 [n] or NULL) are applied in fp32
- * and rounded once to out_type (LS_F32, LS_F16 or LS_BF16).
+ * The sums are exact in 32-bit integers; s_t, then w_scale, then the bias (fp32 [n] or NULL) are
+ * applied in fp32 and rounded once to out_type (LS_F32, LS_F16 or LS_BF16): a token's row has the
+ * same bits whatever tokens are beside it.
  * w: int8 [n, k] (nn.Linear layout, quantised by row).  k: a multiple of 16, at most 131056;
  * rows of x and w 16-byte aligned.  n >= 1; n_tokens 0 does nothing; n_tokens < 2^23 where x is
  * quantised on the way.
@@ -171,7 +172,8 @@ ls_status ls_kv_append(ls_ops* ctx, const ls_kv_cache* cache, const ls_append_ar
  * every row of a sequence with lens[s] < 0, an idle slot.  Nothing else of a masked key reaches
  * the result, whatever it holds.  A page id outside [0, n_pages) masks its keys.
  * prefix_pages: dev int32, ceil(prefix_len / page_size) ids; pages: dev int32
- * [n_seqs, pages_stride]; lens: dev int32 [n_seqs], of which at most max_len counts;
+ * [n_seqs, pages_stride]; lens: dev int32 [n_seqs], of which at most max_len counts (the work is
+ * shared out by max_len: a bound far above the lengths gives each sequence fewer workgroups);
  * pages_stride * page_size >= max_len unless max_len is 0.
  * q, out: [n_seqs * n_q, n_heads, head_dim] of the cache's type (f16 or bf16; LS_E_UNSUPPORTED
  * for LS_F32).  head_dim: a multiple of 8, at most 256; pointers and strides of q, out, k and v

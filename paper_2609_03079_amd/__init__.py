@@ -355,7 +355,8 @@ def Ops(*, workspace_bytes=0, stream=None):
     methods mirror the C entry points (``ls_norm_residual``, ``ls_linear_i8``, ``ls_kv_append``,
     ``ls_attend``, ``ls_ops_sync``; ``close`` releases it).  Sizes, strides and types are those of
     the tensors they are given; a tensor that does not fit or is on another GPU than the context (the
-    one that is current here) raises ``ValueError``, a call that the library refuses ``LsError``."""
+    one that is current here) raises ``ValueError``, a call that the library refuses ``LsError``.
+    Calls only enqueue: tensors must live until the stream is done with them."""
     import torch
     if stream is None:
         stream = torch.cuda.current_stream()

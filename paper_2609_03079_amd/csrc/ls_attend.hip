@@ -19,7 +19,7 @@
 // Two shapes of workgroup:
 //  - wide: four waves of 32 rows share 64 keys in shared memory, the scores of the next 64 computed
 //    while the exponentials of these are: bound by the vector and matrix units together (64
-//    sequences, 64 query and 8 key heads of 128 bfloat16, 32768 prefix keys: 91 to 104 us, 68.7
+//    sequences, 64 query and 8 key heads of 128 bfloat16, 32768 prefix keys: 93 to 107 us, 68.7
 //    GFLOP, the matrix units busy for two fifths of it; 79 without any copies);
 //  - narrow (up to 32 rows): two waves, each taking every second 32 keys through its own share of
 //    shared memory, without barriers, the waves' results joined at the end: bound by each wave's
@@ -28,6 +28,12 @@
 //    the first products wait for each other, about 5.5 us.  Asking for keys and values two tiles
 //    ahead in place of one changed nothing there.
 // In both the next keys are copied straight to shared memory while the present ones are used.
+//
+// Registers, with 512 a lane for one wave a SIMD and 256 for two: the kernels of one token spill 5 to 7 at
+// heads of 128, held to two; a path that takes a sequence's tokens one by one (for values that
+// are no numbers) costs the kernels of several tokens more, 62 to 65 spilled where a wide prefix
+// runs beside narrow sequences at heads of 128, 110 to 127 at heads of 256, and its own
+// launch of wide workgroups runs one of them a compute unit at heads of up to 128, where the others run two.
 #include <algorithm>
 #include <type_traits>
 

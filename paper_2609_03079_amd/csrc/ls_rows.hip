@@ -2,8 +2,7 @@
 // block with its gated residual update, and the append of rotated keys and values to a paged cache.
 //
 // Both are bound by HBM (or, for a handful of tokens, by the latency of one pass of loads): a
-// row is read into registers once, everything is computed there in fp32, and the result is
-// written once.
+// row is read once, everything is computed in fp32, and the result is written once.
 #include <algorithm>
 
 #include "ls_device.h"
@@ -48,6 +47,10 @@ __device__ inline float row_sum(float v, float* part) {
 // and two sums.  Rows of up to 8192 elements have a thread for every vector: 8191 x 8192 bfloat16
 // with a gate for each token 171 us, with four vectors a thread 230; outputs larger than the caches
 // are stored past them: 163 to 173 us (939 MB at 5.4 to 5.7 TB/s; a copy of 1 GiB moves 5.2).
+// The row stays in registers up to 16384 elements in whole vectors, up to 8192 otherwise; longer ones do not
+// fit the 128 that 1024 threads leave a lane (55 to 168 spilled) and go partly through scratch memory: 4096 rows
+// of bfloat16 with a gate for each token take 193 us at 16384 elements, 458 at 20480, 549 at 12289.
+// Rows of odd lengths or addresses move an element an access: 8191 elements 166 us, 8192 94.
 template <typename T, int V, int C, int NT>
 __global__ __launch_bounds__(NT) void norm_kernel(const ls_norm_args p, bool past_caches) {
     __shared__ float part[2][NT / 64];
