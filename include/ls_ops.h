@@ -4,7 +4,8 @@
  * ls_ffn.h computes the FFN half of a decoder layer.  These calls are the other half, for the
  * same decode loop: the norms around a block with its gated residual update, the 8-bit integer
  * projections, the append of rotated keys and values to a paged cache, and the attention of a
- * batch whose sequences share a prefix.
+ * batch whose sequences share a prefix; the same cache held in 4 or 8 bits, written, read back and
+ * attended; and the decision about the tokens that a step drafted.
  *
  * Conventions, beyond those of ls_ffn.h (status codes, nothing aborts or throws, argument
  * validation is synchronous, sticky LS_E_DEVICE, one host thread per context, the same bits on
@@ -33,6 +34,9 @@ extern "C" {
 typedef struct ls_ops ls_ops; /* opaque context; owns the workspace */
 
 #define LS_I8 ((ls_dtype)3) /* 8-bit integers: inputs of ls_linear_i8 only */
+/* codes of a quantised cache (ls_kvq_cache): floating numbers of 4 and 8 bits that share a power of two by 32 */
+#define LS_FP4 ((ls_dtype)4) /* sign, 2 bits of exponent, 1 of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6 */
+#define LS_FP8 ((ls_dtype)5) /* sign, 4 bits of exponent, 3 of mantissa: up to 448; 0x7f and 0xff are NaN */
 
 #define LS_OPS_WORKSPACE_DEFAULT (256ull << 20)
 
@@ -198,6 +202,87 @@ typedef struct {
     const int32_t* lens;
 } ls_attend_args;
 ls_status ls_attend(ls_ops* ctx, const ls_kv_cache* cache, const ls_attend_args* a);
+
+/* The paged cache in 4 or 8 bits.  A row (one head of one token) holds head_dim elements in groups of 32, the last of
+ * which may be shorter.  A group has a scale byte b, the power of two 2^(b - 127), 255: the group holds no
+ * numbers; its element is code * 2^(b - 127).  LS_FP4: two codes a byte, the first in the low half.
+ * Row (page, head, i) of k starts at k + page * page_stride + head * head_stride + i * token_stride, all in bytes:
+ * head_dim / 2 or head_dim contiguous bytes; its ceil(head_dim / 32) scale bytes at k_scale + page * scale_page_stride + ...;
+ * v likewise.  k, v and the strides of codes are multiples of 4 bytes (LS_FP4) or 8 (LS_FP8); scales have no alignment
+ * (aligned to a row's scale bytes they are read faster). */
+typedef struct {
+    void* k;
+    void* v;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    ls_dtype code;       /* LS_FP4 or LS_FP8 */
+    int32_t n_pages;
+    int32_t page_size;   /* tokens per page: a power of two, 1 .. 4096; n_pages * page_size < 2^31 */
+    int32_t n_kv_heads;
+    int32_t head_dim;    /* a multiple of 8 in 8 .. 1024 */
+    int64_t page_stride, head_stride, token_stride;
+    int64_t scale_page_stride, scale_head_stride, scale_token_stride;
+} ls_kvq_cache;
+
+/* ls_kv_append into the quantised cache.  k, v, q and q_out are of `type` (LS_F32, LS_F16 or LS_BF16); keys are turned in fp32 and
+ * quantised from there, values from what they are.  With top the largest magnitude of a group, its scale is the smallest
+ * power of two with top < 7 * 2^e (LS_FP4) or 464 * 2^e (LS_FP8), no smaller than 2^-126 and no larger than leaves the largest
+ * code finite in `type`; a code is the element over the scale, to nearest, ties to the even code, at most the largest code.
+ * A group that holds an infinity or NaN gets the scale byte 255 and zeros for codes.  Slots, positions, q and q_out as in
+ * ls_kv_append (q_out may be q itself). */
+ls_status ls_kvq_append(ls_ops* ctx, const ls_kvq_cache* cache, ls_dtype type, const ls_append_args* a);
+
+/* Reads the keys and values of tokens back: k[t] = the row of slots[t], in `type`, rounded once (exact in LS_F32; in the
+ * 16-bit types wherever a value is inside their range).  slots: dev int32 [n_tokens]; a token whose slot is
+ * outside the cache leaves its rows as they were.  k, v: [n_tokens, n_kv_heads, head_dim]. */
+typedef struct {
+    int32_t n_tokens;
+    ls_dtype type; /* LS_F32, LS_F16 or LS_BF16 */
+    const int32_t* slots;
+    void* k;
+    int64_t k_token_stride, k_head_stride;
+    void* v;
+    int64_t v_token_stride, v_head_stride;
+} ls_kvq_read_args;
+ls_status ls_kvq_read(ls_ops* ctx, const ls_kvq_cache* cache, const ls_kvq_read_args* a);
+
+/* ls_attend over the quantised cache: the same attention, with the values that ls_kvq_read gives in `type` for keys and values
+ * (a value outside the range of LS_F16 is infinite there).  q and out are of `type`: LS_F16 or LS_BF16 (LS_E_UNSUPPORTED for
+ * LS_F32); pointers and strides of q and out 16-byte aligned; head_dim at most 256. */
+ls_status ls_kvq_attend(ls_ops* ctx, const ls_kvq_cache* cache, ls_dtype type, const ls_attend_args* a);
+
+/* Decides about drafted tokens: with p the target's probabilities, q those that drafted them and u given random numbers in [0, 1),
+ *   draft i of sequence s is accepted if those before it were and accept[s, i] q_i(x_i) < p_i(x_i)  (x_i = drafts[s, i]);
+ *   r = the number accepted; the next token comes from w = max(p_r - q_r, 0) if draft r was refused, from w = p_n
+ *   behind the last of the n drafts: the first token t with w_0 + ... + w_t > sample[s] (w_0 + w_1 + ...);
+ *   tokens[s] = x_0 .. x_{r-1}, that token, then -1;  n_accepted[s] = r.
+ * So the tokens are distributed as the target's.  Products, differences and sums are in 64 bits.  Where w is zero
+ * everywhere it is p_r; where that is, too, the token is -1.  What is no number or below zero in w counts as zero,
+ * infinities as the largest fp32 number; sample below 0 as 0, and from 1 on, or NaN, the last token with a weight is taken.  A drafted
+ * id outside the vocabulary is refused (with `draft` NULL nothing is taken off for it).
+ * target: [n_seqs, n_drafts + 1, vocab], draft: [n_seqs, n_drafts, vocab] of `type` (LS_F32, LS_F16, LS_BF16), rows contiguous; draft
+ * NULL: q is one at the drafted token (a draft without chance).  drafts: int32 [n_seqs, n_drafts]; counts: int32 [n_seqs] or NULL:
+ * sequence s has min(counts[s], n_drafts) drafts; below 0 it is an idle slot: tokens -1, n_accepted -1.
+ * accept: fp32 [n_seqs, n_drafts]; sample: fp32 [n_seqs]; tokens: int32 [n_seqs, n_drafts + 1]; n_accepted: int32 [n_seqs]; all on the device.
+ * 0 <= n_drafts <= 63 (0: tokens drawn from p); vocab >= 1; n_seqs 0 does nothing. */
+typedef struct {
+    int32_t n_seqs, n_drafts, vocab;
+    ls_dtype type;
+    const void* target;
+    int64_t target_seq_stride, target_token_stride;
+    const void* draft;
+    int64_t draft_seq_stride, draft_token_stride;
+    const int32_t* drafts;
+    int64_t drafts_stride;
+    const int32_t* counts;
+    const float* accept;
+    int64_t accept_stride;
+    const float* sample;
+    int32_t* tokens;
+    int64_t tokens_stride;
+    int32_t* n_accepted;
+} ls_verify_args;
+ls_status ls_verify(ls_ops* ctx, const ls_verify_args* a);
 
 #ifdef __cplusplus
 }

@@ -23,7 +23,7 @@ LIB_PATH = os.path.join(_HERE, "liblsffn.so")
 LS_OK, LS_E_INVAL, LS_E_NOMEM, LS_E_DEVICE, LS_E_STATE, LS_E_UNSUPPORTED, LS_E_CAPACITY = range(7)
 STATUS_NAMES = {0: "LS_OK", 1: "LS_E_INVAL", 2: "LS_E_NOMEM", 3: "LS_E_DEVICE", 4: "LS_E_STATE",
                 5: "LS_E_UNSUPPORTED", 6: "LS_E_CAPACITY"}
-LS_F32, LS_F16, LS_BF16, LS_I8 = 0, 1, 2, 3
+LS_F32, LS_F16, LS_BF16, LS_I8, LS_FP4, LS_FP8 = range(6)
 LS_ACT_REGLU, LS_ACT_SWIGLU_THRESH = 0, 1
 LS_WEIGHTS_HBM, LS_WEIGHTS_HOST = 0, 1
 LS_SEL_TOPK, LS_SEL_THRESHOLD = 0, 1
@@ -38,7 +38,7 @@ EXPORTS = ("ls_ffn_create", "ls_ffn_set_layer", "ls_ffn_destroy", "ls_predict", 
            "ls_debug_stages_done", "ls_measure_read_bandwidth", "ls_build_digest", "ls_last_error")
 # entry points of ls_ops.h
 OPS_EXPORTS = ("ls_ops_create", "ls_ops_destroy", "ls_ops_sync", "ls_ops_last_error", "ls_norm_residual", "ls_linear_i8",
-               "ls_kv_append", "ls_attend")
+               "ls_kv_append", "ls_attend", "ls_kvq_append", "ls_kvq_read", "ls_kvq_attend", "ls_verify")
 (LS_CFG_DECODE_PATH, LS_CFG_SPEC_BLOCKS, LS_CFG_TRACE_WG, LS_CFG_COOPERATIVE, LS_CFG_BATCH_MFMA, LS_CFG_ZERO_SKIP,
  LS_CFG_STREAM_SYNC, LS_CFG_STAGE_WAIT_US) = range(8)
 LS_SYNC_EVENTS, LS_SYNC_FLAGS, LS_SYNC_HOST = range(3)
@@ -139,10 +139,12 @@ def load():
     lib.ls_ops_destroy.argtypes = [P]
     lib.ls_ops_sync.argtypes = [P]
     lib.ls_ops_last_error.argtypes = [P]
-    for name in ("ls_norm_residual", "ls_linear_i8"):
+    for name in ("ls_norm_residual", "ls_linear_i8", "ls_verify"):
         getattr(lib, name).argtypes = [P, P]
-    for name in ("ls_kv_append", "ls_attend"):
+    for name in ("ls_kv_append", "ls_attend", "ls_kvq_read"):
         getattr(lib, name).argtypes = [P, P, P]
+    for name in ("ls_kvq_append", "ls_kvq_attend"):
+        getattr(lib, name).argtypes = [P, P, ctypes.c_int, P]
     for name in OPS_EXPORTS:
         getattr(lib, name).restype = ctypes.c_char_p if name == "ls_ops_last_error" else ctypes.c_int
     for name in EXPORTS:
@@ -353,7 +355,8 @@ def _load_native():
 def Ops(*, workspace_bytes=0, stream=None):
     """The decoder layer's operators around the FFN (``ls_ops.h``) on one stream: an object whose
     methods mirror the C entry points (``ls_norm_residual``, ``ls_linear_i8``, ``ls_kv_append``,
-    ``ls_attend``, ``ls_ops_sync``; ``close`` releases it).  Sizes, strides and types are those of
+    ``ls_attend``, ``ls_kvq_append``, ``ls_kvq_read``, ``ls_kvq_attend``, ``ls_verify``, ``ls_ops_sync``;
+    ``close`` releases it).  Sizes, strides and types are those of
     the tensors they are given; a tensor that does not fit or is on another GPU than the context (the
     one that is current here) raises ``ValueError``, a call that the library refuses ``LsError``.
     Calls only enqueue: tensors must live until the stream is done with them."""

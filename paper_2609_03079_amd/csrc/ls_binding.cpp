@@ -136,18 +136,101 @@ public:
     void append(const Tensor& k_cache, const Tensor& v_cache, const Tensor& k, const Tensor& v, const Maybe& positions, const Tensor& slots,
                 const Maybe& cos_sin, const Maybe& q, const Maybe& q_out, int style) {
         const ls_kv_cache c = cache(k_cache, v_cache);
+        const ls_append_args a = append_args(c.n_kv_heads, c.head_dim, k_cache.scalar_type(), k, v, positions, slots, cos_sin, q, q_out, style);
+        check(ls_kv_append(ctx_, &c, &a));
+    }
+
+    void attend(const Tensor& q, const Tensor& k_cache, const Tensor& v_cache, const Maybe& pages, const Tensor& lens, const Tensor& out,
+                int64_t max_len, float scale, int64_t n_q, const Maybe& prefix_pages, int64_t prefix_len) {
+        const ls_kv_cache c = cache(k_cache, v_cache);
+        const ls_attend_args a = attend_args(c.page_size, c.head_dim, k_cache.scalar_type(), q, pages, lens, out, max_len, scale, n_q,
+                                             prefix_pages, prefix_len);
+        check(ls_attend(ctx_, &c, &a));
+    }
+
+    void kvq_append(const Tensor& k_codes, const Tensor& k_scales, const Tensor& v_codes, const Tensor& v_scales, const Tensor& k,
+                    const Tensor& v, const Maybe& positions, const Tensor& slots, const Maybe& cos_sin, const Maybe& q, const Maybe& q_out,
+                    int style) {
+        const ls_kvq_cache c = codes(k_codes, k_scales, v_codes, v_scales);
+        const ls_append_args a = append_args(c.n_kv_heads, c.head_dim, k.scalar_type(), k, v, positions, slots, cos_sin, q, q_out, style);
+        check(ls_kvq_append(ctx_, &c, type_of(k, "k"), &a));
+    }
+
+    void kvq_read(const Tensor& k_codes, const Tensor& k_scales, const Tensor& v_codes, const Tensor& v_scales, const Tensor& slots,
+                  const Tensor& k, const Tensor& v) {
+        const ls_kvq_cache c = codes(k_codes, k_scales, v_codes, v_scales);
+        if (k.dim() != 3) bad("k has the wrong shape");
+        ls_kvq_read_args a{};
+        const int64_t T = k.size(0);
+        a.n_tokens = count(T, "k");
+        a.type = type_of(k, "k");
+        expect(v, k.scalar_type(), "v");
+        shaped(k, {T, c.n_kv_heads, c.head_dim}, "k");
+        shaped(v, {T, c.n_kv_heads, c.head_dim}, "v");
+        a.slots = indices(slots, {T}, "slots");
+        a.k = k.data_ptr(), a.k_token_stride = step(k, 0), a.k_head_stride = step(k, 1);
+        a.v = v.data_ptr(), a.v_token_stride = step(v, 0), a.v_head_stride = step(v, 1);
+        check(ls_kvq_read(ctx_, &c, &a));
+    }
+
+    void kvq_attend(const Tensor& q, const Tensor& k_codes, const Tensor& k_scales, const Tensor& v_codes, const Tensor& v_scales,
+                    const Maybe& pages, const Tensor& lens, const Tensor& out, int64_t max_len, float scale, int64_t n_q,
+                    const Maybe& prefix_pages, int64_t prefix_len) {
+        const ls_kvq_cache c = codes(k_codes, k_scales, v_codes, v_scales);
+        const ls_attend_args a = attend_args(c.page_size, c.head_dim, q.scalar_type(), q, pages, lens, out, max_len, scale, n_q, prefix_pages,
+                                             prefix_len);
+        check(ls_kvq_attend(ctx_, &c, type_of(q, "q"), &a));
+    }
+
+    void verify(const Tensor& target, const Tensor& drafts, const Tensor& accept, const Tensor& sample, const Tensor& tokens,
+                const Tensor& n_accepted, const Maybe& draft, const Maybe& n_drafts) {
+        if (target.dim() != 3) bad("target has the wrong shape");
+        ls_verify_args a{};
+        const int64_t S = target.size(0), K = target.size(1) - 1, V = target.size(2);
+        if (K < 0) bad("target has the wrong shape");
+        a.n_seqs = count(S, "target"), a.n_drafts = count(K, "target"), a.vocab = count(V, "target");
+        a.type = type_of(target, "target");
+        shaped(target, {S, K + 1, V}, "target");
+        a.target = target.const_data_ptr(), a.target_seq_stride = step(target, 0), a.target_token_stride = step(target, 1);
+        if (draft) {
+            expect(*draft, target.scalar_type(), "draft");
+            shaped(*draft, {S, K, V}, "draft");
+            a.draft = draft->const_data_ptr(), a.draft_seq_stride = step(*draft, 0), a.draft_token_stride = step(*draft, 1);
+        }
+        a.drafts = indices(drafts, {S, K}, "drafts"), a.drafts_stride = step(drafts, 0);
+        if (n_drafts) a.counts = indices(*n_drafts, {S}, "n_drafts");
+        auto numbers = [&](const Tensor& t, at::IntArrayRef sizes, const char* what) {
+            expect(t, at::kFloat, what);
+            shaped(t, sizes, what);
+            return static_cast<const float*>(t.const_data_ptr());
+        };
+        a.accept = numbers(accept, {S, K}, "accept"), a.accept_stride = step(accept, 0);
+        a.sample = numbers(sample, {S}, "sample");
+        indices(tokens, {S, K + 1}, "tokens");
+        indices(n_accepted, {S}, "n_accepted");
+        a.tokens = static_cast<int32_t*>(tokens.data_ptr()), a.tokens_stride = step(tokens, 0);
+        a.n_accepted = static_cast<int32_t*>(n_accepted.data_ptr());
+        check(ls_verify(ctx_, &a));
+    }
+
+private:
+    ls_ops* ctx_ = nullptr;
+    int device_;
+
+    ls_append_args append_args(int64_t n_kv_heads, int64_t d, at::ScalarType type, const Tensor& k, const Tensor& v, const Maybe& positions,
+                               const Tensor& slots, const Maybe& cos_sin, const Maybe& q, const Maybe& q_out, int style) const {
         if (k.dim() != 3) bad("k has the wrong shape");
         ls_append_args a{};
-        const int64_t T = k.size(0), d = c.head_dim;
+        const int64_t T = k.size(0);
         a.n_tokens = count(T, "k");
         a.style = static_cast<ls_rope>(style);
         auto heads = [&](const Tensor& t, int64_t n, const char* what, int64_t* token, int64_t* head) {
-            expect(t, k_cache.scalar_type(), what);
+            expect(t, type, what);
             shaped(t, {T, n, d}, what);
             *token = step(t, 0), *head = step(t, 1);
         };
-        heads(k, c.n_kv_heads, "k", &a.k_token_stride, &a.k_head_stride);
-        heads(v, c.n_kv_heads, "v", &a.v_token_stride, &a.v_head_stride);
+        heads(k, n_kv_heads, "k", &a.k_token_stride, &a.k_head_stride);
+        heads(v, n_kv_heads, "v", &a.v_token_stride, &a.v_head_stride);
         a.k = k.const_data_ptr(), a.v = v.const_data_ptr();
         if (q) {
             if (q->dim() != 3) bad("q has the wrong shape");
@@ -169,21 +252,21 @@ public:
             a.n_pos = count(cos_sin->size(0), "cos_sin"), a.rot_dim = count(cos_sin->size(1), "cos_sin");
             a.cos_sin = static_cast<const float*>(cos_sin->const_data_ptr());
         }
-        check(ls_kv_append(ctx_, &c, &a));
+        return a;
     }
 
-    void attend(const Tensor& q, const Tensor& k_cache, const Tensor& v_cache, const Maybe& pages, const Tensor& lens, const Tensor& out,
-                int64_t max_len, float scale, int64_t n_q, const Maybe& prefix_pages, int64_t prefix_len) {
-        const ls_kv_cache c = cache(k_cache, v_cache);
+    ls_attend_args attend_args(int64_t page_size, int64_t head_dim, at::ScalarType type, const Tensor& q, const Maybe& pages, const Tensor& lens,
+                               const Tensor& out, int64_t max_len, float scale, int64_t n_q, const Maybe& prefix_pages,
+                               int64_t prefix_len) const {
         if (q.dim() != 3 || lens.dim() != 1) bad("q or lens has the wrong shape");
         ls_attend_args a{};
         const int64_t T = q.size(0), heads = q.size(1), S = lens.size(0);
         a.n_seqs = count(S, "lens"), a.n_q = count(n_q, "n_q"), a.n_heads = count(heads, "q");
         if (T != S * n_q) bad("q must have n_q tokens for every sequence");
-        expect(q, k_cache.scalar_type(), "q");
-        expect(out, k_cache.scalar_type(), "out");
-        shaped(q, {T, heads, c.head_dim}, "q");
-        shaped(out, {T, heads, c.head_dim}, "out");
+        expect(q, type, "q");
+        expect(out, type, "out");
+        shaped(q, {T, heads, head_dim}, "q");
+        shaped(out, {T, heads, head_dim}, "out");
         a.q = q.const_data_ptr(), a.q_token_stride = step(q, 0), a.q_head_stride = step(q, 1);
         a.out = out.data_ptr(), a.out_token_stride = step(out, 0), a.out_head_stride = step(out, 1);
         a.lens = indices(lens, {S}, "lens");
@@ -194,20 +277,16 @@ public:
             if (prefix_pages->dim() != 1) bad("prefix_pages has the wrong shape");
             a.prefix_pages = indices(*prefix_pages, {prefix_pages->size(0)}, "prefix_pages");
         }
-        if (prefix_len > 0 && (!prefix_pages || prefix_pages->size(0) * c.page_size < prefix_len))
+        if (prefix_len > 0 && (!prefix_pages || prefix_pages->size(0) * page_size < prefix_len))
             bad("prefix_pages hold fewer than prefix_len keys");
         if (pages) {
             if (pages->dim() != 2) bad("pages has the wrong shape");
             a.pages = indices(*pages, {S, pages->size(1)}, "pages");
-            if (pages->size(1) * c.page_size < max_len) bad("pages hold fewer than max_len keys");
+            if (pages->size(1) * page_size < max_len) bad("pages hold fewer than max_len keys");
             a.pages_stride = S > 1 ? pages->stride(0) : pages->size(1);
         }
-        check(ls_attend(ctx_, &c, &a));
+        return a;
     }
-
-private:
-    ls_ops* ctx_ = nullptr;
-    int device_;
 
     void on_device(const Tensor& t, const char* what) const {
         if (!t.is_cuda()) bad(std::string(what) + " is not on the GPU");
@@ -251,6 +330,39 @@ private:
         c.page_stride = step(k, 0), c.head_stride = step(k, 1), c.token_stride = step(k, 2);
         return c;
     }
+
+    // Codes [n_pages, n_kv_heads, page_size, bytes of a row] and scales [.., scales of a row], each pair of the same strides in any order.
+    ls_kvq_cache codes(const Tensor& k, const Tensor& ks, const Tensor& v, const Tensor& vs) const {
+        if (k.dim() != 4 || ks.dim() != 4) bad("k_codes or k_scales has the wrong shape");
+        ls_kvq_cache c{};
+        const at::ScalarType type = k.scalar_type();
+        if (type == at::kByte)
+            c.code = LS_FP4;
+        else if (type == at::kFloat8_e4m3fn)
+            c.code = LS_FP8;
+        else
+            bad("k_codes has an unsupported type");
+        expect(v, type, "v_codes");
+        expect(ks, at::kByte, "k_scales");
+        expect(vs, at::kByte, "v_scales");
+        shaped(k, k.sizes(), "k_codes");
+        shaped(v, k.sizes(), "v_codes");
+        c.n_pages = count(k.size(0), "k_codes"), c.n_kv_heads = count(k.size(1), "k_codes");
+        c.page_size = count(k.size(2), "k_codes");
+        c.head_dim = count(k.size(3) * (c.code == LS_FP4 ? 2 : 1), "k_codes");
+        const int64_t scales[4] = {k.size(0), k.size(1), k.size(2), (c.head_dim + 31) / 32};
+        shaped(ks, scales, "k_scales");
+        shaped(vs, scales, "v_scales");
+        for (int i = 0; i < 3; ++i) {
+            if (step(k, i) != step(v, i)) bad("k_codes and v_codes have different strides");
+            if (step(ks, i) != step(vs, i)) bad("k_scales and v_scales have different strides");
+        }
+        c.k = k.data_ptr(), c.v = v.data_ptr();
+        c.k_scale = static_cast<uint8_t*>(ks.data_ptr()), c.v_scale = static_cast<uint8_t*>(vs.data_ptr());
+        c.page_stride = step(k, 0), c.head_stride = step(k, 1), c.token_stride = step(k, 2);
+        c.scale_page_stride = step(ks, 0), c.scale_head_stride = step(ks, 1), c.scale_token_stride = step(ks, 2);
+        return c;
+    }
 };
 
 }  // namespace
@@ -280,5 +392,20 @@ PYBIND11_MODULE(_lsops, m) {
              py::arg("out"), py::kw_only(), py::arg("max_len"), py::arg("scale"), py::arg("n_q") = 1, py::arg("prefix_pages") = py::none(),
              py::arg("prefix_len") = 0,
              "q, out: [n_seqs * n_q, n_heads, head_dim]; pages: int32 [n_seqs, pages of a sequence]; lens: int32 [n_seqs]; "
-             "prefix_pages: int32 [pages of the prefix]; max_len: a bound of lens that the caller knows.");
+             "prefix_pages: int32 [pages of the prefix]; max_len: a bound of lens that the caller knows.")
+        .def("ls_kvq_append", &Ops::kvq_append, py::arg("k_codes"), py::arg("k_scales"), py::arg("v_codes"), py::arg("v_scales"), py::arg("k"),
+             py::arg("v"), py::arg("positions").none(true), py::arg("slots"), py::arg("cos_sin").none(true), py::kw_only(),
+             py::arg("q") = py::none(), py::arg("q_out") = py::none(), py::arg("style") = (int)LS_ROPE_HALF,
+             "Codes: uint8 [n_pages, n_kv_heads, page_size, head_dim / 2] (4 bits) or float8_e4m3fn [.., head_dim]; scales: uint8 "
+             "[.., ceil(head_dim / 32)]; each pair of the same strides in any order.  The rest as in ls_kv_append, of the type of k.")
+        .def("ls_kvq_read", &Ops::kvq_read, py::arg("k_codes"), py::arg("k_scales"), py::arg("v_codes"), py::arg("v_scales"), py::arg("slots"),
+             py::arg("k"), py::arg("v"), "slots: int32 [T]; k, v: [T, n_kv_heads, head_dim], written.")
+        .def("ls_kvq_attend", &Ops::kvq_attend, py::arg("q"), py::arg("k_codes"), py::arg("k_scales"), py::arg("v_codes"), py::arg("v_scales"),
+             py::arg("pages").none(true), py::arg("lens"), py::arg("out"), py::kw_only(), py::arg("max_len"), py::arg("scale"),
+             py::arg("n_q") = 1, py::arg("prefix_pages") = py::none(), py::arg("prefix_len") = 0, "As ls_attend, of the type of q.")
+        .def("ls_verify", &Ops::verify, py::arg("target"), py::arg("drafts"), py::arg("accept"), py::arg("sample"), py::arg("tokens"),
+             py::arg("n_accepted"), py::kw_only(), py::arg("draft") = py::none(), py::arg("n_drafts") = py::none(),
+             "target: [n_seqs, n_drafts + 1, vocab]; draft: [n_seqs, n_drafts, vocab] or None; drafts: int32 [n_seqs, n_drafts]; accept: fp32 "
+             "[n_seqs, n_drafts]; sample: fp32 [n_seqs]; tokens: int32 [n_seqs, n_drafts + 1] and n_accepted: int32 [n_seqs], written; "
+             "n_drafts: int32 [n_seqs], drafts of each sequence, or None.");
 }

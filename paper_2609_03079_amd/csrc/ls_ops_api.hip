@@ -4,6 +4,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <new>
+#include <utility>
 
 #include "ls_ops_internal.h"
 
@@ -56,10 +57,8 @@ bool element_aligned(const void* p, ls_dtype t) { return ls::aligned(p, ls::type
         if (!(cond)) return fail(c, LS_E_INVAL, __VA_ARGS__);      \
     } while (0)
 
-ls_status check_cache(ls_ops* c, const ls_kv_cache* kv) {
-    LS_REQUIRE(kv, "cache is NULL");
-    LS_REQUIRE(kv->k && kv->v, "cache: k or v is NULL");
-    LS_REQUIRE(is_float(kv->dtype), "cache: bad dtype");
+// What a cache of either kind has to be.
+ls_status check_pages(ls_ops* c, const ls_kv_cache* kv) {
     LS_REQUIRE(kv->n_pages >= 1, "cache: n_pages must be >= 1");
     LS_REQUIRE(kv->page_size >= 1 && kv->page_size <= 4096 && !(kv->page_size & (kv->page_size - 1)),
                "cache: page_size must be a power of two in 1..4096");
@@ -67,7 +66,97 @@ ls_status check_cache(ls_ops* c, const ls_kv_cache* kv) {
     LS_REQUIRE(kv->n_kv_heads >= 1 && kv->n_kv_heads <= 4096, "cache: n_kv_heads must be in 1..4096");
     LS_REQUIRE(kv->head_dim >= 1 && kv->head_dim <= 1024, "cache: head_dim must be in 1..1024");
     LS_REQUIRE(kv->page_stride >= 0 && kv->head_stride >= 0 && kv->token_stride >= 0, "cache: negative stride");
+    return LS_OK;
+}
+
+ls_status check_cache(ls_ops* c, const ls_kv_cache* kv) {
+    LS_REQUIRE(kv, "cache is NULL");
+    LS_REQUIRE(kv->k && kv->v, "cache: k or v is NULL");
+    LS_REQUIRE(is_float(kv->dtype), "cache: bad dtype");
+    const ls_status st = check_pages(c, kv);
+    if (st != LS_OK) return st;
     LS_REQUIRE(element_aligned(kv->k, kv->dtype) && element_aligned(kv->v, kv->dtype), "cache: k or v is not aligned to its type");
+    return LS_OK;
+}
+
+ls_status check_kvq(ls_ops* c, const ls_kvq_cache* kv, ls_dtype type) {
+    LS_REQUIRE(kv, "cache is NULL");
+    LS_REQUIRE(kv->k && kv->v && kv->k_scale && kv->v_scale, "cache: k, v or their scales are NULL");
+    LS_REQUIRE(kv->code == LS_FP4 || kv->code == LS_FP8, "cache: code must be LS_FP4 or LS_FP8");
+    LS_REQUIRE(is_float(type), "bad type");
+    const ls_kv_cache shape = ls::shape_of(*kv, type);
+    const ls_status st = check_pages(c, &shape);
+    if (st != LS_OK) return st;
+    LS_REQUIRE(kv->head_dim % 8 == 0, "cache: head_dim must be a multiple of 8");
+    LS_REQUIRE(kv->scale_page_stride >= 0 && kv->scale_head_stride >= 0 && kv->scale_token_stride >= 0, "cache: negative stride of the scales");
+    const int64_t eight = kv->code == LS_FP4 ? 4 : 8;  // bytes of eight codes
+    LS_REQUIRE(ls::aligned(kv->k, eight) && ls::aligned(kv->v, eight) && kv->page_stride % eight == 0 && kv->head_stride % eight == 0 &&
+                   kv->token_stride % eight == 0,
+               "cache: codes and their strides must be multiples of %d bytes", (int)eight);
+    return LS_OK;
+}
+
+ls_status check_append(ls_ops* c, int head_dim, ls_dtype type, const ls_append_args* a) {
+    LS_REQUIRE(a, "args is NULL");
+    LS_REQUIRE(a->n_tokens >= 0, "n_tokens must be >= 0");
+    LS_REQUIRE(a->n_heads >= 0 && a->n_heads <= 4096, "n_heads must be in 0..4096");
+    LS_REQUIRE(a->rot_dim >= 0 && a->rot_dim % 2 == 0 && a->rot_dim <= head_dim, "rot_dim must be even and at most head_dim");
+    LS_REQUIRE(a->style == LS_ROPE_HALF || a->style == LS_ROPE_PAIR, "bad style");
+    LS_REQUIRE(a->n_tokens == 0 || ((a->q != nullptr) == (a->n_heads > 0) && (a->q_out != nullptr) == (a->n_heads > 0)),
+               "q and q_out go with n_heads > 0, and only with it");
+    if (a->n_tokens == 0) return LS_OK;
+    LS_REQUIRE(a->k && a->v && a->slots, "k, v or slots is NULL");
+    LS_REQUIRE(a->rot_dim == 0 || (a->positions && a->cos_sin && a->n_pos >= 1), "a rotation needs positions and cos_sin of n_pos >= 1 rows");
+    for (int64_t s : {a->k_token_stride, a->k_head_stride, a->v_token_stride, a->v_head_stride, a->q_token_stride, a->q_head_stride,
+                      a->q_out_token_stride, a->q_out_head_stride})
+        LS_REQUIRE(s >= 0, "negative stride");
+    LS_REQUIRE(element_aligned(a->k, type) && element_aligned(a->v, type) && element_aligned(a->q, type) &&
+                   element_aligned(a->q_out, type) && ls::aligned(a->positions, 4) && ls::aligned(a->slots, 4) && ls::aligned(a->cos_sin, 4),
+               "a pointer is not aligned to its type");
+    return LS_OK;
+}
+
+ls_status check_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a, const char* no_f32) {
+    LS_REQUIRE(a, "args is NULL");
+    if (kv->dtype == LS_F32) return fail(c, LS_E_UNSUPPORTED, "%s", no_f32);
+    LS_REQUIRE(kv->head_dim % 8 == 0 && kv->head_dim <= 256, "head_dim must be a multiple of 8, at most 256");
+    LS_REQUIRE(a->n_seqs >= 0, "n_seqs must be >= 0");
+    LS_REQUIRE(a->n_q >= 1 && a->n_q <= 16, "n_q must be in 1..16");
+    LS_REQUIRE(a->n_heads >= 1 && a->n_heads <= 4096 && a->n_heads % kv->n_kv_heads == 0, "n_heads must be a multiple of n_kv_heads, at most 4096");
+    LS_REQUIRE(a->prefix_len >= 0 && a->prefix_len < 1 << 22 && a->max_len >= 0 && a->max_len < 1 << 22,
+               "prefix_len and max_len must be in 0..2^22 - 1");
+    LS_REQUIRE(std::isfinite(a->scale) && a->scale > 0.f, "scale must be finite and > 0");
+    if (a->n_seqs == 0) return LS_OK;
+    LS_REQUIRE(a->q && a->out && a->lens, "q, out or lens is NULL");
+    LS_REQUIRE(a->prefix_len == 0 || a->prefix_pages, "prefix_pages is NULL");
+    LS_REQUIRE(a->max_len == 0 || a->pages, "pages is NULL");
+    LS_REQUIRE(a->max_len == 0 || (a->pages_stride >= 1 && a->pages_stride >= ls::ceil_div(a->max_len, kv->page_size)),
+               "pages_stride pages hold fewer than max_len keys");
+    for (int64_t s : {a->q_token_stride, a->q_head_stride, a->out_token_stride, a->out_head_stride})
+        LS_REQUIRE(s >= 0 && s % 8 == 0, "strides must be multiples of 8 elements");
+    LS_REQUIRE(ls::aligned(a->q, 16) && ls::aligned(a->out, 16), "q, out, k and v must be 16-byte aligned");
+    LS_REQUIRE(ls::aligned(a->prefix_pages, 4) && ls::aligned(a->pages, 4) && ls::aligned(a->lens, 4), "a pointer is not aligned to its type");
+    return LS_OK;
+}
+
+// Launches an attention that was found right, in as many pieces as it takes.
+template <typename Launch>
+ls_status attend_pieces(ls_ops* c, const ls_kv_cache& kv, const ls_attend_args* a, const char* what, Launch launch) {
+    ls_status st;
+    // A launch holds fewer than 2^32 threads: more rows than 2^20 (at most 2^21 workgroups for a part) are taken in pieces.
+    const int64_t piece = std::max<int64_t>(1, (1 << 20) / ((int64_t)a->n_q * a->n_heads)), es = (int64_t)ls::type_size(kv.dtype);
+    for (int64_t s = 0; s < a->n_seqs; s += piece) {
+        ls_attend_args b = *a;
+        b.n_seqs = (int32_t)std::min<int64_t>(piece, a->n_seqs - s);
+        b.q = static_cast<const char*>(a->q) + s * a->n_q * a->q_token_stride * es;
+        b.out = static_cast<char*>(a->out) + s * a->n_q * a->out_token_stride * es;
+        if (b.pages) b.pages += s * a->pages_stride;
+        b.lens += s;
+        ls::AttendPlan plan;
+        if (!ls::plan_attend(kv, b, c->ws_bytes, c->n_cu, &plan))
+            return fail(c, LS_E_CAPACITY, "the partial results do not fit the workspace of %zu bytes", c->ws_bytes);
+        if ((st = launched(c, launch(b, plan), what)) != LS_OK) return st;
+    }
     return LS_OK;
 }
 
@@ -174,22 +263,7 @@ ls_status ls_kv_append(ls_ops* c, const ls_kv_cache* kv, const ls_append_args* a
     ls_status st = check_ctx(c);
     if (st != LS_OK) return st;
     if ((st = check_cache(c, kv)) != LS_OK) return st;
-    LS_REQUIRE(a, "args is NULL");
-    LS_REQUIRE(a->n_tokens >= 0, "n_tokens must be >= 0");
-    LS_REQUIRE(a->n_heads >= 0 && a->n_heads <= 4096, "n_heads must be in 0..4096");
-    LS_REQUIRE(a->rot_dim >= 0 && a->rot_dim % 2 == 0 && a->rot_dim <= kv->head_dim, "rot_dim must be even and at most head_dim");
-    LS_REQUIRE(a->style == LS_ROPE_HALF || a->style == LS_ROPE_PAIR, "bad style");
-    LS_REQUIRE(a->n_tokens == 0 || ((a->q != nullptr) == (a->n_heads > 0) && (a->q_out != nullptr) == (a->n_heads > 0)),
-               "q and q_out go with n_heads > 0, and only with it");
-    if (a->n_tokens == 0) return LS_OK;
-    LS_REQUIRE(a->k && a->v && a->slots, "k, v or slots is NULL");
-    LS_REQUIRE(a->rot_dim == 0 || (a->positions && a->cos_sin && a->n_pos >= 1), "a rotation needs positions and cos_sin of n_pos >= 1 rows");
-    for (int64_t s : {a->k_token_stride, a->k_head_stride, a->v_token_stride, a->v_head_stride, a->q_token_stride, a->q_head_stride,
-                      a->q_out_token_stride, a->q_out_head_stride})
-        LS_REQUIRE(s >= 0, "negative stride");
-    LS_REQUIRE(element_aligned(a->k, kv->dtype) && element_aligned(a->v, kv->dtype) && element_aligned(a->q, kv->dtype) &&
-                   element_aligned(a->q_out, kv->dtype) && ls::aligned(a->positions, 4) && ls::aligned(a->slots, 4) && ls::aligned(a->cos_sin, 4),
-               "a pointer is not aligned to its type");
+    if ((st = check_append(c, kv->head_dim, kv->dtype, a)) != LS_OK || a->n_tokens == 0) return st;
     return launched(c, ls::launch_append(*kv, *a, c->stream), "ls_kv_append");
 }
 
@@ -197,42 +271,67 @@ ls_status ls_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a) {
     ls_status st = check_ctx(c);
     if (st != LS_OK) return st;
     if ((st = check_cache(c, kv)) != LS_OK) return st;
+    if ((st = check_attend(c, kv, a, "ls_attend takes f16 and bf16 caches")) != LS_OK || a->n_seqs == 0) return st;
+    for (int64_t s : {kv->page_stride, kv->head_stride, kv->token_stride}) LS_REQUIRE(s % 8 == 0, "strides must be multiples of 8 elements");
+    LS_REQUIRE(ls::aligned(kv->k, 16) && ls::aligned(kv->v, 16), "q, out, k and v must be 16-byte aligned");
+    return attend_pieces(c, *kv, a, "ls_attend", [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
+        return ls::launch_attend(*kv, b, plan, c->ws, c->stream);
+    });
+}
+
+ls_status ls_kvq_append(ls_ops* c, const ls_kvq_cache* kv, ls_dtype type, const ls_append_args* a) {
+    ls_status st = check_ctx(c);
+    if (st != LS_OK) return st;
+    if ((st = check_kvq(c, kv, type)) != LS_OK) return st;
+    if ((st = check_append(c, kv->head_dim, type, a)) != LS_OK || a->n_tokens == 0) return st;
+    return launched(c, ls::launch_kvq_append(*kv, type, *a, c->stream), "ls_kvq_append");
+}
+
+ls_status ls_kvq_read(ls_ops* c, const ls_kvq_cache* kv, const ls_kvq_read_args* a) {
+    ls_status st = check_ctx(c);
+    if (st != LS_OK) return st;
     LS_REQUIRE(a, "args is NULL");
-    if (kv->dtype == LS_F32) return fail(c, LS_E_UNSUPPORTED, "ls_attend takes f16 and bf16 caches");
-    LS_REQUIRE(kv->head_dim % 8 == 0 && kv->head_dim <= 256, "head_dim must be a multiple of 8, at most 256");
+    if ((st = check_kvq(c, kv, a->type)) != LS_OK) return st;
+    LS_REQUIRE(a->n_tokens >= 0, "n_tokens must be >= 0");
+    if (a->n_tokens == 0) return LS_OK;
+    LS_REQUIRE(a->k && a->v && a->slots, "k, v or slots is NULL");
+    for (int64_t s : {a->k_token_stride, a->k_head_stride, a->v_token_stride, a->v_head_stride}) LS_REQUIRE(s >= 0, "negative stride");
+    for (const auto& x : {std::make_pair(a->k_token_stride, a->k_head_stride), std::make_pair(a->v_token_stride, a->v_head_stride)})
+        LS_REQUIRE((kv->n_kv_heads == 1 || x.second >= kv->head_dim) && (a->n_tokens == 1 || x.first >= kv->head_dim), "k or v: rows overlap");
+    LS_REQUIRE(element_aligned(a->k, a->type) && element_aligned(a->v, a->type) && ls::aligned(a->slots, 4), "a pointer is not aligned to its type");
+    return launched(c, ls::launch_kvq_read(*kv, *a, c->stream), "ls_kvq_read");
+}
+
+ls_status ls_kvq_attend(ls_ops* c, const ls_kvq_cache* kv, ls_dtype type, const ls_attend_args* a) {
+    ls_status st = check_ctx(c);
+    if (st != LS_OK) return st;
+    if ((st = check_kvq(c, kv, type)) != LS_OK) return st;
+    const ls_kv_cache shape = ls::shape_of(*kv, type);
+    if ((st = check_attend(c, &shape, a, "ls_kvq_attend takes f16 and bf16 queries")) != LS_OK || a->n_seqs == 0) return st;
+    return attend_pieces(c, shape, a, "ls_kvq_attend", [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
+        return kv->code == LS_FP4 ? ls::launch_attend_fp4(*kv, type, b, plan, c->ws, c->stream)
+                                  : ls::launch_attend_fp8(*kv, type, b, plan, c->ws, c->stream);
+    });
+}
+
+ls_status ls_verify(ls_ops* c, const ls_verify_args* a) {
+    ls_status st = check_ctx(c);
+    if (st != LS_OK) return st;
+    LS_REQUIRE(a, "args is NULL");
+    LS_REQUIRE(is_float(a->type), "bad type");
     LS_REQUIRE(a->n_seqs >= 0, "n_seqs must be >= 0");
-    LS_REQUIRE(a->n_q >= 1 && a->n_q <= 16, "n_q must be in 1..16");
-    LS_REQUIRE(a->n_heads >= 1 && a->n_heads <= 4096 && a->n_heads % kv->n_kv_heads == 0, "n_heads must be a multiple of n_kv_heads, at most 4096");
-    LS_REQUIRE(a->prefix_len >= 0 && a->prefix_len < 1 << 22 && a->max_len >= 0 && a->max_len < 1 << 22,
-               "prefix_len and max_len must be in 0..2^22 - 1");
-    LS_REQUIRE(std::isfinite(a->scale) && a->scale > 0.f, "scale must be finite and > 0");
+    LS_REQUIRE(a->n_drafts >= 0 && a->n_drafts <= 63, "n_drafts must be in 0..63");
+    LS_REQUIRE(a->vocab >= 1, "vocab must be >= 1");
     if (a->n_seqs == 0) return LS_OK;
-    LS_REQUIRE(a->q && a->out && a->lens, "q, out or lens is NULL");
-    LS_REQUIRE(a->prefix_len == 0 || a->prefix_pages, "prefix_pages is NULL");
-    LS_REQUIRE(a->max_len == 0 || a->pages, "pages is NULL");
-    LS_REQUIRE(a->max_len == 0 || (a->pages_stride >= 1 && a->pages_stride >= ls::ceil_div(a->max_len, kv->page_size)),
-               "pages_stride pages hold fewer than max_len keys");
-    for (int64_t s : {a->q_token_stride, a->q_head_stride, a->out_token_stride, a->out_head_stride, kv->page_stride, kv->head_stride,
-                      kv->token_stride})
-        LS_REQUIRE(s >= 0 && s % 8 == 0, "strides must be multiples of 8 elements");
-    LS_REQUIRE(ls::aligned(a->q, 16) && ls::aligned(a->out, 16) && ls::aligned(kv->k, 16) && ls::aligned(kv->v, 16),
-               "q, out, k and v must be 16-byte aligned");
-    LS_REQUIRE(ls::aligned(a->prefix_pages, 4) && ls::aligned(a->pages, 4) && ls::aligned(a->lens, 4), "a pointer is not aligned to its type");
-    // A launch holds fewer than 2^32 threads: more rows than 2^20 (at most 2^21 workgroups for a part) are taken in pieces.
-    const int64_t piece = std::max<int64_t>(1, (1 << 20) / ((int64_t)a->n_q * a->n_heads)), es = (int64_t)ls::type_size(kv->dtype);
-    for (int64_t s = 0; s < a->n_seqs; s += piece) {
-        ls_attend_args b = *a;
-        b.n_seqs = (int32_t)std::min<int64_t>(piece, a->n_seqs - s);
-        b.q = static_cast<const char*>(a->q) + s * a->n_q * a->q_token_stride * es;
-        b.out = static_cast<char*>(a->out) + s * a->n_q * a->out_token_stride * es;
-        if (b.pages) b.pages += s * a->pages_stride;
-        b.lens += s;
-        ls::AttendPlan plan;
-        if (!ls::plan_attend(*kv, b, c->ws_bytes, c->n_cu, &plan))
-            return fail(c, LS_E_CAPACITY, "the partial results do not fit the workspace of %zu bytes", c->ws_bytes);
-        if ((st = launched(c, ls::launch_attend(*kv, b, plan, c->ws, c->stream), "ls_attend")) != LS_OK) return st;
-    }
-    return LS_OK;
+    LS_REQUIRE(a->target && a->sample && a->tokens && a->n_accepted, "target, sample, tokens or n_accepted is NULL");
+    LS_REQUIRE(a->n_drafts == 0 || (a->drafts && a->accept), "drafts or accept is NULL");
+    for (int64_t s : {a->target_seq_stride, a->target_token_stride, a->draft_seq_stride, a->draft_token_stride, a->drafts_stride, a->accept_stride})
+        LS_REQUIRE(s >= 0, "negative stride");
+    LS_REQUIRE(a->n_seqs == 1 || a->tokens_stride > a->n_drafts, "tokens_stride is shorter than a row");
+    LS_REQUIRE(element_aligned(a->target, a->type) && element_aligned(a->draft, a->type) && ls::aligned(a->drafts, 4) && ls::aligned(a->counts, 4) &&
+                   ls::aligned(a->accept, 4) && ls::aligned(a->sample, 4) && ls::aligned(a->tokens, 4) && ls::aligned(a->n_accepted, 4),
+               "a pointer is not aligned to its type");
+    return launched(c, ls::launch_verify(*a, c->ws, c->ws_bytes, c->n_cu, c->stream), "ls_verify");
 }
 
 }  // extern "C"

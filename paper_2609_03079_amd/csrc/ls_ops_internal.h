@@ -36,6 +36,21 @@ bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes,
 hipError_t launch_attend(const ls_kv_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws,
                          hipStream_t st);
 
+// ---- a cache in 4 or 8 bits (ls_kvq.hip, ls_attend_fp4.hip, ls_attend_fp8.hip) -----------------
+hipError_t launch_kvq_append(const ls_kvq_cache& c, ls_dtype type, const ls_append_args& a, hipStream_t st);
+hipError_t launch_kvq_read(const ls_kvq_cache& c, const ls_kvq_read_args& a, hipStream_t st);
+hipError_t launch_attend_fp4(const ls_kvq_cache& c, ls_dtype type, const ls_attend_args& a, const AttendPlan& plan, void* ws,
+                             hipStream_t st);
+hipError_t launch_attend_fp8(const ls_kvq_cache& c, ls_dtype type, const ls_attend_args& a, const AttendPlan& plan, void* ws,
+                             hipStream_t st);
+// The shape of a quantised cache, its codes' places and strides in bytes, for the calls that take either.
+inline ls_kv_cache shape_of(const ls_kvq_cache& c, ls_dtype type) {
+    return {c.k, c.v, type, c.n_pages, c.page_size, c.n_kv_heads, c.head_dim, c.page_stride, c.head_stride, c.token_stride};
+}
+
+// ---- drafted tokens (ls_verify.hip) --------------------------------------------------------
+hipError_t launch_verify(const ls_verify_args& a, void* ws, size_t ws_bytes, int n_cu, hipStream_t st);
+
 // ---- elements ------------------------------------------------------------------------------
 // V elements moved as one access of up to 16 bytes.
 template <typename T, int V>
