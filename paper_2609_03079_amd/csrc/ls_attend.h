@@ -92,6 +92,7 @@ struct AttendP {
     const uint8_t* k_scale;  // codes only
     const uint8_t* v_scale;
     int64_t s_page, s_head, s_token;
+    bool rows16;             // rows of codes are whole chunks of 16 bytes, and aligned to them
     int n_pages, page_shift;
     const int32_t* prefix_pages;
     const int32_t* pages;
@@ -138,20 +139,26 @@ struct Whole {
     static constexpr int kBits = 16;
 };
 
-// How a wave takes the codes of its rows: each lane kInstr pieces of kBytes of one row, piece i PPR + sub of it, where
-// sub is the lane's place among the PPR lanes of that row.
+// Codes in shared memory: rows of kRowBytes, in chunks of 16 bytes.
 template <class C, typename T, int DP, bool WIDE>
-struct Pieces {
-    static constexpr int PPR = 64 / Shape<T, DP, WIDE>::kRows;
-    static constexpr int kLane = DP * C::kBits / 8 / PPR;  // bytes of a lane
-    static constexpr int kBytes = kLane < 16 ? kLane : 16, kInstr = kLane / kBytes;
-    static constexpr int kElems = kBytes * 8 / C::kBits, kWords = kBytes / 4;
-    static constexpr int kWord8 = C::kBits / 4;  // words of eight elements
+struct Raw {
+    static constexpr int kRows = Shape<T, DP, WIDE>::kRows;      // rows a wave copies
+    static constexpr int kRowBytes = DP * C::kBits / 8, CR = kRowBytes / 16;
+    static constexpr int kElems = 128 / C::kBits;                // elements of a chunk
+    static constexpr int RPI = 64 / CR;                          // rows per copy instruction
+    static constexpr int kInstr = kRows > RPI ? kRows / RPI : 1;
+    static constexpr int kOf8 = C::kBits / 4;                    // words of eight elements
+    // Narrow: a lane reads half a row's chunks, of whole groups: chunk i of its own is chunk_of(i, half) of the row.
+    static constexpr int kOwn = CR / 2, kPerGroup = kGroup / kElems, kScales = DP / 64;
+    __device__ static constexpr int chunk_of(int i, int half) { return (i / kPerGroup * 2 + half) * kPerGroup + i % kPerGroup; }
+    // Rows lie with their chunks permuted, so that eight lanes that read a chunk of eight rows meet in no bank.
+    __device__ static constexpr int swz(int row) { return (row / (CR < 16 ? 16 / CR : 1)) & (CR - 1); }
 };
-template <class C, typename T, int DP, bool WIDE>
-struct Held {
-    uint32_t w[Pieces<C, T, DP, WIDE>::kInstr][Pieces<C, T, DP, WIDE>::kWords];
-    uint32_t scale[Pieces<C, T, DP, WIDE>::kInstr];
+// Scale bytes of a tile, as they are loaded: a lane waits for them where it uses them.
+template <int N>
+struct Scales {
+    uint8_t b[N];
+    bool there[N];  // false: a masked row's, nothing
 };
 
 // The value of lane ^ 32.
@@ -210,8 +217,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     constexpr bool PIPE = WIDE && !MULTI;  // scores one tile ahead (MULTI's rare path leaves no registers)
     constexpr int NW = Sh::NW, KT = Sh::KT, CPR = Sh::CPR, NF = DP / 16, ND = DP / 32, SUB = KT / 32;
     constexpr bool CODES = C::kBits < 16, DIRECT = CODES && !WIDE;
-    using Pc = Pieces<C, T, DP, WIDE>;
-    using Codes = Held<C, T, DP, WIDE>;
+    using R = Raw<C, T, DP, WIDE>;
     Item it;
     if (!item_of<Sh::kTileRows>(p, prefix, b, &it)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -247,8 +253,8 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         const T* src = static_cast<const T*>(p.q) + token * p.q_token + head * p.q_head;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
-            // DIRECT: the order in which this half's lanes hold a key's pieces
-            const int d = DIRECT ? (f * 8 / Pc::kElems * 2 + h) * Pc::kElems + f * 8 % Pc::kElems : f * 16 + h * 8;
+            // DIRECT: the order in which this half's lanes read a key's chunks
+            const int d = DIRECT ? R::chunk_of(f * 8 / R::kElems, h) * R::kElems + f * 8 % R::kElems : f * 16 + h * 8;
             q[f] = row_ok && d < p.D ? *reinterpret_cast<const vec8<T>*>(src + d) : vec8<T>{};
         }
     }
@@ -273,51 +279,42 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     auto scale_place = [&](int key0, int id) {
         return CODES ? (int64_t)id * p.s_page + (int64_t)((key0 + (lane & (KT - 1))) & page_mask) * p.s_token + it.kv * p.s_head : 0;
     };
-    // Codes and scales of this lane's pieces of a tile's rows.  What is masked or past a row is read as zeros.
-    const bool pieces = CODES && p.D % Pc::kElems == 0;
-    auto fetch = [&](const uint8_t* codes, const uint8_t* scales, int64_t at, int64_t s_at, Codes& x) {
-        const int sub = WIDE ? lane % Pc::PPR : h;
-        if (WIDE) {
-            const int r = wave * Sh::kRows + lane / Pc::PPR;  // this lane's row, looked up by lane r
-            at = (int64_t)(((uint64_t)__shfl((uint32_t)(at >> 32), r, 64) << 32) | __shfl((uint32_t)at, r, 64));
-            s_at = (int64_t)(((uint64_t)__shfl((uint32_t)(s_at >> 32), r, 64) << 32) | __shfl((uint32_t)s_at, r, 64));
-        }
+    // Copies the codes of this wave's rows of a tile to shared memory, RPI rows an instruction (or, where rows are no
+    // multiple of 16 bytes, a word a lane): lane -> row lane / CR, chunk lane % CR, permuted for DIRECT.  What is
+    // masked or past a row's end comes from the row of zeros.
+    // The value at lane r of a 64-bit number.
+    auto of_lane = [&](int64_t x, int r) {
+        return (int64_t)(((uint64_t)__shfl((uint32_t)(x >> 32), r, 64) << 32) | __shfl((uint32_t)x, r, 64));
+    };
+    auto copy_codes = [&](const Elem* base, int64_t at, uint8_t* to) {
+        const uint8_t* codes = reinterpret_cast<const uint8_t*>(base);
         const uint8_t* none = reinterpret_cast<const uint8_t*>(g_zero_row);
+        const int first = WIDE ? wave * R::kRows : 0;
+        if (p.rows16) {
 #pragma unroll
-        for (int i = 0; i < Pc::kInstr; ++i) {
-            const int piece = i * Pc::PPR + sub, e = piece * Pc::kElems;
-            const bool there = at >= 0 && e < p.D;
-            const uint8_t* from = there ? codes + at + piece * Pc::kBytes : none;
-            if (pieces) {
-                if constexpr (Pc::kWords == 4) {
-                    const u32x4a v = *reinterpret_cast<const u32x4a*>(from);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x.w[i][j] = v[j];
-                } else {
-                    const u32x2a v = *reinterpret_cast<const u32x2a*>(from);
-                    x.w[i][0] = v[0], x.w[i][1] = v[1];
-                }
-            } else {  // a row ends inside a piece
-#pragma unroll
-                for (int j = 0; j < Pc::kWords; ++j)
-                    x.w[i][j] = *reinterpret_cast<const uint32_t*>(there && e + j * (32 / C::kBits) < p.D ? from + 4 * j : none);
+            for (int i = 0; i < R::kInstr; ++i) {
+                const int r = i * R::RPI + lane / R::CR, chunk = (lane % R::CR) ^ (DIRECT ? R::swz(r) : 0);
+                const int64_t row = of_lane(at, (first + r) & (KT - 1));
+                const bool there = row >= 0 && chunk * R::kElems < p.D;
+                if (R::kRows >= R::RPI || r < R::kRows)
+                    __builtin_amdgcn_global_load_lds((gptr)(there ? codes + row + chunk * 16 : none), (lptr)(to + i * 1024), 16, 0, 0);
             }
-            x.scale[i] = *(there ? scales + s_at + e / kGroup : none);
+        } else {
+#pragma unroll
+            for (int i = 0; i < R::kRows * R::CR / 16; ++i) {
+                const int g = i * 64 + lane, r = g / (R::CR * 4);
+                const int word = ((g / 4 % R::CR) ^ (DIRECT ? R::swz(r) : 0)) * 4 + g % 4;
+                const int64_t row = of_lane(at, first + r);
+                const bool there = row >= 0 && word * (32 / C::kBits) < p.D;
+                __builtin_amdgcn_global_load_lds((gptr)(there ? codes + row + word * 4 : none), (lptr)(to + i * 256), 4, 0, 0);
+            }
         }
     };
-    // They widened into a tile in shared memory, where the 16-bit copies would lie.
-    auto put_tile = [&](const Codes& x, T* buf) {
-        const int sub = WIDE ? lane % Pc::PPR : h, r = WIDE ? wave * Sh::kRows + lane / Pc::PPR : n;
-        T* row = buf + (WIDE ? r : wave * KT + r) * DP;
-#pragma unroll
-        for (int i = 0; i < Pc::kInstr; ++i)
-#pragma unroll
-            for (int j = 0; j < Pc::kElems / 8; ++j) {
-                vec8<T> v;
-                widen8<C, T>(&x.w[i][j * Pc::kWord8], scale_of(x.scale[i]), &v);
-                const int chunk = (i * Pc::PPR + sub) * (Pc::kElems / 8) + j;
-                *reinterpret_cast<vec8<T>*>(row + (chunk ^ swz<CPR>(r)) * 8) = v;
-            }
+    // Eight elements of a lane's codes.
+    auto widen = [&](const uint32_t* w, uint8_t scale, bool there) {
+        vec8<T> v;
+        widen8<C, T>(w, scale_of(there ? scale : 0), &v);
+        return v;
     };
     // Copies a tile's rows, RPI of them an instruction: lane -> row lane / CPR, chunk lane % CPR permuted.
     // 16 rows that are all there lie in one page (of 16 keys or more): one address for the wave and
@@ -388,28 +385,85 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
                 s.u[u] = mma(*reinterpret_cast<const vec8<T>*>(kt + (k_at ^ (f * 16)) + u * 32 * DP), q[f], s.u[u]);
         return s;
     };
-    // DIRECT: each lane widens half of a key's row to its operands.
-    auto scores_of = [&](const Codes& x) {
+    // DIRECT: the scales of half of this lane's key, its codes widened to operands, its value's put where
+    // the second product reads them.  The codes are the wave's own, and so are the values.
+    using Own = Scales<R::kScales>;
+    auto own_scales = [&](const uint8_t* scales, int64_t at, int64_t s_at, Own& x) {
+        const uint8_t* row = scales + (at >= 0 ? s_at : 0);  // of a masked key: some scale, which is not used
+#pragma unroll
+        for (int i = 0; i < R::kScales; ++i) {
+            const int g = 2 * i + h;
+            x.b[i] = row[g * kGroup < p.D ? g : 0];
+            x.there[i] = at >= 0;
+        }
+    };
+    auto own_chunk = [&](const uint8_t* rows, int i) {
+        return *reinterpret_cast<const u32x4*>(rows + n * R::kRowBytes + ((R::chunk_of(i, h) ^ R::swz(n)) * 16));
+    };
+    auto scores_of = [&](const uint8_t* rows, const Own& x) {
         Scores s;
         s.u[0] = f32x16{};
 #pragma unroll
-        for (int i = 0; i < Pc::kInstr; ++i)
+        for (int i = 0; i < R::kOwn; ++i) {
+            const u32x4 c = own_chunk(rows, i);
+            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-            for (int j = 0; j < Pc::kElems / 8; ++j) {
-                vec8<T> v;
-                widen8<C, T>(&x.w[i][j * Pc::kWord8], scale_of(x.scale[i]), &v);
-                s.u[0] = mma(v, q[i * (Pc::kElems / 8) + j], s.u[0]);
-            }
+            for (int j = 0; j < R::kElems / 8; ++j)
+                s.u[0] = mma(widen(w + j * R::kOf8, x.b[i / R::kPerGroup], x.there[i / R::kPerGroup]), q[i * (R::kElems / 8) + j], s.u[0]);
+        }
         return s;
+    };
+    auto put_values = [&](const uint8_t* rows, const Own& x, T* vt) {
+#pragma unroll
+        for (int i = 0; i < R::kOwn; ++i) {
+            const u32x4 c = own_chunk(rows, i);
+            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int j = 0; j < R::kElems / 8; ++j) {
+                const int chunk = R::chunk_of(i, h) * (R::kElems / 8) + j;
+                *reinterpret_cast<vec8<T>*>(vt + n * DP + (chunk ^ swz<CPR>(n)) * 8) =
+                    widen(w + j * R::kOf8, x.b[i / R::kPerGroup], x.there[i / R::kPerGroup]);
+            }
+        }
+    };
+    // WIDE: the scales of what this lane copied; the codes in the last part of the wave's rows of a tile, all of them read, then
+    // widened into these rows.
+    using Copied = Scales<R::kInstr>;
+    auto copied_scales = [&](const uint8_t* scales, int64_t at, int64_t s_at, Copied& x) {
+#pragma unroll
+        for (int i = 0; i < R::kInstr; ++i) {
+            const int r = (wave * R::kRows + i * R::RPI + lane / R::CR) & (KT - 1), e = lane % R::CR * R::kElems;
+            const int64_t row = of_lane(at, r), s = of_lane(s_at, r);
+            x.b[i] = scales[(row >= 0 ? s : 0) + (e < p.D ? e / kGroup : 0)];
+            x.there[i] = row >= 0;
+        }
+    };
+    constexpr int kRawAt = R::kRows * DP * (int)sizeof(T) - R::kRows * R::kRowBytes;  // bytes into the wave's rows
+    auto raw_of = [&](T* buf) { return reinterpret_cast<uint8_t*>(buf + wave * R::kRows * DP) + kRawAt; };
+    auto spread = [&](T* buf, const Copied& x) {
+        if (R::kRows < R::RPI && lane / R::CR >= R::kRows) return;
+        u32x4 c[R::kInstr];
+#pragma unroll
+        for (int i = 0; i < R::kInstr; ++i) c[i] = *reinterpret_cast<const u32x4*>(raw_of(buf) + i * 1024 + lane * 16);
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // read by every lane before one of them writes there (vmcnt and expcnt untouched)
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+#pragma unroll
+        for (int i = 0; i < R::kInstr; ++i) {
+            const int r = wave * R::kRows + i * R::RPI + lane / R::CR;
+            const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+            for (int j = 0; j < R::kElems / 8; ++j) {
+                const int chunk = lane % R::CR * (R::kElems / 8) + j;
+                *reinterpret_cast<vec8<T>*>(buf + r * DP + (chunk ^ swz<CPR>(r)) * 8) = widen(w + j * R::kOf8, x.b[i], x.there[i]);
+            }
+        }
     };
     // One tile.  PIPE: its scores are in s already, and those of the next tile (keys in kbuf) are
     // computed while its exponentials are: matrix and vector instructions of one wave run side by
     // side, so the next maximum is part of the same stretch of code.
-    auto use = [&](Scores& s, int key0, int64_t at, T* vbuf, const T* kbuf, const Codes* kx, const Codes* vx) {
+    auto use = [&](Scores& s, int key0, int64_t at, const T* vbuf, const T* kbuf) {
         if constexpr (DIRECT) {
-            s = scores_of(*kx);
-            largest(s);
-            put_tile(*vx, vbuf);  // the wave's own rows: its reads follow its writes
+            largest(s);  // the scores are there
         } else if (!PIPE) {
             s = scores(kbuf);
             largest(s);
@@ -508,64 +562,93 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
     };
 
-    const uint8_t* ks = p.k_scale;
-    const uint8_t* vs = p.v_scale;
     if constexpr (DIRECT) {
-        // While tile j is used, the codes of j + 1 arrive in registers.
+        // The codes of two tiles are on their way while one is used, in two shares of shared memory: those of tile j + 2 are
+        // asked for once tile j's are operands.
         if (key < it.end) {
-            int64_t at0 = place(key, first0), at1 = place(key + kStep, first1), s_at1 = scale_place(key + kStep, first1);
+            int64_t at0 = place(key, first0), at1 = place(key + kStep, first1);
+            constexpr int kHalf = KT * R::kRowBytes, kCopies = 2 * R::kInstr;
+            uint8_t* c0 = reinterpret_cast<uint8_t*>(k0) + wave * 2 * kHalf;
+            uint8_t* c1 = reinterpret_cast<uint8_t*>(k1) + wave * 2 * kHalf;
+            T* vt = v0 + wave * KT * DP;
+            Own kx0, vx0, kx1, vx1;
             Scores s;
-            Codes ka, va, kb, vb;
-            fetch(kbase, ks, at0, scale_place(key, first0), ka);
-            fetch(vbase, vs, at0, scale_place(key, first0), va);
-            auto tile = [&](Codes& k_now, Codes& v_now, Codes& k_next, Codes& v_next) {
+            auto ask = [&](int64_t at, int64_t s_at, uint8_t* c, Own& kx, Own& vx) {
+                own_scales(p.k_scale, at, s_at, kx);
+                own_scales(p.v_scale, at, s_at, vx);
+                __atomic_signal_fence(__ATOMIC_SEQ_CST);
+                copy_codes(kbase, at, c);
+                copy_codes(vbase, at, c + kHalf);
+            };
+            ask(at0, scale_place(key, first0), c0, kx0, vx0);
+            ask(at1, scale_place(key + kStep, first1), c1, kx1, vx1);
+            auto tile = [&](uint8_t* c, Own& kx, Own& vx) {
+                // the copies of this tile are done: only those of the next one, asked for after them, may not be
+                if (p.rows16)
+                    __builtin_amdgcn_s_waitcnt(0x0f70 | (kCopies & 15) | (kCopies >> 4) << 14);
+                else
+                    __builtin_amdgcn_s_waitcnt(0x0f70);
+                __atomic_signal_fence(__ATOMIC_SEQ_CST);
+                s = scores_of(c, kx);
+                put_values(c + kHalf, vx, vt);
                 const int64_t at2 = place(key + 2 * kStep, id2), s_at2 = scale_place(key + 2 * kStep, id2);
-                id2 = page_id(key + 3 * kStep);
-                if (key + kStep < it.end) {
-                    fetch(kbase, ks, at1, s_at1, k_next);
-                    fetch(vbase, vs, at1, s_at1, v_next);
-                }
-                use(s, key, at0, v0, nullptr, &k_now, &v_now);
+                __builtin_amdgcn_s_waitcnt(0xc07f);  // its codes have been read
+                __atomic_signal_fence(__ATOMIC_SEQ_CST);
+                id2 = page_id(key + 3 * kStep);  // before the copies: whoever waits for it does not wait for them
+                ask(at2, s_at2, c, kx, vx);
+                use(s, key, at0, v0, nullptr);
                 key += kStep;
-                at0 = at1, at1 = at2, s_at1 = s_at2;
+                at0 = at1, at1 = at2;
             };
             for (;;) {
-                tile(ka, va, kb, vb);
+                tile(c0, kx0, vx0);
                 if (key >= it.end) break;
-                tile(kb, vb, ka, va);
+                tile(c1, kx1, vx1);
                 if (key >= it.end) break;
             }
+            landed();  // nothing is under way when the arrays are used again
         }
     } else if constexpr (CODES) {
-        // As below, the codes on their way in registers while a tile is used, widened into the other buffers after that.
+        // As below; the codes are copied to the end of the rows that they become while a tile is used, and spread after it.
         if (key < it.end) {
             int64_t at0 = place(key, first0), at1 = place(key + kStep, first1), s_at1 = scale_place(key + kStep, first1);
-            Codes kx, vx;
+            Copied kx, vx;
             Scores s;
-            fetch(kbase, ks, at0, scale_place(key, first0), kx);
-            fetch(vbase, vs, at0, scale_place(key, first0), vx);
-            put_tile(kx, k0);
-            put_tile(vx, v0);
+            auto ask = [&](const Elem* base, const uint8_t* scales, int64_t at, int64_t s_at, T* buf, Copied& x) {
+                copied_scales(scales, at, s_at, x);
+                copy_codes(base, at, raw_of(buf));
+            };
+            auto arrived = [&] {
+                __builtin_amdgcn_s_waitcnt(0x0f70);
+                __atomic_signal_fence(__ATOMIC_SEQ_CST);
+            };
+            ask(kbase, p.k_scale, at0, scale_place(key, first0), k0, kx);
+            ask(vbase, p.v_scale, at0, scale_place(key, first0), v0, vx);
+            arrived();
+            spread(k0, kx);
+            spread(v0, vx);
             if (PIPE) {
-                fetch(kbase, ks, at1, s_at1, kx);
-                put_tile(kx, k1);
+                ask(kbase, p.k_scale, at1, s_at1, k1, kx);
+                arrived();
+                spread(k1, kx);
                 landed();
                 s = scores(k0);
                 largest(s);
             }
-            auto tile = [&](T* ka, T* kb, T* va, T* vb) {
+            auto tile = [&](T* ka, T* kb, T* va, T* vb) {  // as below
                 const int64_t at2 = place(key + 2 * kStep, id2), s_at2 = scale_place(key + 2 * kStep, id2);
                 landed();
                 id2 = page_id(key + 3 * kStep);
                 const bool more = PIPE || key + kStep < it.end;
                 if (more) {
-                    fetch(kbase, ks, PIPE ? at2 : at1, PIPE ? s_at2 : s_at1, kx);
-                    fetch(vbase, vs, at1, s_at1, vx);
+                    ask(kbase, p.k_scale, PIPE ? at2 : at1, PIPE ? s_at2 : s_at1, PIPE ? ka : kb, kx);
+                    ask(vbase, p.v_scale, at1, s_at1, vb, vx);
                 }
-                if (!idle_wave) use(s, key, at0, va, PIPE ? kb : ka, nullptr, nullptr);
+                if (!idle_wave) use(s, key, at0, va, PIPE ? kb : ka);
                 if (more) {
-                    put_tile(kx, PIPE ? ka : kb);
-                    put_tile(vx, vb);
+                    arrived();
+                    spread(PIPE ? ka : kb, kx);
+                    spread(vb, vx);
                 }
                 key += kStep;
                 at0 = at1, at1 = at2, s_at1 = s_at2;
@@ -599,7 +682,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
                 copy(kbase, PIPE ? at2 : at1, PIPE ? ka : kb);
                 copy(vbase, at1, vb);
             }
-            if (!idle_wave) use(s, key, at0, va, PIPE ? kb : ka, nullptr, nullptr);
+            if (!idle_wave) use(s, key, at0, va, PIPE ? kb : ka);
             key += kStep;
             at0 = at1, at1 = at2;
         };
@@ -662,6 +745,36 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         const float wl = wave_ml[w][1][n];
         if (wl != 0.f) sum += wl * __builtin_amdgcn_exp2f(wave_ml[w][0][n] - base);
     }
+    if constexpr (DIRECT) {
+        // the second wave's sums through the values' array, to be added by the first, lane by lane
+        static_assert(NW == 2 && Sh::kBuf * sizeof(T) >= ND * 16 * 64 * 4, "room for a wave's sums");
+        const float scale = __builtin_amdgcn_exp2f(m - base);
+        f32x4* sums = reinterpret_cast<f32x4*>(v0) + lane;
+        if (wave == 1) {
+#pragma unroll
+            for (int t = 0; t < ND; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : o[t][i + e] * scale;
+                    sums[(t * 4 + i / 4) * 64] = v;
+                }
+        }
+        __syncthreads();
+        if (wave == 1 || !row_ok) return;
+#pragma unroll
+        for (int t = 0; t < ND; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                f32x4 v = sums[(t * 4 + i / 4) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += l == 0.f ? 0.f : o[t][i + e] * scale;
+                put(token, head, t * 32 + 2 * i + 4 * h, v, sum);
+            }
+        if (h == 0) put_ml(top, sum);
+        return;
+    }
     // [wave][row][DP], 16-byte chunks permuted by the row: half of each row in the keys' array, half in the values'
     static_assert(WIDE || Sh::kBuf * sizeof(T) >= NW * 32 * DP / 2 * 4, "room for the waves' sums");
     auto joined = [&](int w, int r, int chunk) {
@@ -702,12 +815,13 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
 enum Roles { NARROW, WIDE_ROWS, BOTH };
 
 template <typename T, int DP, Roles ROLES, bool MULTI, class C>
-__global__ __launch_bounds__((Shape<T, DP, ROLES != NARROW>::NW * 64), (ROLES != NARROW && DP <= 128 && (ROLES == BOTH || !MULTI) ? 2 : 1)) void attend_kernel(const AttendP p) {
+__global__ __launch_bounds__((Shape<T, DP, ROLES != NARROW>::NW * 64), (ROLES == NARROW ? (C::kBits < 16 && DP <= 128 && !MULTI ? 2 : 1) : DP <= 128 && (ROLES == BOTH || !MULTI) ? 2 : 1)) void attend_kernel(const AttendP p) {
     constexpr int kBuf = ROLES == WIDE_ROWS ? Shape<T, DP, true>::kBuf : Shape<T, DP, false>::kBuf;
     static_assert(Shape<T, DP, false>::kBuf >= Shape<T, DP, true>::kBuf, "room for either shape");
-    // narrow workgroups on codes: a tile of values a wave, and as much again for the waves' sums
-    constexpr int kSecond = ROLES == NARROW && C::kBits < 16 ? 1 : kBuf;
-    __shared__ __attribute__((aligned(16))) T k0[kBuf], k1[kSecond], v0[kBuf], v1[kSecond];
+    // narrow workgroups on codes: two tiles of codes, keys and values, and a tile of values for each wave
+    constexpr bool kCodes = ROLES == NARROW && C::kBits < 16;
+    constexpr int kKeys = kCodes ? kBuf * 2 * C::kBits / 16 : kBuf;
+    __shared__ __attribute__((aligned(16))) T k0[kKeys], k1[kKeys], v0[kBuf], v1[kCodes ? 1 : kBuf];
     __shared__ float wave_ml[Shape<T, DP, false>::NW][2][32], row_sum[32];
     int b = blockIdx.x;
     if constexpr (ROLES == BOTH) {
@@ -826,6 +940,9 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_kvq_cache* codes, const ls
     p.page_stride = c.page_stride, p.head_stride = c.head_stride, p.token_stride = c.token_stride;
     if (codes) {
         p.k_scale = codes->k_scale, p.v_scale = codes->v_scale;
+        const int64_t row = (int64_t)c.head_dim * C::kBits / 8;
+        p.rows16 = row % 16 == 0 && aligned(c.k, 16) && aligned(c.v, 16) && c.page_stride % 16 == 0 && c.head_stride % 16 == 0 &&
+                   c.token_stride % 16 == 0;
         p.s_page = codes->scale_page_stride, p.s_head = codes->scale_head_stride, p.s_token = codes->scale_token_stride;
     }
     p.n_pages = c.n_pages, p.page_shift = __builtin_ctz(c.page_size);
