@@ -264,7 +264,7 @@ ls_status ls_kvq_attend(ls_ops* ctx, const ls_kvq_cache* cache, ls_dtype type, c
  * NULL: q is one at the drafted token (a draft without chance).  drafts: int32 [n_seqs, n_drafts]; counts: int32 [n_seqs] or NULL:
  * sequence s has min(counts[s], n_drafts) drafts; below 0 it is an idle slot: tokens -1, n_accepted -1.
  * accept: fp32 [n_seqs, n_drafts]; sample: fp32 [n_seqs]; tokens: int32 [n_seqs, n_drafts + 1]; n_accepted: int32 [n_seqs]; all on the device.
- * 0 <= n_drafts <= 63 (0: tokens drawn from p); vocab >= 1; n_seqs 0 does nothing. */
+ * 0 <= n_drafts <= 63 (0: tokens drawn from p); 1 <= vocab <= 2^30; n_seqs 0 does nothing. */
 typedef struct {
     int32_t n_seqs, n_drafts, vocab;
     ls_dtype type;

@@ -3,7 +3,7 @@
 
 namespace ls {
 
-bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan) {
+bool plan_attend(const ls_kv_cache& c, int bits, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan) {
     const int G = a.n_heads / c.n_kv_heads;
     const int64_t pre_rows = (int64_t)a.n_seqs * a.n_q * G, suf_rows = (int64_t)a.n_q * G;
     const int64_t part_bytes = (int64_t)a.n_seqs * a.n_q * a.n_heads * (c.head_dim + 2) * 4;
@@ -17,7 +17,7 @@ bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes,
     enum Kind { NARROW_ITEM, WIDE_ITEM, TOKENS_ITEM };
     const Kind pre_kind = plan->pre_wide ? WIDE_ITEM : NARROW_ITEM;
     const Kind suf_kind = !plan->suf_wide ? NARROW_ITEM : a.n_q > 1 && a.max_len ? TOKENS_ITEM : WIDE_ITEM;
-    const int wide_cu = c.head_dim <= 128 ? 2 : 1, narrow_cu = c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 2 : 1;
+    const int wide_cu = c.head_dim <= 128 ? 2 : 1, narrow_cu = bits < 16 ? (c.head_dim <= 128 ? 4 : 2) : c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 2 : 1;
     const double by_dim = (c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256) / 128.0;
     const double tokens_key = c.head_dim <= 64 ? 0.024 : c.head_dim <= 128 ? 0.038 : 0.139;
     auto item_us = [&](Kind kind, int64_t chunk) {

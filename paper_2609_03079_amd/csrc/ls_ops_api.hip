@@ -141,7 +141,7 @@ ls_status check_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a
 
 // Launches an attention that was found right, in as many pieces as it takes.
 template <typename Launch>
-ls_status attend_pieces(ls_ops* c, const ls_kv_cache& kv, const ls_attend_args* a, const char* what, Launch launch) {
+ls_status attend_pieces(ls_ops* c, const ls_kv_cache& kv, int bits, const ls_attend_args* a, const char* what, Launch launch) {
     ls_status st;
     // A launch holds fewer than 2^32 threads: more rows than 2^20 (at most 2^21 workgroups for a part) are taken in pieces.
     const int64_t piece = std::max<int64_t>(1, (1 << 20) / ((int64_t)a->n_q * a->n_heads)), es = (int64_t)ls::type_size(kv.dtype);
@@ -153,7 +153,7 @@ ls_status attend_pieces(ls_ops* c, const ls_kv_cache& kv, const ls_attend_args* 
         if (b.pages) b.pages += s * a->pages_stride;
         b.lens += s;
         ls::AttendPlan plan;
-        if (!ls::plan_attend(kv, b, c->ws_bytes, c->n_cu, &plan))
+        if (!ls::plan_attend(kv, bits, b, c->ws_bytes, c->n_cu, &plan))
             return fail(c, LS_E_CAPACITY, "the partial results do not fit the workspace of %zu bytes", c->ws_bytes);
         if ((st = launched(c, launch(b, plan), what)) != LS_OK) return st;
     }
@@ -274,7 +274,7 @@ ls_status ls_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a) {
     if ((st = check_attend(c, kv, a, "ls_attend takes f16 and bf16 caches")) != LS_OK || a->n_seqs == 0) return st;
     for (int64_t s : {kv->page_stride, kv->head_stride, kv->token_stride}) LS_REQUIRE(s % 8 == 0, "strides must be multiples of 8 elements");
     LS_REQUIRE(ls::aligned(kv->k, 16) && ls::aligned(kv->v, 16), "q, out, k and v must be 16-byte aligned");
-    return attend_pieces(c, *kv, a, "ls_attend", [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
+    return attend_pieces(c, *kv, 16, a, "ls_attend", [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
         return ls::launch_attend(*kv, b, plan, c->ws, c->stream);
     });
 }
@@ -308,7 +308,7 @@ ls_status ls_kvq_attend(ls_ops* c, const ls_kvq_cache* kv, ls_dtype type, const 
     if ((st = check_kvq(c, kv, type)) != LS_OK) return st;
     const ls_kv_cache shape = ls::shape_of(*kv, type);
     if ((st = check_attend(c, &shape, a, "ls_kvq_attend takes f16 and bf16 queries")) != LS_OK || a->n_seqs == 0) return st;
-    return attend_pieces(c, shape, a, "ls_kvq_attend", [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
+    return attend_pieces(c, shape, kv->code == LS_FP4 ? 4 : 8, a, "ls_kvq_attend", [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
         return kv->code == LS_FP4 ? ls::launch_attend_fp4(*kv, type, b, plan, c->ws, c->stream)
                                   : ls::launch_attend_fp8(*kv, type, b, plan, c->ws, c->stream);
     });
@@ -321,7 +321,7 @@ ls_status ls_verify(ls_ops* c, const ls_verify_args* a) {
     LS_REQUIRE(is_float(a->type), "bad type");
     LS_REQUIRE(a->n_seqs >= 0, "n_seqs must be >= 0");
     LS_REQUIRE(a->n_drafts >= 0 && a->n_drafts <= 63, "n_drafts must be in 0..63");
-    LS_REQUIRE(a->vocab >= 1, "vocab must be >= 1");
+    LS_REQUIRE(a->vocab >= 1 && a->vocab <= 1 << 30, "vocab must be in 1..2^30");
     if (a->n_seqs == 0) return LS_OK;
     LS_REQUIRE(a->target && a->sample && a->tokens && a->n_accepted, "target, sample, tokens or n_accepted is NULL");
     LS_REQUIRE(a->n_drafts == 0 || (a->drafts && a->accept), "drafts or accept is NULL");

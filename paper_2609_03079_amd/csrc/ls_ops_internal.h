@@ -31,8 +31,9 @@ struct AttendPlan {
     bool alike;                           // prefix and sequences by the same kernel, in one launch
     bool together;                        // a wide prefix and narrow sequences in one launch
 };
-// For at most 2^20 rows n_seqs n_q n_heads, or one sequence.  False where no split fits the workspace.
-bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan);
+// For at most 2^20 rows n_seqs n_q n_heads, or one sequence; bits: those of an element in the cache.  False where no split
+// fits the workspace.
+bool plan_attend(const ls_kv_cache& c, int bits, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan);
 hipError_t launch_attend(const ls_kv_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws,
                          hipStream_t st);
 
