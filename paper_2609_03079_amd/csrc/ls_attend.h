@@ -66,6 +66,12 @@ __device__ inline f32x16 mma(const f16x8& a, const f16x8& b, const f32x16& c) {
 __device__ inline f32x16 mma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
+__device__ inline f32x4 mma16(const f16x8& a, const f16x8& b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x4 mma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
 
 // Quotients of 0 <= n < 2^31 by a number the host knows: a product and a shift.
 struct Div {
@@ -165,6 +171,31 @@ struct Scales {
 __device__ inline float other_half(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// Of this lane's value and that of lane ^ D (16 or 32): the same in both.
+template <int D>
+__device__ inline void both_of(float v, float* a, float* b) {
+    const uint32_t x = __float_as_uint(v);
+    if constexpr (D == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        *a = __uint_as_float(r[0]), *b = __uint_as_float(r[1]);
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        *a = __uint_as_float(r[0]), *b = __uint_as_float(r[1]);
+    }
+}
+template <int D>
+__device__ inline float pair_max(float v) {
+    float a, b;
+    both_of<D>(v, &a, &b);
+    return fmaxf(a, b);
+}
+template <int D>
+__device__ inline float pair_sum(float v) {
+    float a, b;
+    both_of<D>(v, &a, &b);
+    return a + b;
 }
 
 // What a workgroup works on.
@@ -810,18 +841,304 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     }
 }
 
-// Which shapes a launch holds.  BOTH: a wide prefix beside narrow sequences, eight workgroups of one after
-// eight of the other (one for each XCD).
-enum Roles { NARROW, WIDE_ROWS, BOTH };
+// Up to 16 rows over codes.  The products run on the 16 x 16 x 32 instructions: half the scores, sums and
+// query operands a lane of the narrow shape, which leaves registers for three waves a SIMD (and the codes need no shared memory on
+// their way).  A lane takes a quarter of a key's row, straight from the cache: key n of the first 16 of a tile and of the
+// second, elements g DP / 4 and on; its scores are those of keys 16 t + 4 g + i and query row n.
+template <typename T, int DP, bool MULTI, class C>
+__device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b, T* v0, float (*wave_ml)[2][32]) {
+    using Sh = Shape<T, DP, false>;
+    constexpr int NW = Sh::NW, KT = 32, kStep = NW * KT, CPR = DP / 8, NF = DP / 32, ND = DP / 16;
+    constexpr int kOwn = DP / 4, kWords = kOwn * C::kBits / 32, kOf8 = C::kBits / 4, kScales = kOwn > kGroup ? kOwn / kGroup : 1;
+    Item it;
+    if (!item_of<16>(p, prefix, b, &it)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, g = lane >> 4;
+
+    int key = it.begin + wave * KT;
+    auto page_id = [&](int key0, int t) {
+        const int at = key0 + t * 16 + n;
+        return at < it.end ? it.table[at >> p.page_shift] : -1;
+    };
+    int ids0[2] = {page_id(key, 0), page_id(key, 1)}, ids1[2] = {page_id(key + kStep, 0), page_id(key + kStep, 1)};
+    it.len = it.seq < 0 ? p.prefix_len : min(p.lens[it.seq], p.max_len);
+    it.end = min(it.end, it.len);
+    if (it.begin >= it.end && !p.direct) return;
+
+    const int row = it.row0 + n;
+    const bool row_ok = row < it.rows;
+    const int rr = row_ok ? row : it.rows - 1;
+    const int tk = p.by_G.of(rr), head = it.kv * p.G + rr - tk * p.G;
+    const int64_t token = it.seq < 0 ? tk : (int64_t)it.seq * p.n_q + tk;
+    const int limit = it.seq < 0 ? it.end : min(it.end, it.len - p.n_q + 1 + tk);
+    const int full_len = it.seq < 0 ? it.end : it.len - p.n_q + 1, full = min(it.end, full_len);
+
+    vec8<T> q[NF];
+    {
+        const T* src = static_cast<const T*>(p.q) + token * p.q_token + head * p.q_head;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            const int d = g * kOwn + f * 8;
+            q[f] = row_ok && d < p.D ? *reinterpret_cast<const vec8<T>*>(src + d) : vec8<T>{};
+        }
+    }
+    f32x4 o[ND];
+#pragma unroll
+    for (auto& x : o) x = f32x4{};
+    float m = -INFINITY, l = 0.f;
+
+    const uint8_t* kbase = static_cast<const uint8_t*>(p.k) + it.kv * p.head_stride;
+    const uint8_t* vbase = static_cast<const uint8_t*>(p.v) + it.kv * p.head_stride;
+    const uint8_t* ksbase = p.k_scale + it.kv * p.s_head;
+    const uint8_t* vsbase = p.v_scale + it.kv * p.s_head;
+    const int page_mask = (1 << p.page_shift) - 1;
+    const bool whole = p.D % kOwn == 0;  // no row ends inside a lane's share
+
+    struct Codes {
+        uint32_t k[2][kWords], v[2][kWords];
+        uint8_t ks[2][kScales], vs[2][kScales];  // bytes as they are loaded: a lane waits for them where it uses them
+        bool there[2];
+    };
+    // A lane's codes and scales of a tile.  A masked key's are those of the cache's first row (`clear` makes zeros of them), so that
+    // there is nothing but loads here: a choice between these and zeros becomes branches that wait for what they have loaded.
+    // What is past a row's end is its start once more: it meets zeros of the query, or becomes columns that are not written.
+    auto fetch = [&](int key0, const int (&ids)[2], Codes& x) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int at = key0 + t * 16 + n;
+            x.there[t] = (unsigned)ids[t] < (unsigned)p.n_pages && at < it.end;
+            const int64_t id = x.there[t] ? ids[t] : 0, place = x.there[t] ? at & page_mask : 0;
+            const int64_t c_at = id * p.page_stride + place * p.token_stride, s_at = id * p.s_page + place * p.s_token;
+            const int e = g * kOwn;
+#pragma unroll
+            for (int i = 0; i < kScales; ++i) {
+                const int of = e + i * kGroup < p.D ? (e + i * kGroup) / kGroup : 0;
+                x.ks[t][i] = ksbase[s_at + of];
+                x.vs[t][i] = vsbase[s_at + of];
+            }
+            if (whole) {
+                const int64_t of = c_at + (e < p.D ? e * C::kBits / 8 : 0);
+                auto take = [&](const uint8_t* from, uint32_t (&w)[kWords]) {
+                    if constexpr (kWords == 2) {
+                        const u32x2a v = *reinterpret_cast<const u32x2a*>(from);
+                        w[0] = v[0], w[1] = v[1];
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kWords; i += 4) {
+                            const u32x4a v = *reinterpret_cast<const u32x4a*>(from + i * 4);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) w[i + j] = v[j];
+                        }
+                    }
+                };
+                take(kbase + of, x.k[t]);
+                take(vbase + of, x.v[t]);
+            } else {
+                int dim = p.D;
+                asm volatile("" : "+s"(dim));  // places computed anew for each tile: kept, they take registers that the loop needs
+#pragma unroll
+                for (int j = 0; j < kWords; ++j) {
+                    const int w = e + j * (32 / C::kBits);
+                    const int64_t of = c_at + (w < dim ? w * C::kBits / 8 : 0);
+                    x.k[t][j] = *reinterpret_cast<const uint32_t*>(kbase + of);
+                    x.v[t][j] = *reinterpret_cast<const uint32_t*>(vbase + of);
+                }
+            }
+        }
+    };
+    auto widen = [&](const uint32_t* w, uint8_t scale) {
+        vec8<T> v;
+        widen8<C, T>(w, scale_of(scale), &v);
+        return v;
+    };
+    T* vt = v0 + wave * KT * DP;
+    const int r4 = (lane & 15) >> 2, row_a = 4 * g + r4;
+    const int v_at = row_a * DP + (((lane & 3) >> 1) ^ swz<CPR>(row_a)) * 8 + (lane & 1) * 4;
+    const int v_at16 = (row_a + 16) * DP + (((lane & 3) >> 1) ^ swz<CPR>(row_a + 16)) * 8 + (lane & 1) * 4;
+
+    auto use = [&](Codes& x, int key0) {
+        const uint32_t valid = ((uint32_t)__ballot(x.there[0]) & 0xffff) | (uint32_t)__ballot(x.there[1]) << 16;
+        const bool some = key0 + KT > full || ~valid != 0;  // keys that not every row sees
+        if (~valid != 0) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int j = 0; j < kWords; ++j) x.k[t][j] = x.there[t] ? x.k[t][j] : 0, x.v[t][j] = x.there[t] ? x.v[t][j] : 0;
+#pragma unroll
+                for (int i = 0; i < kScales; ++i) x.ks[t][i] = x.there[t] ? x.ks[t][i] : 0, x.vs[t][i] = x.there[t] ? x.vs[t][i] : 0;
+            }
+        }
+        f32x4 s[2] = {f32x4{}, f32x4{}};
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) s[t] = mma16(widen(&x.k[t][f * kOf8], x.ks[t][f * 8 / kGroup]), q[f], s[t]);
+        if (some) {
+            const int left = limit - key0;
+            const uint32_t below = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1, seen = (below & valid) >> (4 * g);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[t][i] = (seen >> (16 * t + i)) & 1 ? s[t][i] : -INFINITY;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                const int r = t * 16 + n, chunk = g * (kOwn / 8) + f;
+                *reinterpret_cast<vec8<T>*>(vt + r * DP + (chunk ^ swz<CPR>(r)) * 8) = widen(&x.v[t][f * kOf8], x.vs[t][f * 8 / kGroup]);
+            }
+        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        top = pair_max<16>(top);
+        top = pair_max<32>(top);
+        const float next = fmaxf(m, top * p.c - Sh::kLift), base = next == -INFINITY ? 0.f : next;
+        if (__any(next > m)) {
+            const float scale = __builtin_amdgcn_exp2f(m - base);  // m = -inf: 0
+            l *= scale;
+#pragma unroll
+            for (auto& y : o) y *= scale;
+            m = next;
+        }
+        vec8<T> pr;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[t][i], p.c, -base));
+                l += e;
+                pr[4 * t + i] = (T)e;
+            }
+        auto value = [&](int d) {
+            typedef __attribute__((address_space(3))) s16x4* lds4;
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vt + (v_at ^ (d * 16))));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vt + (v_at16 ^ (d * 16))));
+            struct { s16x4 a, b; } both{a, b};
+            return __builtin_bit_cast(vec8<T>, both);
+        };
+        bool odd = false;
+        if (MULTI && it.seq >= 0 && key0 + KT > full) {  // as above: a weight of zero must keep out a value that is no number
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const auto v = value(d);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) odd |= key0 + 16 * (j / 4) + 4 * g + j % 4 >= full && !(fabsf((float)v[j]) < INFINITY);
+            }
+        }
+        if (MULTI && __any(odd)) {
+#pragma unroll 1
+            for (int i = 0; i < p.n_q; ++i) {
+                const int seen = full_len + i;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    auto v = value(d);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (key0 + 16 * (j / 4) + 4 * g + j % 4 >= seen) v[j] = (T)0.f;
+                    const f32x4 y = mma16(v, pr, o[d]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[d][e] = tk == i ? y[e] : o[d][e];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int d = 0; d < ND; ++d) o[d] = mma16(value(d), pr, o[d]);
+        }
+    };
+    // While a tile is used, the codes of the next are on their way, and the page ids of the one behind it.
+    if (key < it.end) {
+        Codes a, b;
+        fetch(key, ids0, a);
+        auto tile = [&](Codes& now, Codes& next) {
+            const int ids2[2] = {page_id(key + 2 * kStep, 0), page_id(key + 2 * kStep, 1)};
+            fetch(key + kStep, ids1, next);  // (past the end: the cache's first row)
+            use(now, key);
+            key += kStep;
+            ids1[0] = ids2[0], ids1[1] = ids2[1];
+        };
+        for (;;) {
+            tile(a, b);
+            if (key >= it.end) break;
+            tile(b, a);
+            if (key >= it.end) break;
+        }
+    }
+    l = pair_sum<32>(pair_sum<16>(l));
+
+    // the waves' results joined: the second's sums through the values' array, to be added by the first, lane by lane
+    if (g == 0) {
+        wave_ml[wave][0][n] = m;
+        wave_ml[wave][1][n] = l;
+    }
+    __syncthreads();
+    const float top = fmaxf(wave_ml[0][0][n], wave_ml[1][0][n]), base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const float wl = wave_ml[w][1][n];
+        if (wl != 0.f) sum += wl * __builtin_amdgcn_exp2f(wave_ml[w][0][n] - base);
+    }
+    static_assert(NW == 2 && Sh::kBuf * sizeof(T) >= ND * 64 * 16, "room for a wave's sums");
+    const float scale = __builtin_amdgcn_exp2f(m - base);
+    f32x4* sums = reinterpret_cast<f32x4*>(v0) + lane;
+    if (wave == 1) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : o[d][e] * scale;
+            sums[d * 64] = v;
+        }
+    }
+    __syncthreads();
+    if (wave == 1 || !row_ok) return;
+    const int64_t out_row = token * p.H + head;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+        const int e0 = d * 16 + 4 * g;
+        f32x4 v = sums[d * 64];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += l == 0.f ? 0.f : o[d][e] * scale;
+        if (e0 >= p.D) continue;
+        if (p.direct) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            Pack<T, 4> y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y.e[e] = (T)(v[e] * inv);
+            store_pack<T, 4>(p.out, token * p.o_token + head * p.o_head + e0, y);
+        } else {
+            *reinterpret_cast<f32x4*>(p.part + (out_row * p.parts + it.part) * p.D + e0) = v;
+        }
+    }
+    if (g == 0 && !p.direct) {
+        float* at = p.ml + (out_row * p.parts + it.part) * 2;
+        at[0] = top;
+        at[1] = sum;
+    }
+}
+
+// Which shapes a launch holds.  BOTH: a wide prefix beside narrow (of codes: thin) sequences, eight workgroups of one after
+// eight of the other (one for each XCD).  THIN: codes only.
+enum Roles { NARROW, WIDE_ROWS, BOTH, THIN };
+
+// Waves a SIMD that the registers are shared out for.
+template <int DP, Roles ROLES, bool MULTI, class C>
+constexpr int waves_of() {
+    if (ROLES == THIN) return DP <= 64 ? (C::kBits == 4 && !MULTI ? 4 : 3) : DP <= 128 ? (C::kBits == 4 && !MULTI ? 3 : 2) : 1;
+    if (ROLES == NARROW) return C::kBits < 16 && DP <= 128 && !MULTI ? 2 : 1;
+    return DP <= 128 && (ROLES == BOTH || !MULTI) ? 2 : 1;
+}
+template <typename T, int DP, Roles ROLES>
+constexpr int threads_of = Shape<T, DP, ROLES == WIDE_ROWS || ROLES == BOTH>::NW * 64;
 
 template <typename T, int DP, Roles ROLES, bool MULTI, class C>
-__global__ __launch_bounds__((Shape<T, DP, ROLES != NARROW>::NW * 64), (ROLES == NARROW ? (C::kBits < 16 && DP <= 128 && !MULTI ? 2 : 1) : DP <= 128 && (ROLES == BOTH || !MULTI) ? 2 : 1)) void attend_kernel(const AttendP p) {
+__global__ __launch_bounds__((threads_of<T, DP, ROLES>), (waves_of<DP, ROLES, MULTI, C>())) void attend_kernel(const AttendP p) {
+    constexpr bool kCodes = C::kBits < 16;
     constexpr int kBuf = ROLES == WIDE_ROWS ? Shape<T, DP, true>::kBuf : Shape<T, DP, false>::kBuf;
     static_assert(Shape<T, DP, false>::kBuf >= Shape<T, DP, true>::kBuf, "room for either shape");
-    // narrow workgroups on codes: two tiles of codes, keys and values, and a tile of values for each wave
-    constexpr bool kCodes = ROLES == NARROW && C::kBits < 16;
-    constexpr int kKeys = kCodes ? kBuf * 2 * C::kBits / 16 : kBuf;
-    __shared__ __attribute__((aligned(16))) T k0[kKeys], k1[kKeys], v0[kBuf], v1[kCodes ? 1 : kBuf];
+    // narrow workgroups on codes: two tiles of codes, keys and values, and a tile of values for each wave; thin ones: that tile
+    constexpr int kKeys = ROLES == THIN ? 1 : ROLES == NARROW && kCodes ? kBuf * 2 * C::kBits / 16 : kBuf;
+    constexpr int kMore = ROLES == THIN || (ROLES == NARROW && kCodes) ? 1 : kBuf;
+    __shared__ __attribute__((aligned(16))) T k0[kKeys], k1[kKeys], v0[kBuf], v1[kMore];
     __shared__ float wave_ml[Shape<T, DP, false>::NW][2][32], row_sum[32];
     int b = blockIdx.x;
     if constexpr (ROLES == BOTH) {
@@ -838,11 +1155,17 @@ __global__ __launch_bounds__((Shape<T, DP, ROLES != NARROW>::NW * 64), (ROLES ==
         if (prefix) {
             attend<T, DP, true, false, C>(p, true, b, k0, k1, v0, v1, wave_ml, row_sum);
         } else if (threadIdx.x < Shape<T, DP, false>::NW * 64) {
-            attend<T, DP, false, MULTI, C>(p, false, b, k0, k1, v0, v1, wave_ml, row_sum);
+            if constexpr (kCodes)
+                attend_thin<T, DP, MULTI, C>(p, false, b, v0, wave_ml);
+            else
+                attend<T, DP, false, MULTI, C>(p, false, b, k0, k1, v0, v1, wave_ml, row_sum);
         }
     } else {
         const bool prefix = b < p.pre_items;
-        attend<T, DP, ROLES == WIDE_ROWS, MULTI, C>(p, prefix, prefix ? b : b - p.pre_items, k0, k1, v0, v1, wave_ml, row_sum);
+        if constexpr (ROLES == THIN)
+            attend_thin<T, DP, MULTI, C>(p, prefix, prefix ? b : b - p.pre_items, v0, wave_ml);
+        else
+            attend<T, DP, ROLES == WIDE_ROWS, MULTI, C>(p, prefix, prefix ? b : b - p.pre_items, k0, k1, v0, v1, wave_ml, row_sum);
     }
 }
 
@@ -974,6 +1297,13 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_kvq_cache* codes, const ls
                 hipLaunchKernelGGL((attend_kernel<T, DP, WIDE_ROWS, true, C>), grid, wide_wg, 0, st, p);
             else
                 hipLaunchKernelGGL((attend_kernel<T, DP, WIDE_ROWS, false, C>), grid, wide_wg, 0, st, p);
+        } else if (roles == THIN) {
+            if constexpr (C::kBits < 16) {
+                if (multi)
+                    hipLaunchKernelGGL((attend_kernel<T, DP, THIN, true, C>), grid, narrow_wg, 0, st, p);
+                else
+                    hipLaunchKernelGGL((attend_kernel<T, DP, THIN, false, C>), grid, narrow_wg, 0, st, p);
+            }
         } else {
             if (multi)
                 hipLaunchKernelGGL((attend_kernel<T, DP, BOTH, true, C>), grid, wide_wg, 0, st, p);
@@ -982,7 +1312,8 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_kvq_cache* codes, const ls
         }
         return hipGetLastError();
     };
-    const Roles pre_role = plan.pre_wide ? WIDE_ROWS : NARROW, suf_role = plan.suf_wide ? WIDE_ROWS : NARROW;
+    const Roles pre_role = plan.pre_thin ? THIN : plan.pre_wide ? WIDE_ROWS : NARROW;
+    const Roles suf_role = plan.suf_thin ? THIN : plan.suf_wide ? WIDE_ROWS : NARROW;
     hipError_t e;
     if (pre == 0 || suf == 0 || plan.alike) {
         e = go(pre ? pre_role : suf_role, pre, suf);

@@ -12,12 +12,15 @@ bool plan_attend(const ls_kv_cache& c, int bits, const ls_attend_args& a, size_t
     plan->pre_tiles = (int)ceil_div(pre_rows, plan->pre_wide ? 128 : 32);
     plan->suf_tiles = (int)ceil_div(suf_rows, plan->suf_wide ? 128 : 32);
     plan->alike = plan->pre_wide == plan->suf_wide;
+    // up to 16 rows of codes; prefix and sequences in one launch are of one shape
+    plan->pre_thin = bits < 16 && pre_rows <= 16;
+    plan->suf_thin = bits < 16 && suf_rows <= 16 && (plan->pre_thin || plan->pre_wide || !a.prefix_len);
     // Workgroups that run at once on a compute unit (by shared memory and registers: wide ones of several tokens
     // take more than half of those); the time of a key and of a start and end, as measured with the unit full (us).
     enum Kind { NARROW_ITEM, WIDE_ITEM, TOKENS_ITEM };
     const Kind pre_kind = plan->pre_wide ? WIDE_ITEM : NARROW_ITEM;
     const Kind suf_kind = !plan->suf_wide ? NARROW_ITEM : a.n_q > 1 && a.max_len ? TOKENS_ITEM : WIDE_ITEM;
-    const int wide_cu = c.head_dim <= 128 ? 2 : 1, narrow_cu = bits < 16 ? (c.head_dim <= 128 ? 4 : 2) : c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 2 : 1;
+    const int wide_cu = c.head_dim <= 128 ? 2 : 1, narrow_cu = plan->suf_thin ? (c.head_dim <= 64 ? 6 : c.head_dim <= 128 ? (bits == 4 && a.n_q == 1 ? 6 : 4) : 2) : bits < 16 ? (c.head_dim <= 128 ? 4 : 2) : c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 2 : 1;
     const double by_dim = (c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256) / 128.0;
     const double tokens_key = c.head_dim <= 64 ? 0.024 : c.head_dim <= 128 ? 0.038 : 0.139;
     auto item_us = [&](Kind kind, int64_t chunk) {
@@ -86,7 +89,7 @@ bool plan_attend(const ls_kv_cache& c, int bits, const ls_attend_args& a, size_t
     // A wide prefix and narrow sequences in one launch where all their workgroups run at once (5 x 4 tokens
     // behind 333 keys 20.4 -> 16.3 us).  Larger ones apart: the sequences' stream through the caches takes
     // from the prefix more than running beside it gives (64 sequences behind 32768 keys 149 -> 184 us).
-    plan->together = plan->pre_parts && plan->suf_parts && plan->pre_wide && !plan->suf_wide && at_once(plan->pre_chunk, plan->suf_chunk);
+    plan->together = plan->pre_parts && plan->suf_parts && plan->pre_wide && !plan->suf_wide && (bits == 16 || plan->suf_thin) && at_once(plan->pre_chunk, plan->suf_chunk);
     return true;
 }
 

@@ -28,6 +28,7 @@ struct AttendPlan {
     int pre_chunk, pre_parts, pre_tiles;  // keys per part of the prefix, parts, row tiles
     int suf_chunk, suf_parts, suf_tiles;
     bool pre_wide, suf_wide;              // 128-row tiles instead of 32-row tiles
+    bool pre_thin, suf_thin;              // 16-row tiles (codes only; in one launch: both or, beside a wide prefix, the sequences)
     bool alike;                           // prefix and sequences by the same kernel, in one launch
     bool together;                        // a wide prefix and narrow sequences in one launch
 };
