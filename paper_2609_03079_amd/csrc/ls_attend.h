@@ -892,8 +892,6 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     const uint8_t* ksbase = p.k_scale + it.kv * p.s_head;
     const uint8_t* vsbase = p.v_scale + it.kv * p.s_head;
     const int page_mask = (1 << p.page_shift) - 1;
-    const bool whole = p.D % kOwn == 0;  // no row ends inside a lane's share
-
     struct Codes {
         uint32_t k[2][kWords], v[2][kWords];
         uint8_t ks[2][kScales], vs[2][kScales];  // bytes as they are loaded: a lane waits for them where it uses them
@@ -902,7 +900,8 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     // A lane's codes and scales of a tile.  A masked key's are those of the cache's first row (`clear` makes zeros of them), so that
     // there is nothing but loads here: a choice between these and zeros becomes branches that wait for what they have loaded.
     // What is past a row's end is its start once more: it meets zeros of the query, or becomes columns that are not written.
-    auto fetch = [&](int key0, const int (&ids)[2], Codes& x) {
+    // WHOLE: no row ends inside a lane's share.
+    auto fetch = [&](auto WHOLE, int key0, const int (&ids)[2], Codes& x) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int at = key0 + t * 16 + n;
@@ -916,7 +915,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
                 x.ks[t][i] = ksbase[s_at + of];
                 x.vs[t][i] = vsbase[s_at + of];
             }
-            if (whole) {
+            if constexpr (decltype(WHOLE)::value) {
                 const int64_t of = c_at + (e < p.D ? e * C::kBits / 8 : 0);
                 auto take = [&](const uint8_t* from, uint32_t (&w)[kWords]) {
                     if constexpr (kWords == 2) {
@@ -1045,12 +1044,13 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         }
     };
     // While a tile is used, the codes of the next are on their way, and the page ids of the one behind it.
-    if (key < it.end) {
+    // (One loop for whole shares, another for others: a branch inside would wait for the loads that each side has under way.)
+    auto run = [&](auto WHOLE) {
         Codes a, b;
-        fetch(key, ids0, a);
+        fetch(WHOLE, key, ids0, a);
         auto tile = [&](Codes& now, Codes& next) {
             const int ids2[2] = {page_id(key + 2 * kStep, 0), page_id(key + 2 * kStep, 1)};
-            fetch(key + kStep, ids1, next);  // (past the end: the cache's first row)
+            fetch(WHOLE, key + kStep, ids1, next);  // (past the end: the cache's first row)
             use(now, key);
             key += kStep;
             ids1[0] = ids2[0], ids1[1] = ids2[1];
@@ -1061,6 +1061,12 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
             tile(b, a);
             if (key >= it.end) break;
         }
+    };
+    if (key < it.end) {
+        if (p.D % kOwn == 0)
+            run(std::true_type{});
+        else
+            run(std::false_type{});
     }
     l = pair_sum<32>(pair_sum<16>(l));
 
