@@ -841,6 +841,8 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     }
 }
 
+constexpr int kThinPad = 8;  // elements
+
 // Up to 16 rows over codes.  The products run on the 16 x 16 x 32 instructions: half the scores, sums and
 // query operands a lane of the narrow shape, which leaves registers for three waves a SIMD (and the codes need no shared memory on
 // their way).  A lane takes a quarter of a key's row, straight from the cache: key n of the first 16 of a tile and of the
@@ -848,7 +850,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
 template <typename T, int DP, bool MULTI, class C>
 __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b, T* v0, float (*wave_ml)[2][32]) {
     using Sh = Shape<T, DP, false>;
-    constexpr int NW = Sh::NW, KT = 32, kStep = NW * KT, CPR = DP / 8, NF = DP / 32, ND = DP / 16;
+    constexpr int NW = Sh::NW, KT = 32, kStep = NW * KT, NF = DP / 32, ND = DP / 16;
     constexpr int kOwn = DP / 4, kWords = kOwn * C::kBits / 32, kOf8 = C::kBits / 4, kScales = kOwn > kGroup ? kOwn / kGroup : 1;
     Item it;
     if (!item_of<16>(p, prefix, b, &it)) return;
@@ -950,10 +952,12 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         widen8<C, T>(w, scale_of(scale), &v);
         return v;
     };
-    T* vt = v0 + wave * KT * DP;
-    const int r4 = (lane & 15) >> 2, row_a = 4 * g + r4;
-    const int v_at = row_a * DP + (((lane & 3) >> 1) ^ swz<CPR>(row_a)) * 8 + (lane & 1) * 4;
-    const int v_at16 = (row_a + 16) * DP + (((lane & 3) >> 1) ^ swz<CPR>(row_a + 16)) * 8 + (lane & 1) * 4;
+    // The wave's values: rows 16 bytes longer than they are, so that neither eight rows at one place (written) nor 16 rows at 32
+    // bytes (read) meet in a bank more often than their number asks, and one address serves with fixed offsets.
+    constexpr int kPitch = DP + kThinPad;
+    T* vt = v0 + wave * KT * kPitch;
+    T* v_put = vt + n * kPitch + g * kOwn;
+    const T* v_get = vt + (4 * g + ((lane & 15) >> 2)) * kPitch + (lane & 3) * 4;
 
     auto use = [&](Codes& x, int key0) {
         const uint32_t valid = ((uint32_t)__ballot(x.there[0]) & 0xffff) | (uint32_t)__ballot(x.there[1]) << 16;
@@ -983,10 +987,8 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                const int r = t * 16 + n, chunk = g * (kOwn / 8) + f;
-                *reinterpret_cast<vec8<T>*>(vt + r * DP + (chunk ^ swz<CPR>(r)) * 8) = widen(&x.v[t][f * kOf8], x.vs[t][f * 8 / kGroup]);
-            }
+            for (int f = 0; f < NF; ++f)
+                *reinterpret_cast<vec8<T>*>(v_put + t * 16 * kPitch + f * 8) = widen(&x.v[t][f * kOf8], x.vs[t][f * 8 / kGroup]);
         float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         top = pair_max<16>(top);
         top = pair_max<32>(top);
@@ -1009,8 +1011,8 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
             }
         auto value = [&](int d) {
             typedef __attribute__((address_space(3))) s16x4* lds4;
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vt + (v_at ^ (d * 16))));
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vt + (v_at16 ^ (d * 16))));
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(v_get + d * 16));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(v_get + 16 * kPitch + d * 16));
             struct { s16x4 a, b; } both{a, b};
             return __builtin_bit_cast(vec8<T>, both);
         };
@@ -1083,7 +1085,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         const float wl = wave_ml[w][1][n];
         if (wl != 0.f) sum += wl * __builtin_amdgcn_exp2f(wave_ml[w][0][n] - base);
     }
-    static_assert(NW == 2 && Sh::kBuf * sizeof(T) >= ND * 64 * 16, "room for a wave's sums");
+    static_assert(NW == 2 && NW * KT * kPitch * sizeof(T) >= ND * 64 * 16, "room for a wave's sums");
     const float scale = __builtin_amdgcn_exp2f(m - base);
     f32x4* sums = reinterpret_cast<f32x4*>(v0) + lane;
     if (wave == 1) {
@@ -1143,8 +1145,10 @@ __global__ __launch_bounds__((threads_of<T, DP, ROLES>), (waves_of<DP, ROLES, MU
     static_assert(Shape<T, DP, false>::kBuf >= Shape<T, DP, true>::kBuf, "room for either shape");
     // narrow workgroups on codes: two tiles of codes, keys and values, and a tile of values for each wave; thin ones: that tile
     constexpr int kKeys = ROLES == THIN ? 1 : ROLES == NARROW && kCodes ? kBuf * 2 * C::kBits / 16 : kBuf;
+    constexpr int kValues = kCodes && (ROLES == THIN || ROLES == BOTH) ? Shape<T, DP, false>::NW * 32 * (DP + kThinPad) : kBuf;
+    static_assert(kValues >= kBuf || ROLES == THIN, "room for a wide tile");
     constexpr int kMore = ROLES == THIN || (ROLES == NARROW && kCodes) ? 1 : kBuf;
-    __shared__ __attribute__((aligned(16))) T k0[kKeys], k1[kKeys], v0[kBuf], v1[kMore];
+    __shared__ __attribute__((aligned(16))) T k0[kKeys], k1[kKeys], v0[kValues], v1[kMore];
     __shared__ float wave_ml[Shape<T, DP, false>::NW][2][32], row_sum[32];
     int b = blockIdx.x;
     if constexpr (ROLES == BOTH) {
