@@ -841,6 +841,17 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     }
 }
 
+typedef const __attribute__((address_space(1))) uint8_t* gbyte;
+typedef const __attribute__((address_space(1))) uint32_t* gword;
+typedef const __attribute__((address_space(1))) u32x2a* gwords2;
+typedef const __attribute__((address_space(1))) u32x4a* gwords4;
+
+// An address that is the same in every lane, in scalar registers.
+__device__ inline const uint8_t* wave_address(const uint8_t* p) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uint64_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)p >> 32));
+    return reinterpret_cast<const uint8_t*>(((uint64_t)hi << 32) | lo);
+}
+
 constexpr int kThinPad = 8;  // elements
 
 // Up to 16 rows over codes.  The products run on the 16 x 16 x 32 instructions: half the scores, sums and
@@ -897,54 +908,60 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     struct Codes {
         uint32_t k[2][kWords], v[2][kWords];
         uint8_t ks[2][kScales], vs[2][kScales];  // bytes as they are loaded: a lane waits for them where it uses them
-        bool there[2];
+        uint32_t valid;                          // bit j: key j of the tile is not masked
     };
-    // A lane's codes and scales of a tile.  A masked key's are those of the cache's first row (`clear` makes zeros of them), so that
+    // A lane's codes and scales of a tile.  A masked key's are those of the cache's first rows (`use` makes zeros of them), so that
     // there is nothing but loads here: a choice between these and zeros becomes branches that wait for what they have loaded.
     // What is past a row's end is its start once more: it meets zeros of the query, or becomes columns that are not written.
-    // WHOLE: no row ends inside a lane's share.
-    auto fetch = [&](auto WHOLE, int key0, const int (&ids)[2], Codes& x) {
+    // WHOLE: no row ends inside a lane's share.  PAGED: the 16 keys of a half lie in one page, at an address that the wave
+    // shares and places that the lanes keep; otherwise each lane works out its own.
+    const int e = g * kOwn;
+    int s_of[kScales], w_of[kWords];
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) s_of[i] = e + i * kGroup < p.D ? (e + i * kGroup) / kGroup : 0;
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) {
+        const int w = e + j * (32 / C::kBits);
+        w_of[j] = w < p.D ? w * C::kBits / 8 : 0;
+    }
+    auto load = [&](auto WHOLE, auto PAGED, const uint8_t* codes, const uint8_t* scales, int64_t c_at, int64_t s_at, uint32_t (&w)[kWords],
+                    uint8_t (&s)[kScales]) {
+        const int c_n = decltype(PAGED)::value ? n * (int)p.token_stride : 0, s_n = decltype(PAGED)::value ? n * (int)p.s_token : 0;
+        const uint8_t* from = decltype(PAGED)::value ? wave_address(codes + c_at) : codes + c_at;
+        const uint8_t* s_from = decltype(PAGED)::value ? wave_address(scales + s_at) : scales + s_at;
+#pragma unroll
+        for (int i = 0; i < kScales; ++i) s[i] = *(gbyte)(s_from + (uint32_t)(s_n + s_of[i]));
+        if constexpr (!decltype(WHOLE)::value) {
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) w[j] = *(gword)(from + (uint32_t)(c_n + w_of[j]));
+        } else if constexpr (kWords == 2) {
+            const u32x2a v = *(gwords2)(from + (uint32_t)(c_n + w_of[0]));
+            w[0] = v[0], w[1] = v[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const u32x4a v = *(gwords4)(from + (uint32_t)(c_n + w_of[0]) + i * 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[i + j] = v[j];
+            }
+        }
+    };
+    auto fetch = [&](auto WHOLE, auto PAGED, int key0, const int (&ids)[2], Codes& x) {
+        x.valid = 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int at = key0 + t * 16 + n;
-            x.there[t] = (unsigned)ids[t] < (unsigned)p.n_pages && at < it.end;
-            const int64_t id = x.there[t] ? ids[t] : 0, place = x.there[t] ? at & page_mask : 0;
+            const int at = key0 + t * 16 + (decltype(PAGED)::value ? 0 : n);
+            int id = decltype(PAGED)::value ? __builtin_amdgcn_readfirstlane(ids[t]) : ids[t];
+            const bool there = (unsigned)id < (unsigned)p.n_pages && at < it.end;
+            if (decltype(PAGED)::value)
+                x.valid |= there ? (it.end - at >= 16 ? 0xffffu : (1u << (it.end - at)) - 1) << (16 * t) : 0u;
+            else
+                x.valid |= ((uint32_t)__ballot(there) & 0xffff) << (16 * t);
+            id = there ? id : 0;
+            const int64_t place = at & page_mask;
             const int64_t c_at = id * p.page_stride + place * p.token_stride, s_at = id * p.s_page + place * p.s_token;
-            const int e = g * kOwn;
-#pragma unroll
-            for (int i = 0; i < kScales; ++i) {
-                const int of = e + i * kGroup < p.D ? (e + i * kGroup) / kGroup : 0;
-                x.ks[t][i] = ksbase[s_at + of];
-                x.vs[t][i] = vsbase[s_at + of];
-            }
-            if constexpr (decltype(WHOLE)::value) {
-                const int64_t of = c_at + (e < p.D ? e * C::kBits / 8 : 0);
-                auto take = [&](const uint8_t* from, uint32_t (&w)[kWords]) {
-                    if constexpr (kWords == 2) {
-                        const u32x2a v = *reinterpret_cast<const u32x2a*>(from);
-                        w[0] = v[0], w[1] = v[1];
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < kWords; i += 4) {
-                            const u32x4a v = *reinterpret_cast<const u32x4a*>(from + i * 4);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) w[i + j] = v[j];
-                        }
-                    }
-                };
-                take(kbase + of, x.k[t]);
-                take(vbase + of, x.v[t]);
-            } else {
-                int dim = p.D;
-                asm volatile("" : "+s"(dim));  // places computed anew for each tile: kept, they take registers that the loop needs
-#pragma unroll
-                for (int j = 0; j < kWords; ++j) {
-                    const int w = e + j * (32 / C::kBits);
-                    const int64_t of = c_at + (w < dim ? w * C::kBits / 8 : 0);
-                    x.k[t][j] = *reinterpret_cast<const uint32_t*>(kbase + of);
-                    x.v[t][j] = *reinterpret_cast<const uint32_t*>(vbase + of);
-                }
-            }
+            load(WHOLE, PAGED, kbase, ksbase, c_at, s_at, x.k[t], x.ks[t]);
+            load(WHOLE, PAGED, vbase, vsbase, c_at, s_at, x.v[t], x.vs[t]);
         }
     };
     auto widen = [&](const uint32_t* w, uint8_t scale) {
@@ -960,15 +977,16 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     const T* v_get = vt + (4 * g + ((lane & 15) >> 2)) * kPitch + (lane & 3) * 4;
 
     auto use = [&](Codes& x, int key0) {
-        const uint32_t valid = ((uint32_t)__ballot(x.there[0]) & 0xffff) | (uint32_t)__ballot(x.there[1]) << 16;
+        const uint32_t valid = x.valid;
         const bool some = key0 + KT > full || ~valid != 0;  // keys that not every row sees
         if (~valid != 0) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
+                const bool there = (valid >> (16 * t + n)) & 1;
 #pragma unroll
-                for (int j = 0; j < kWords; ++j) x.k[t][j] = x.there[t] ? x.k[t][j] : 0, x.v[t][j] = x.there[t] ? x.v[t][j] : 0;
+                for (int j = 0; j < kWords; ++j) x.k[t][j] = there ? x.k[t][j] : 0, x.v[t][j] = there ? x.v[t][j] : 0;
 #pragma unroll
-                for (int i = 0; i < kScales; ++i) x.ks[t][i] = x.there[t] ? x.ks[t][i] : 0, x.vs[t][i] = x.there[t] ? x.vs[t][i] : 0;
+                for (int i = 0; i < kScales; ++i) x.ks[t][i] = there ? x.ks[t][i] : 0, x.vs[t][i] = there ? x.vs[t][i] : 0;
             }
         }
         f32x4 s[2] = {f32x4{}, f32x4{}};
@@ -1046,13 +1064,13 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         }
     };
     // While a tile is used, the codes of the next are on their way, and the page ids of the one behind it.
-    // (One loop for whole shares, another for others: a branch inside would wait for the loads that each side has under way.)
-    auto run = [&](auto WHOLE) {
+    // (A loop for each way to load: a branch inside would wait for the loads that each side has under way.)
+    auto run = [&](auto WHOLE, auto PAGED) {
         Codes a, b;
-        fetch(WHOLE, key, ids0, a);
+        fetch(WHOLE, PAGED, key, ids0, a);
         auto tile = [&](Codes& now, Codes& next) {
             const int ids2[2] = {page_id(key + 2 * kStep, 0), page_id(key + 2 * kStep, 1)};
-            fetch(WHOLE, key + kStep, ids1, next);  // (past the end: the cache's first row)
+            fetch(WHOLE, PAGED, key + kStep, ids1, next);  // (past the end: the cache's first rows)
             use(now, key);
             key += kStep;
             ids1[0] = ids2[0], ids1[1] = ids2[1];
@@ -1065,10 +1083,15 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         }
     };
     if (key < it.end) {
-        if (p.D % kOwn == 0)
-            run(std::true_type{});
+        const bool paged = page_mask >= 15 && p.token_stride < 1 << 26 && p.s_token < 1 << 26;
+        if (p.D % kOwn == 0 && paged)
+            run(std::true_type{}, std::true_type{});
+        else if (p.D % kOwn == 0)
+            run(std::true_type{}, std::false_type{});
+        else if (paged)
+            run(std::false_type{}, std::true_type{});
         else
-            run(std::false_type{});
+            run(std::false_type{}, std::false_type{});
     }
     l = pair_sum<32>(pair_sum<16>(l));
 
