@@ -145,20 +145,15 @@ struct Whole {
     static constexpr int kBits = 16;
 };
 
-// Codes in shared memory: rows of kRowBytes, in chunks of 16 bytes.
-template <class C, typename T, int DP, bool WIDE>
+// Codes on their way through shared memory (wide workgroups): rows of kRowBytes, in chunks of 16 bytes.
+template <class C, typename T, int DP>
 struct Raw {
-    static constexpr int kRows = Shape<T, DP, WIDE>::kRows;      // rows a wave copies
+    static constexpr int kRows = Shape<T, DP, true>::kRows;      // rows a wave copies
     static constexpr int kRowBytes = DP * C::kBits / 8, CR = kRowBytes / 16;
     static constexpr int kElems = 128 / C::kBits;                // elements of a chunk
     static constexpr int RPI = 64 / CR;                          // rows per copy instruction
     static constexpr int kInstr = kRows > RPI ? kRows / RPI : 1;
     static constexpr int kOf8 = C::kBits / 4;                    // words of eight elements
-    // Narrow: a lane reads half a row's chunks, of whole groups: chunk i of its own is chunk_of(i, half) of the row.
-    static constexpr int kOwn = CR / 2, kPerGroup = kGroup / kElems, kScales = DP / 64;
-    __device__ static constexpr int chunk_of(int i, int half) { return (i / kPerGroup * 2 + half) * kPerGroup + i % kPerGroup; }
-    // Rows lie with their chunks permuted, so that eight lanes that read a chunk of eight rows meet in no bank.
-    __device__ static constexpr int swz(int row) { return (row / (CR < 16 ? 16 / CR : 1)) & (CR - 1); }
 };
 // Scale bytes of a tile, as they are loaded: a lane waits for them where it uses them.
 template <int N>
@@ -247,8 +242,9 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     using Sh = Shape<T, DP, WIDE>;
     constexpr bool PIPE = WIDE && !MULTI;  // scores one tile ahead (MULTI's rare path leaves no registers)
     constexpr int NW = Sh::NW, KT = Sh::KT, CPR = Sh::CPR, NF = DP / 16, ND = DP / 32, SUB = KT / 32;
-    constexpr bool CODES = C::kBits < 16, DIRECT = CODES && !WIDE;
-    using R = Raw<C, T, DP, WIDE>;
+    constexpr bool CODES = C::kBits < 16;
+    static_assert(WIDE || !CODES, "few rows of codes are thin");
+    using R = Raw<C, T, DP>;
     Item it;
     if (!item_of<Sh::kTileRows>(p, prefix, b, &it)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -284,8 +280,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         const T* src = static_cast<const T*>(p.q) + token * p.q_token + head * p.q_head;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
-            // DIRECT: the order in which this half's lanes read a key's chunks
-            const int d = DIRECT ? R::chunk_of(f * 8 / R::kElems, h) * R::kElems + f * 8 % R::kElems : f * 16 + h * 8;
+            const int d = f * 16 + h * 8;
             q[f] = row_ok && d < p.D ? *reinterpret_cast<const vec8<T>*>(src + d) : vec8<T>{};
         }
     }
@@ -311,7 +306,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         return CODES ? (int64_t)id * p.s_page + (int64_t)((key0 + (lane & (KT - 1))) & page_mask) * p.s_token + it.kv * p.s_head : 0;
     };
     // Copies the codes of this wave's rows of a tile to shared memory, RPI rows an instruction (or, where rows are no
-    // multiple of 16 bytes, a word a lane): lane -> row lane / CR, chunk lane % CR, permuted for DIRECT.  What is
+    // multiple of 16 bytes, a word a lane): lane -> row lane / CR, chunk lane % CR.  What is
     // masked or past a row's end comes from the row of zeros.
     // The value at lane r of a 64-bit number.
     auto of_lane = [&](int64_t x, int r) {
@@ -320,11 +315,11 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     auto copy_codes = [&](const Elem* base, int64_t at, uint8_t* to) {
         const uint8_t* codes = reinterpret_cast<const uint8_t*>(base);
         const uint8_t* none = reinterpret_cast<const uint8_t*>(g_zero_row);
-        const int first = WIDE ? wave * R::kRows : 0;
+        const int first = wave * R::kRows;
         if (p.rows16) {
 #pragma unroll
             for (int i = 0; i < R::kInstr; ++i) {
-                const int r = i * R::RPI + lane / R::CR, chunk = (lane % R::CR) ^ (DIRECT ? R::swz(r) : 0);
+                const int r = i * R::RPI + lane / R::CR, chunk = lane % R::CR;
                 const int64_t row = of_lane(at, (first + r) & (KT - 1));
                 const bool there = row >= 0 && chunk * R::kElems < p.D;
                 if (R::kRows >= R::RPI || r < R::kRows)
@@ -334,7 +329,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
 #pragma unroll
             for (int i = 0; i < R::kRows * R::CR / 16; ++i) {
                 const int g = i * 64 + lane, r = g / (R::CR * 4);
-                const int word = ((g / 4 % R::CR) ^ (DIRECT ? R::swz(r) : 0)) * 4 + g % 4;
+                const int word = g % (R::CR * 4);
                 const int64_t row = of_lane(at, first + r);
                 const bool there = row >= 0 && word * (32 / C::kBits) < p.D;
                 __builtin_amdgcn_global_load_lds((gptr)(there ? codes + row + word * 4 : none), (lptr)(to + i * 256), 4, 0, 0);
@@ -416,48 +411,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
                 s.u[u] = mma(*reinterpret_cast<const vec8<T>*>(kt + (k_at ^ (f * 16)) + u * 32 * DP), q[f], s.u[u]);
         return s;
     };
-    // DIRECT: the scales of half of this lane's key, its codes widened to operands, its value's put where
-    // the second product reads them.  The codes are the wave's own, and so are the values.
-    using Own = Scales<R::kScales>;
-    auto own_scales = [&](const uint8_t* scales, int64_t at, int64_t s_at, Own& x) {
-        const uint8_t* row = scales + (at >= 0 ? s_at : 0);  // of a masked key: some scale, which is not used
-#pragma unroll
-        for (int i = 0; i < R::kScales; ++i) {
-            const int g = 2 * i + h;
-            x.b[i] = row[g * kGroup < p.D ? g : 0];
-            x.there[i] = at >= 0;
-        }
-    };
-    auto own_chunk = [&](const uint8_t* rows, int i) {
-        return *reinterpret_cast<const u32x4*>(rows + n * R::kRowBytes + ((R::chunk_of(i, h) ^ R::swz(n)) * 16));
-    };
-    auto scores_of = [&](const uint8_t* rows, const Own& x) {
-        Scores s;
-        s.u[0] = f32x16{};
-#pragma unroll
-        for (int i = 0; i < R::kOwn; ++i) {
-            const u32x4 c = own_chunk(rows, i);
-            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-            for (int j = 0; j < R::kElems / 8; ++j)
-                s.u[0] = mma(widen(w + j * R::kOf8, x.b[i / R::kPerGroup], x.there[i / R::kPerGroup]), q[i * (R::kElems / 8) + j], s.u[0]);
-        }
-        return s;
-    };
-    auto put_values = [&](const uint8_t* rows, const Own& x, T* vt) {
-#pragma unroll
-        for (int i = 0; i < R::kOwn; ++i) {
-            const u32x4 c = own_chunk(rows, i);
-            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-            for (int j = 0; j < R::kElems / 8; ++j) {
-                const int chunk = R::chunk_of(i, h) * (R::kElems / 8) + j;
-                *reinterpret_cast<vec8<T>*>(vt + n * DP + (chunk ^ swz<CPR>(n)) * 8) =
-                    widen(w + j * R::kOf8, x.b[i / R::kPerGroup], x.there[i / R::kPerGroup]);
-            }
-        }
-    };
-    // WIDE: the scales of what this lane copied; the codes in the last part of the wave's rows of a tile, all of them read, then
+    // The scales of what this lane copied; the codes in the last part of the wave's rows of a tile, all of them read, then
     // widened into these rows.
     using Copied = Scales<R::kInstr>;
     auto copied_scales = [&](const uint8_t* scales, int64_t at, int64_t s_at, Copied& x) {
@@ -493,9 +447,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
     // computed while its exponentials are: matrix and vector instructions of one wave run side by
     // side, so the next maximum is part of the same stretch of code.
     auto use = [&](Scores& s, int key0, int64_t at, const T* vbuf, const T* kbuf) {
-        if constexpr (DIRECT) {
-            largest(s);  // the scores are there
-        } else if (!PIPE) {
+        if (!PIPE) {
             s = scores(kbuf);
             largest(s);
         }
@@ -593,53 +545,7 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
     };
 
-    if constexpr (DIRECT) {
-        // The codes of two tiles are on their way while one is used, in two shares of shared memory: those of tile j + 2 are
-        // asked for once tile j's are operands.
-        if (key < it.end) {
-            int64_t at0 = place(key, first0), at1 = place(key + kStep, first1);
-            constexpr int kHalf = KT * R::kRowBytes, kCopies = 2 * R::kInstr;
-            uint8_t* c0 = reinterpret_cast<uint8_t*>(k0) + wave * 2 * kHalf;
-            uint8_t* c1 = reinterpret_cast<uint8_t*>(k1) + wave * 2 * kHalf;
-            T* vt = v0 + wave * KT * DP;
-            Own kx0, vx0, kx1, vx1;
-            Scores s;
-            auto ask = [&](int64_t at, int64_t s_at, uint8_t* c, Own& kx, Own& vx) {
-                own_scales(p.k_scale, at, s_at, kx);
-                own_scales(p.v_scale, at, s_at, vx);
-                __atomic_signal_fence(__ATOMIC_SEQ_CST);
-                copy_codes(kbase, at, c);
-                copy_codes(vbase, at, c + kHalf);
-            };
-            ask(at0, scale_place(key, first0), c0, kx0, vx0);
-            ask(at1, scale_place(key + kStep, first1), c1, kx1, vx1);
-            auto tile = [&](uint8_t* c, Own& kx, Own& vx) {
-                // the copies of this tile are done: only those of the next one, asked for after them, may not be
-                if (p.rows16)
-                    __builtin_amdgcn_s_waitcnt(0x0f70 | (kCopies & 15) | (kCopies >> 4) << 14);
-                else
-                    __builtin_amdgcn_s_waitcnt(0x0f70);
-                __atomic_signal_fence(__ATOMIC_SEQ_CST);
-                s = scores_of(c, kx);
-                put_values(c + kHalf, vx, vt);
-                const int64_t at2 = place(key + 2 * kStep, id2), s_at2 = scale_place(key + 2 * kStep, id2);
-                __builtin_amdgcn_s_waitcnt(0xc07f);  // its codes have been read
-                __atomic_signal_fence(__ATOMIC_SEQ_CST);
-                id2 = page_id(key + 3 * kStep);  // before the copies: whoever waits for it does not wait for them
-                ask(at2, s_at2, c, kx, vx);
-                use(s, key, at0, v0, nullptr);
-                key += kStep;
-                at0 = at1, at1 = at2;
-            };
-            for (;;) {
-                tile(c0, kx0, vx0);
-                if (key >= it.end) break;
-                tile(c1, kx1, vx1);
-                if (key >= it.end) break;
-            }
-            landed();  // nothing is under way when the arrays are used again
-        }
-    } else if constexpr (CODES) {
+    if constexpr (CODES) {
         // As below; the codes are copied to the end of the rows that they become while a tile is used, and spread after it.
         if (key < it.end) {
             int64_t at0 = place(key, first0), at1 = place(key + kStep, first1), s_at1 = scale_place(key + kStep, first1);
@@ -776,36 +682,6 @@ __device__ __forceinline__ void attend(const AttendP& p, bool prefix, int b, T* 
         const float wl = wave_ml[w][1][n];
         if (wl != 0.f) sum += wl * __builtin_amdgcn_exp2f(wave_ml[w][0][n] - base);
     }
-    if constexpr (DIRECT) {
-        // the second wave's sums through the values' array, to be added by the first, lane by lane
-        static_assert(NW == 2 && Sh::kBuf * sizeof(T) >= ND * 16 * 64 * 4, "room for a wave's sums");
-        const float scale = __builtin_amdgcn_exp2f(m - base);
-        f32x4* sums = reinterpret_cast<f32x4*>(v0) + lane;
-        if (wave == 1) {
-#pragma unroll
-            for (int t = 0; t < ND; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    f32x4 v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : o[t][i + e] * scale;
-                    sums[(t * 4 + i / 4) * 64] = v;
-                }
-        }
-        __syncthreads();
-        if (wave == 1 || !row_ok) return;
-#pragma unroll
-        for (int t = 0; t < ND; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                f32x4 v = sums[(t * 4 + i / 4) * 64];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += l == 0.f ? 0.f : o[t][i + e] * scale;
-                put(token, head, t * 32 + 2 * i + 4 * h, v, sum);
-            }
-        if (h == 0) put_ml(top, sum);
-        return;
-    }
     // [wave][row][DP], 16-byte chunks permuted by the row: half of each row in the keys' array, half in the values'
     static_assert(WIDE || Sh::kBuf * sizeof(T) >= NW * 32 * DP / 2 * 4, "room for the waves' sums");
     auto joined = [&](int w, int r, int chunk) {
@@ -913,7 +789,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     // A lane's codes and scales of a tile.  A masked key's are those of the cache's first rows (`use` makes zeros of them), so that
     // there is nothing but loads here: a choice between these and zeros becomes branches that wait for what they have loaded.
     // What is past a row's end is its start once more: it meets zeros of the query, or becomes columns that are not written.
-    // WHOLE: no row ends inside a lane's share.  PAGED: the 16 keys of a half lie in one page, at an address that the wave
+    // GRAIN: elements that are there or past a row's end together, the lane's whole share or 16 or 8.  PAGED: the 16 keys of a half lie in one page, at an address that the wave
     // shares and places that the lanes keep; otherwise each lane works out its own.
     const int e = g * kOwn;
     int s_of[kScales], w_of[kWords];
@@ -924,29 +800,33 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         const int w = e + j * (32 / C::kBits);
         w_of[j] = w < p.D ? w * C::kBits / 8 : 0;
     }
-    auto load = [&](auto WHOLE, auto PAGED, const uint8_t* codes, const uint8_t* scales, int64_t c_at, int64_t s_at, uint32_t (&w)[kWords],
+    auto load = [&](auto GRAIN, auto PAGED, const uint8_t* codes, const uint8_t* scales, int64_t c_at, int64_t s_at, uint32_t (&w)[kWords],
                     uint8_t (&s)[kScales]) {
+        constexpr int kTake = decltype(GRAIN)::value * C::kBits / 32;  // words together
         const int c_n = decltype(PAGED)::value ? n * (int)p.token_stride : 0, s_n = decltype(PAGED)::value ? n * (int)p.s_token : 0;
         const uint8_t* from = decltype(PAGED)::value ? wave_address(codes + c_at) : codes + c_at;
         const uint8_t* s_from = decltype(PAGED)::value ? wave_address(scales + s_at) : scales + s_at;
 #pragma unroll
         for (int i = 0; i < kScales; ++i) s[i] = *(gbyte)(s_from + (uint32_t)(s_n + s_of[i]));
-        if constexpr (!decltype(WHOLE)::value) {
 #pragma unroll
-            for (int j = 0; j < kWords; ++j) w[j] = *(gword)(from + (uint32_t)(c_n + w_of[j]));
-        } else if constexpr (kWords == 2) {
-            const u32x2a v = *(gwords2)(from + (uint32_t)(c_n + w_of[0]));
-            w[0] = v[0], w[1] = v[1];
-        } else {
+        for (int i = 0; i < kWords; i += kTake) {
+            const uint8_t* at = from + (uint32_t)(c_n + w_of[i]);
+            if constexpr (kTake == 1) {
+                w[i] = *(gword)at;
+            } else if constexpr (kTake == 2) {
+                const u32x2a v = *(gwords2)at;
+                w[i] = v[0], w[i + 1] = v[1];
+            } else {
 #pragma unroll
-            for (int i = 0; i < kWords; i += 4) {
-                const u32x4a v = *(gwords4)(from + (uint32_t)(c_n + w_of[0]) + i * 4);
+                for (int k = 0; k < kTake; k += 4) {
+                    const u32x4a v = *(gwords4)(at + k * 4);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[i + j] = v[j];
+                    for (int j = 0; j < 4; ++j) w[i + k + j] = v[j];
+                }
             }
         }
     };
-    auto fetch = [&](auto WHOLE, auto PAGED, int key0, const int (&ids)[2], Codes& x) {
+    auto fetch = [&](auto GRAIN, auto PAGED, int key0, const int (&ids)[2], Codes& x) {
         x.valid = 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -960,8 +840,8 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
             id = there ? id : 0;
             const int64_t place = at & page_mask;
             const int64_t c_at = id * p.page_stride + place * p.token_stride, s_at = id * p.s_page + place * p.s_token;
-            load(WHOLE, PAGED, kbase, ksbase, c_at, s_at, x.k[t], x.ks[t]);
-            load(WHOLE, PAGED, vbase, vsbase, c_at, s_at, x.v[t], x.vs[t]);
+            load(GRAIN, PAGED, kbase, ksbase, c_at, s_at, x.k[t], x.ks[t]);
+            load(GRAIN, PAGED, vbase, vsbase, c_at, s_at, x.v[t], x.vs[t]);
         }
     };
     auto widen = [&](const uint32_t* w, uint8_t scale) {
@@ -1065,12 +945,12 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     };
     // While a tile is used, the codes of the next are on their way, and the page ids of the one behind it.
     // (A loop for each way to load: a branch inside would wait for the loads that each side has under way.)
-    auto run = [&](auto WHOLE, auto PAGED) {
+    auto run = [&](auto GRAIN, auto PAGED) {
         Codes a, b;
-        fetch(WHOLE, PAGED, key, ids0, a);
+        fetch(GRAIN, PAGED, key, ids0, a);
         auto tile = [&](Codes& now, Codes& next) {
             const int ids2[2] = {page_id(key + 2 * kStep, 0), page_id(key + 2 * kStep, 1)};
-            fetch(WHOLE, PAGED, key + kStep, ids1, next);  // (past the end: the cache's first rows)
+            fetch(GRAIN, PAGED, key + kStep, ids1, next);  // (past the end: the cache's first rows)
             use(now, key);
             key += kStep;
             ids1[0] = ids2[0], ids1[1] = ids2[1];
@@ -1084,14 +964,18 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     };
     if (key < it.end) {
         const bool paged = page_mask >= 15 && p.token_stride < 1 << 26 && p.s_token < 1 << 26;
-        if (p.D % kOwn == 0 && paged)
-            run(std::true_type{}, std::true_type{});
-        else if (p.D % kOwn == 0)
-            run(std::true_type{}, std::false_type{});
-        else if (paged)
-            run(std::false_type{}, std::true_type{});
+        auto by_page = [&](auto GRAIN) {
+            if (paged)
+                run(GRAIN, std::true_type{});
+            else
+                run(GRAIN, std::false_type{});
+        };
+        if (p.D % kOwn == 0)
+            by_page(std::integral_constant<int, kOwn>{});
+        else if (kOwn > 16 && p.D % 16 == 0)
+            by_page(std::integral_constant<int, 16>{});
         else
-            run(std::false_type{}, std::false_type{});
+            by_page(std::integral_constant<int, 8>{});
     }
     l = pair_sum<32>(pair_sum<16>(l));
 
@@ -1148,14 +1032,14 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
 }
 
 // Which shapes a launch holds.  BOTH: a wide prefix beside narrow (of codes: thin) sequences, eight workgroups of one after
-// eight of the other (one for each XCD).  THIN: codes only.
+// eight of the other (one for each XCD).  NARROW: elements of 16 bits only, THIN: codes only.
 enum Roles { NARROW, WIDE_ROWS, BOTH, THIN };
 
 // Waves a SIMD that the registers are shared out for.
 template <int DP, Roles ROLES, bool MULTI, class C>
 constexpr int waves_of() {
     if (ROLES == THIN) return DP <= 64 ? (C::kBits == 4 && !MULTI ? 4 : 3) : DP <= 128 ? (C::kBits == 4 && !MULTI ? 3 : 2) : 1;
-    if (ROLES == NARROW) return C::kBits < 16 && DP <= 128 && !MULTI ? 2 : 1;
+    if (ROLES == NARROW) return 1;
     return DP <= 128 && (ROLES == BOTH || !MULTI) ? 2 : 1;
 }
 template <typename T, int DP, Roles ROLES>
@@ -1166,12 +1050,11 @@ __global__ __launch_bounds__((threads_of<T, DP, ROLES>), (waves_of<DP, ROLES, MU
     constexpr bool kCodes = C::kBits < 16;
     constexpr int kBuf = ROLES == WIDE_ROWS ? Shape<T, DP, true>::kBuf : Shape<T, DP, false>::kBuf;
     static_assert(Shape<T, DP, false>::kBuf >= Shape<T, DP, true>::kBuf, "room for either shape");
-    // narrow workgroups on codes: two tiles of codes, keys and values, and a tile of values for each wave; thin ones: that tile
-    constexpr int kKeys = ROLES == THIN ? 1 : ROLES == NARROW && kCodes ? kBuf * 2 * C::kBits / 16 : kBuf;
+    // thin workgroups: a tile of values for each wave
+    constexpr int kKeys = ROLES == THIN ? 1 : kBuf;
     constexpr int kValues = kCodes && (ROLES == THIN || ROLES == BOTH) ? Shape<T, DP, false>::NW * 32 * (DP + kThinPad) : kBuf;
     static_assert(kValues >= kBuf || ROLES == THIN, "room for a wide tile");
-    constexpr int kMore = ROLES == THIN || (ROLES == NARROW && kCodes) ? 1 : kBuf;
-    __shared__ __attribute__((aligned(16))) T k0[kKeys], k1[kKeys], v0[kValues], v1[kMore];
+    __shared__ __attribute__((aligned(16))) T k0[kKeys], k1[kKeys], v0[kValues], v1[kKeys];
     __shared__ float wave_ml[Shape<T, DP, false>::NW][2][32], row_sum[32];
     int b = blockIdx.x;
     if constexpr (ROLES == BOTH) {
@@ -1321,7 +1204,9 @@ hipError_t attend_type(const ls_kv_cache& c, const ls_kvq_cache* codes, const ls
         const dim3 grid((unsigned)(pre_items + suf_items)), narrow_wg(Shape<T, DP, false>::NW * 64), wide_wg(256);
         const bool multi = p.n_q > 1 && suf_items;
         if (roles == NARROW) {
-            if (multi)
+            if constexpr (C::kBits < 16)
+                return hipErrorInvalidValue;  // (never: codes are thin)
+            else if (multi)
                 hipLaunchKernelGGL((attend_kernel<T, DP, NARROW, true, C>), grid, narrow_wg, 0, st, p);
             else
                 hipLaunchKernelGGL((attend_kernel<T, DP, NARROW, false, C>), grid, narrow_wg, 0, st, p);

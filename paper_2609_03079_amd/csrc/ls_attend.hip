@@ -9,12 +9,11 @@ bool plan_attend(const ls_kv_cache& c, int bits, const ls_attend_args& a, size_t
     const int64_t part_bytes = (int64_t)a.n_seqs * a.n_q * a.n_heads * (c.head_dim + 2) * 4;
     plan->pre_wide = pre_rows > 32;
     plan->suf_wide = suf_rows > 32;
-    plan->pre_tiles = (int)ceil_div(pre_rows, plan->pre_wide ? 128 : 32);
-    plan->suf_tiles = (int)ceil_div(suf_rows, plan->suf_wide ? 128 : 32);
+    plan->pre_thin = bits < 16 && !plan->pre_wide;
+    plan->suf_thin = bits < 16 && !plan->suf_wide;
+    plan->pre_tiles = (int)ceil_div(pre_rows, plan->pre_wide ? 128 : plan->pre_thin ? 16 : 32);
+    plan->suf_tiles = (int)ceil_div(suf_rows, plan->suf_wide ? 128 : plan->suf_thin ? 16 : 32);
     plan->alike = plan->pre_wide == plan->suf_wide;
-    // up to 16 rows of codes; prefix and sequences in one launch are of one shape
-    plan->pre_thin = bits < 16 && pre_rows <= 16;
-    plan->suf_thin = bits < 16 && suf_rows <= 16 && (plan->pre_thin || plan->pre_wide || !a.prefix_len);
     // Workgroups that run at once on a compute unit (by shared memory and registers: wide ones of several tokens
     // take more than half of those); the time of a key and of a start and end, as measured with the unit full (us).
     enum Kind { NARROW_ITEM, WIDE_ITEM, TOKENS_ITEM };
@@ -89,7 +88,7 @@ bool plan_attend(const ls_kv_cache& c, int bits, const ls_attend_args& a, size_t
     // A wide prefix and narrow sequences in one launch where all their workgroups run at once (5 x 4 tokens
     // behind 333 keys 20.4 -> 16.3 us).  Larger ones apart: the sequences' stream through the caches takes
     // from the prefix more than running beside it gives (64 sequences behind 32768 keys 149 -> 184 us).
-    plan->together = plan->pre_parts && plan->suf_parts && plan->pre_wide && !plan->suf_wide && (bits == 16 || plan->suf_thin) && at_once(plan->pre_chunk, plan->suf_chunk);
+    plan->together = plan->pre_parts && plan->suf_parts && plan->pre_wide && !plan->suf_wide && at_once(plan->pre_chunk, plan->suf_chunk);
     return true;
 }
 
