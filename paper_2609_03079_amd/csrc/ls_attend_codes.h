@@ -60,6 +60,16 @@ __device__ inline const uint8_t* wave_address(const uint8_t* p) {
     return reinterpret_cast<const uint8_t*>(((uint64_t)hi << 32) | lo);
 }
 
+// The place of a page's token where 32 bits hold both strides, in two scalar products.
+__device__ inline int64_t place_of(int id, int64_t page_stride, int place, int64_t token_stride) {
+    return (int64_t)((uint64_t)(uint32_t)id * (uint32_t)page_stride + (uint32_t)place * (uint32_t)token_stride);
+}
+
+// A row's sums are rescaled where its maximum has grown by more than this since they last were (in powers of two): while it creeps up, by
+// a little in most steps, its largest weight is above 2^kLift instead.  float16 has room for one more power (ls_attend.h).
+template <typename T>
+constexpr float kSlack = std::is_same_v<T, _Float16> ? 1.f : 8.f;
+
 // Eight elements of a lane's codes.
 template <class C, typename T>
 __device__ inline vec8<T> widened(const uint32_t* w, uint8_t scale) {
@@ -117,7 +127,9 @@ struct Share {
 // loads that either side has under way.)
 template <int OWN, typename Run>
 __device__ __forceinline__ void by_grain(const AttendP& p, bool paged, Run run) {
-    paged = paged && p.token_stride < 1 << 26 && p.s_token < 1 << 26;  // 32 bits hold a tile's offsets
+    // 32 bits hold the offsets within a page, and a page
+    paged = paged && (p.token_stride << p.page_shift) < (int64_t)1 << 31 && (p.s_token << p.page_shift) < (int64_t)1 << 31 &&
+            p.page_stride < (int64_t)1 << 32 && p.s_page < (int64_t)1 << 32;
     auto by_page = [&](auto GRAIN) __attribute__((always_inline)) {
         if (paged)
             run(GRAIN, std::true_type{});
@@ -207,8 +219,15 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
             else
                 x.valid |= ((uint32_t)__ballot(there) & 0xffff) << (16 * t);
             id = there ? id : 0;
-            const int64_t place = at & page_mask;
-            const int64_t c_at = id * p.page_stride + place * p.token_stride, s_at = id * p.s_page + place * p.s_token;
+            const int place = at & page_mask;
+            int64_t c_at, s_at;
+            if (decltype(PAGED)::value) {
+                c_at = place_of(id, p.page_stride, place, p.token_stride);
+                s_at = place_of(id, p.s_page, place, p.s_token);
+            } else {
+                c_at = id * p.page_stride + place * p.token_stride;
+                s_at = id * p.s_page + place * p.s_token;
+            }
             share.load(GRAIN, PAGED, kbase + c_at, ksbase + s_at, c_n, s_n, x.k[t], x.ks[t]);
             share.load(GRAIN, PAGED, vbase + c_at, vsbase + s_at, c_n, s_n, x.v[t], x.vs[t]);
         }
@@ -254,14 +273,16 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         top = pair_max<16>(top);
         top = pair_max<32>(top);
-        const float next = fmaxf(m, top * p.c - kLift<T>), base = next == -INFINITY ? 0.f : next;
-        if (__any(next > m)) {
-            const float scale = __builtin_amdgcn_exp2f(m - base);  // m = -inf: 0
+        const float next = top * p.c - kLift<T>;
+        const bool grown = next > m + kSlack<T>;
+        if (__any(grown)) {
+            const float to = grown ? next : m, scale = grown ? __builtin_amdgcn_exp2f(m - next) : 1.f;  // m = -inf: 0
             l *= scale;
 #pragma unroll
             for (auto& y : o) y *= scale;
-            m = next;
+            m = to;
         }
+        const float base = m == -INFINITY ? 0.f : m;
         vec8<T> pr;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -464,9 +485,9 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
                 const int at = key0 + t * 16, its = __builtin_amdgcn_readlane(id, t * 16);
                 const bool there = (unsigned)its < (unsigned)p.n_pages && at < it.end;
                 x.valid |= there ? (it.end - at >= 16 ? 0xffffu : (1u << (it.end - at)) - 1) << (16 * t) : 0u;
-                const int64_t pg = there ? its : 0, place = at & page_mask;
-                c_at[t] = pg * p.page_stride + place * p.token_stride;
-                s_at[t] = pg * p.s_page + place * p.s_token;
+                const int pg = there ? its : 0, place = at & page_mask;
+                c_at[t] = place_of(pg, p.page_stride, place, p.token_stride);
+                s_at[t] = place_of(pg, p.s_page, place, p.s_token);
             }
             const bool second = n >= 16;
             const uint32_t in = n & 15;
@@ -486,9 +507,9 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
         x.there = (unsigned)id < (unsigned)p.n_pages && first + vn < it.end;
         if constexpr (decltype(PAGED)::value) {
             const int its = __builtin_amdgcn_readfirstlane(id);
-            const int64_t pg = (unsigned)its < (unsigned)p.n_pages ? its : 0, place = first & page_mask;
-            value_share.load(GRAIN, PAGED, vbase + pg * p.page_stride + place * p.token_stride, vsbase + pg * p.s_page + place * p.s_token,
-                             vn * (uint32_t)p.token_stride, vn * (uint32_t)p.s_token, x.w, x.s);
+            const int pg = (unsigned)its < (unsigned)p.n_pages ? its : 0, place = first & page_mask;
+            value_share.load(GRAIN, PAGED, vbase + place_of(pg, p.page_stride, place, p.token_stride),
+                             vsbase + place_of(pg, p.s_page, place, p.s_token), vn * (uint32_t)p.token_stride, vn * (uint32_t)p.s_token, x.w, x.s);
         } else {
             const int64_t pg = x.there ? id : 0, place = (first + vn) & page_mask;
             value_share.load(GRAIN, PAGED, vbase + pg * p.page_stride + place * p.token_stride, vsbase + pg * p.s_page + place * p.s_token, 0, 0,
@@ -535,14 +556,16 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         top = pair_max<32>(top);
-        const float next = fmaxf(m, top * p.c - kLift<T>), base = next == -INFINITY ? 0.f : next;
-        if (__any(next > m)) {
-            const float scale = __builtin_amdgcn_exp2f(m - base);  // m = -inf: 0
+        const float next = top * p.c - kLift<T>;
+        const bool grown = next > m + kSlack<T>;
+        if (__any(grown)) {
+            const float to = grown ? next : m, scale = grown ? __builtin_amdgcn_exp2f(m - next) : 1.f;  // m = -inf: 0
             l *= scale;
 #pragma unroll
             for (auto& x : o) x *= scale;
-            m = next;
+            m = to;
         }
+        const float base = m == -INFINITY ? 0.f : m;
         const f32x16 after = ahead();
         vec8<T> pr[2];
 #pragma unroll
