@@ -527,24 +527,24 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
 #pragma unroll
         for (int f = 0; f < DP / 32; ++f) *reinterpret_cast<vec8<T>*>(to + f * 8) = widened<C, T>(&x.w[f * kOf8], x.s[f * 8 / kGroup]);
     };
-    auto scores = [&](Keys& x) __attribute__((always_inline)) {
-        if (~x.valid != 0) {
-            const bool there = (x.valid >> n) & 1;
+    auto clear = [&](Keys& x) __attribute__((always_inline)) {
+        if (~x.valid == 0) return;
+        const bool there = (x.valid >> n) & 1;
 #pragma unroll
-            for (int j = 0; j < KeyShare::kWords; ++j) x.w[j] = there ? x.w[j] : 0;
+        for (int j = 0; j < KeyShare::kWords; ++j) x.w[j] = there ? x.w[j] : 0;
 #pragma unroll
-            for (int i = 0; i < KeyShare::kScales; ++i) x.s[i] = there ? x.s[i] : 0;
-        }
-        f32x16 s{};
-#pragma unroll
-        for (int f = 0; f < NF; ++f) s = mma(widened<C, T>(&x.w[f * kOf8], x.s[f * 8 / kGroup]), q[f], s);
-        return s;
+        for (int i = 0; i < KeyShare::kScales; ++i) x.s[i] = there ? x.s[i] : 0;
+    };
+    auto score = [&](const Keys& x, int f, f32x16& s) __attribute__((always_inline)) {  // the f-th product of NF
+        s = mma(widened<C, T>(&x.w[f * kOf8], x.s[f * 8 / kGroup]), q[f], s);
     };
     // where this lane finds element 32 t + n of keys 4 h + 0 .. 3 and + 8, by fours, transposed (rows 32 bytes apart in their banks)
     const int v_get = (4 * h + ((lane & 15) >> 2)) * kPitch + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 
-    // 32 keys: their scores are in s, `ahead` computes those of the next 32.
-    auto use = [&](f32x16& s, uint32_t valid, int key0, const T* vt, auto ahead) __attribute__((always_inline)) {
+    // 32 keys: their scores are in s; those of the next 32 are computed ahead.  Matrix and vector instructions of a wave run side
+    // by side where they are asked for in turn, so the order is written down: a product of the scores ahead, each of which waits for
+    // the one before, beside two exponentials; then the values' products, their operands read three products early.
+    auto use = [&](f32x16& s, uint32_t valid, int key0, const T* vt, Keys& ahead) __attribute__((always_inline)) {
         // score i of a lane belongs to key 8 (i / 4) + 4 h + i % 4
         if (key0 + 32 > full || ~valid != 0) {
             const int left = limit - key0;
@@ -566,14 +566,6 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             m = to;
         }
         const float base = m == -INFINITY ? 0.f : m;
-        const f32x16 after = ahead();
-        vec8<T> pr[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[i], p.c, -base));
-            l += e;
-            pr[i / 8][i % 8] = (T)e;
-        }
         auto value = [&](int kk, int t) __attribute__((always_inline)) {
             typedef __attribute__((address_space(3))) s16x4* lds4;
             const T* at = vt + v_get + kk * 16 * kPitch + t * 32;
@@ -582,6 +574,22 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             struct { s16x4 a, b; } both{a, b};
             return __builtin_bit_cast(vec8<T>, both);
         };
+        clear(ahead);
+        constexpr int kEarly = 3;
+        vec8<T> pr[2], val[2 * ND];
+        f32x16 after{};
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            score(ahead, f, after);
+#pragma unroll
+            for (int i = f * 16 / NF; i < (f + 1) * 16 / NF; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[i], p.c, -base));
+                l += e;
+                pr[i / 8][i % 8] = (T)e;
+            }
+            if (f >= NF - kEarly) val[f - (NF - kEarly)] = value((f - (NF - kEarly)) / ND, (f - (NF - kEarly)) % ND);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         bool odd = false;
         if (MULTI && it.seq >= 0 && key0 + 32 > full) {  // a weight of zero must keep out a value that is no number
 #pragma unroll
@@ -616,9 +624,11 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             }
         } else {
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int t = 0; t < ND; ++t) o[t] = mma(value(kk, t), pr[kk], o[t]);
+            for (int i = 0; i < 2 * ND; ++i) {
+                if (i + kEarly < 2 * ND) val[i + kEarly] = value((i + kEarly) / ND, (i + kEarly) % ND);
+                o[i % ND] = mma(val[i], pr[i / ND], o[i % ND]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         s = after;
     };
@@ -636,7 +646,10 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
         fetch_keys(GRAIN, PAGED, key, ids0.k[0], ka);
         fetch_keys(GRAIN, PAGED, key + 32, ids0.k[1], kb);
         put_values(x, v0);
-        f32x16 s = scores(ka);
+        f32x16 s{};
+        clear(ka);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) score(ka, f, s);
         uint32_t valid_a = ka.valid;
         // While a tile is used, the next one's values are on their way, and 32 keys behind those whose scores are computed.
         auto tile = [&](const T* now, T* next) __attribute__((always_inline)) {
@@ -644,11 +657,11 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             const Ids ids2 = page_ids(key + 2 * KT);
             fetch_values(GRAIN, PAGED, key + KT, ids1.v, x);
             fetch_keys(GRAIN, PAGED, key + KT, ids1.k[0], ka);
-            if (!idle_wave) use(s, valid_a, key, now, [&] { return scores(kb); });
+            if (!idle_wave) use(s, valid_a, key, now, kb);
             const uint32_t valid_b = kb.valid;
             valid_a = ka.valid;
             fetch_keys(GRAIN, PAGED, key + KT + 32, ids1.k[1], kb);
-            if (!idle_wave) use(s, valid_b, key + 32, now + 32 * kPitch, [&] { return scores(ka); });
+            if (!idle_wave) use(s, valid_b, key + 32, now + 32 * kPitch, ka);
             put_values(x, next);
             key += KT;
             ids1 = ids2;
