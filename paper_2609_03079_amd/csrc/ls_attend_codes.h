@@ -574,6 +574,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             struct { s16x4 a, b; } both{a, b};
             return __builtin_bit_cast(vec8<T>, both);
         };
+        __builtin_amdgcn_s_setprio(1);  // before waves that work out addresses or wait (114.3 -> 112.5 us)
         clear(ahead);
         constexpr int kEarly = 3;
         vec8<T> pr[2], val[2 * ND];
@@ -631,6 +632,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             }
         }
         s = after;
+        __builtin_amdgcn_s_setprio(0);
     };
     // The values of a tile are in shared memory; what this wave wrote there is seen by the others.
     auto landed = [&] {
