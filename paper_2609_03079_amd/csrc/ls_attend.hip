@@ -486,23 +486,21 @@ hipError_t attend_dim(const ls_kv_cache& c, const ls_attend_args& a, const Atten
 
 }  // namespace
 
-bool plan_attend(const ls_kv_cache& c, int bits, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan) {
+bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan) {
     const int G = a.n_heads / c.n_kv_heads;
     const int64_t pre_rows = (int64_t)a.n_seqs * a.n_q * G, suf_rows = (int64_t)a.n_q * G;
     const int64_t part_bytes = (int64_t)a.n_seqs * a.n_q * a.n_heads * (c.head_dim + 2) * 4;
     plan->pre_wide = pre_rows > 32;
     plan->suf_wide = suf_rows > 32;
-    plan->pre_thin = bits < 16 && !plan->pre_wide;
-    plan->suf_thin = bits < 16 && !plan->suf_wide;
-    plan->pre_tiles = (int)ceil_div(pre_rows, plan->pre_wide ? 128 : plan->pre_thin ? 16 : 32);
-    plan->suf_tiles = (int)ceil_div(suf_rows, plan->suf_wide ? 128 : plan->suf_thin ? 16 : 32);
+    plan->pre_tiles = (int)ceil_div(pre_rows, plan->pre_wide ? 128 : 32);
+    plan->suf_tiles = (int)ceil_div(suf_rows, plan->suf_wide ? 128 : 32);
     plan->alike = plan->pre_wide == plan->suf_wide;
     // Workgroups that run at once on a compute unit (by shared memory and registers: wide ones of several tokens
     // take more than half of those); the time of a key and of a start and end, as measured with the unit full (us).
     enum Kind { NARROW_ITEM, WIDE_ITEM, TOKENS_ITEM };
     const Kind pre_kind = plan->pre_wide ? WIDE_ITEM : NARROW_ITEM;
     const Kind suf_kind = !plan->suf_wide ? NARROW_ITEM : a.n_q > 1 && a.max_len ? TOKENS_ITEM : WIDE_ITEM;
-    const int wide_cu = c.head_dim <= 128 ? 2 : 1, narrow_cu = plan->suf_thin ? (c.head_dim <= 64 ? 6 : c.head_dim <= 128 ? (bits == 4 && a.n_q == 1 ? 6 : 4) : 2) : bits < 16 ? (c.head_dim <= 128 ? 4 : 2) : c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 2 : 1;
+    const int wide_cu = c.head_dim <= 128 ? 2 : 1, narrow_cu = c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 2 : 1;
     const double by_dim = (c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256) / 128.0;
     const double tokens_key = c.head_dim <= 64 ? 0.024 : c.head_dim <= 128 ? 0.038 : 0.139;
     auto item_us = [&](Kind kind, int64_t chunk) {

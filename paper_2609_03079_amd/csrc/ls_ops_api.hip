@@ -140,11 +140,11 @@ ls_status check_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a
 }
 
 // Launches an attention that was found right, in as many pieces as it takes.
-template <typename Launch>
-ls_status attend_pieces(ls_ops* c, const ls_kv_cache& kv, int bits, const ls_attend_args* a, const char* what, Launch launch) {
+template <typename Plan, typename Launch>
+ls_status attend_pieces(ls_ops* c, ls_dtype type, const ls_attend_args* a, const char* what, Plan plan_of, Launch launch) {
     ls_status st;
     // A launch holds fewer than 2^32 threads: more rows than 2^20 (at most 2^21 workgroups for a part) are taken in pieces.
-    const int64_t piece = std::max<int64_t>(1, (1 << 20) / ((int64_t)a->n_q * a->n_heads)), es = (int64_t)ls::type_size(kv.dtype);
+    const int64_t piece = std::max<int64_t>(1, (1 << 20) / ((int64_t)a->n_q * a->n_heads)), es = (int64_t)ls::type_size(type);
     for (int64_t s = 0; s < a->n_seqs; s += piece) {
         ls_attend_args b = *a;
         b.n_seqs = (int32_t)std::min<int64_t>(piece, a->n_seqs - s);
@@ -153,7 +153,7 @@ ls_status attend_pieces(ls_ops* c, const ls_kv_cache& kv, int bits, const ls_att
         if (b.pages) b.pages += s * a->pages_stride;
         b.lens += s;
         ls::AttendPlan plan;
-        if (!ls::plan_attend(kv, bits, b, c->ws_bytes, c->n_cu, &plan))
+        if (!plan_of(b, &plan))
             return fail(c, LS_E_CAPACITY, "the partial results do not fit the workspace of %zu bytes", c->ws_bytes);
         if ((st = launched(c, launch(b, plan), what)) != LS_OK) return st;
     }
@@ -274,7 +274,8 @@ ls_status ls_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a) {
     if ((st = check_attend(c, kv, a, "ls_attend takes f16 and bf16 caches")) != LS_OK || a->n_seqs == 0) return st;
     for (int64_t s : {kv->page_stride, kv->head_stride, kv->token_stride}) LS_REQUIRE(s % 8 == 0, "strides must be multiples of 8 elements");
     LS_REQUIRE(ls::aligned(kv->k, 16) && ls::aligned(kv->v, 16), "q, out, k and v must be 16-byte aligned");
-    return attend_pieces(c, *kv, 16, a, "ls_attend", [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
+    auto plan = [&](const ls_attend_args& b, ls::AttendPlan* out) { return ls::plan_attend(*kv, b, c->ws_bytes, c->n_cu, out); };
+    return attend_pieces(c, kv->dtype, a, "ls_attend", plan, [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
         return ls::launch_attend(*kv, b, plan, c->ws, c->stream);
     });
 }
@@ -308,7 +309,8 @@ ls_status ls_kvq_attend(ls_ops* c, const ls_kvq_cache* kv, ls_dtype type, const 
     if ((st = check_kvq(c, kv, type)) != LS_OK) return st;
     const ls_kv_cache shape = ls::shape_of(*kv, type);
     if ((st = check_attend(c, &shape, a, "ls_kvq_attend takes f16 and bf16 queries")) != LS_OK || a->n_seqs == 0) return st;
-    return attend_pieces(c, shape, kv->code == LS_FP4 ? 4 : 8, a, "ls_kvq_attend", [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
+    auto plan = [&](const ls_attend_args& b, ls::AttendPlan* out) { return ls::plan_attend_codes(*kv, b, c->ws_bytes, c->n_cu, out); };
+    return attend_pieces(c, type, a, "ls_kvq_attend", plan, [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
         return kv->code == LS_FP4 ? ls::launch_attend_fp4(*kv, type, b, plan, c->ws, c->stream)
                                   : ls::launch_attend_fp8(*kv, type, b, plan, c->ws, c->stream);
     });

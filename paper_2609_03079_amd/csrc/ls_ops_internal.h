@@ -27,20 +27,19 @@ constexpr int kMaxParts = 128;  // partial results of one row, at most
 struct AttendPlan {
     int pre_chunk, pre_parts, pre_tiles;  // keys per part of the prefix, parts, row tiles
     int suf_chunk, suf_parts, suf_tiles;
-    bool pre_wide, suf_wide;              // 128-row tiles instead of 32-row tiles
-    bool pre_thin, suf_thin;              // 16-row tiles (codes only; in one launch: both or, beside a wide prefix, the sequences)
+    bool pre_wide, suf_wide;              // 128-row tiles instead of 32-row tiles (of codes: 16-row tiles)
     bool alike;                           // prefix and sequences by the same kernel, in one launch
     bool together;                        // a wide prefix and narrow sequences in one launch
 };
-// For at most 2^20 rows n_seqs n_q n_heads, or one sequence; bits: those of an element in the cache.  False where no split
-// fits the workspace.
-bool plan_attend(const ls_kv_cache& c, int bits, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan);
+// For at most 2^20 rows n_seqs n_q n_heads, or one sequence.  False where no split fits the workspace.
+bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan);
 hipError_t launch_attend(const ls_kv_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws,
                          hipStream_t st);
 
-// ---- a cache in 4 or 8 bits (ls_kvq.hip, ls_attend_fp4.hip, ls_attend_fp8.hip) -----------------
+// ---- a cache in 4 or 8 bits (ls_kvq.hip, ls_attend_plan.hip, ls_attend_fp4.hip, ls_attend_fp8.hip)
 hipError_t launch_kvq_append(const ls_kvq_cache& c, ls_dtype type, const ls_append_args& a, hipStream_t st);
 hipError_t launch_kvq_read(const ls_kvq_cache& c, const ls_kvq_read_args& a, hipStream_t st);
+bool plan_attend_codes(const ls_kvq_cache& c, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan);
 hipError_t launch_attend_fp4(const ls_kvq_cache& c, ls_dtype type, const ls_attend_args& a, const AttendPlan& plan, void* ws,
                              hipStream_t st);
 hipError_t launch_attend_fp8(const ls_kvq_cache& c, ls_dtype type, const ls_attend_args& a, const AttendPlan& plan, void* ws,
