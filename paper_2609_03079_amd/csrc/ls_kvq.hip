@@ -9,6 +9,18 @@
 namespace ls {
 namespace {
 
+// Calls whose data is more than the eight L2 caches hold together (4 MiB each) pass them by, and leave a page's tokens to
+// one of them: writing 8192 tokens (64 query heads, 8 key heads of 128, FP4) took 73 us and takes 46, of which 15 by loads and
+// stores that are not kept, 5 by lanes of four heads; reading 32768 tokens of 8 heads (FP8) 51 and 30 (tokens by two 4, stores 15, one
+// L2 for a page 3).  Smaller ones stay in the caches for whoever reads them next.
+constexpr int64_t kStreamBytes = 32 << 20;
+
+// Block b of n, such that runs of 64 are on one die (they take blocks in turn): tokens of a page share cache lines.
+__device__ inline int64_t in_runs(uint32_t b, uint32_t n) {
+    const uint32_t first = b / 512 * 512, k = b - first;
+    return first + 512 <= n ? first + k % 8 * 64 + k / 8 : b;
+}
+
 // Elements e .. e + 7 of a row in fp32.  VEC: the row's start and e are aligned to 16 bytes.
 template <typename T, bool VEC>
 __device__ inline void load8(const void* row, int64_t at, float* x) {
@@ -26,7 +38,19 @@ __device__ inline void load8(const void* row, int64_t at, float* x) {
     }
 }
 
-template <typename T, bool VEC>
+// 16 bytes that the caches need not keep.
+typedef uint32_t u32x4n __attribute__((ext_vector_type(4)));
+template <typename T, int V>
+__device__ inline Pack<T, V> load_nt(const void* p, int64_t elem) {
+    return __builtin_bit_cast(Pack<T, V>, __builtin_nontemporal_load(reinterpret_cast<const u32x4n*>(static_cast<const T*>(p) + elem)));
+}
+template <typename T, int V>
+__device__ inline void store_nt(void* p, int64_t elem, const Pack<T, V>& v) {
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4n, v), reinterpret_cast<u32x4n*>(static_cast<T*>(p) + elem));
+}
+
+// STREAM: past the caches.
+template <typename T, bool VEC, bool STREAM = false>
 __device__ inline void store8(void* row, int64_t at, const float* x) {
     if (VEC) {
         constexpr int V = sizeof(T) == 4 ? 4 : 8;
@@ -35,7 +59,10 @@ __device__ inline void store8(void* row, int64_t at, const float* x) {
             Pack<T, V> v;
 #pragma unroll
             for (int k = 0; k < V; ++k) v.e[k] = (T)x[i + k];
-            store_pack<T, V>(row, at + i, v);
+            if (STREAM)
+                store_nt<T, V>(row, at + i, v);
+            else
+                store_pack<T, V>(row, at + i, v);
         }
     } else {
 #pragma unroll
@@ -50,10 +77,20 @@ struct KvqAppendP {
     int q_pairs;  // units of a query head that turn, 1 or (vectors) 8 pairs each, 4 of neighbours
     int q_units;  // those and what is copied, an element or eight
     int quads;    // lanes of a head in the cache: four to a group of 32
+    int q_by;     // query heads, or a fourth of them: those that one lane takes are so far apart
     int q_total;  // lanes for the queries, a multiple of four
     int total;
     int most;     // largest scale byte
 };
+
+// x turned by its partner y, c and s cosine and sine (minus it for a pair's first half).  One product is rounded, the sum is in
+// fp32 and then in T, in every kernel, so that no bit depends on how many tokens or what strides a call has: without the empty
+// asm some kernels would round the sum to float16 at once.
+__device__ inline float turn(float x, float y, float c, float s) {
+    float r = __builtin_fmaf(y, s, x * c);
+    asm("" : "+v"(r));
+    return r;
+}
 
 // Elements e .. e + 7 of a head turned to their position.  VEC: whole vectors of them turn or do not, with partners
 // in one vector; otherwise element by element.
@@ -67,8 +104,8 @@ __device__ inline void turned8(const ls_append_args& a, const float* cs, const v
         for (int i = 0; i < 8; i += 2) {
             if (!VEC && e + i >= a.rot_dim) break;
             const float co = cs[(e + i) / 2], si = cs[half + (e + i) / 2], l = x[i], m = x[i + 1];
-            x[i] = l * co - m * si;
-            x[i + 1] = m * co + l * si;
+            x[i] = turn(l, m, co, -si);
+            x[i + 1] = turn(m, l, co, si);
         }
     } else if (VEC) {
         const bool second = e >= half;
@@ -77,7 +114,7 @@ __device__ inline void turned8(const ls_append_args& a, const float* cs, const v
         load8<float, true>(cs, second ? e - half : e, co);
         load8<float, true>(cs, second ? e : e + half, si);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = second ? x[i] * co[i] + y[i] * si[i] : x[i] * co[i] - y[i] * si[i];
+        for (int i = 0; i < 8; ++i) x[i] = turn(x[i], y[i], co[i], second ? si[i] : -si[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -86,7 +123,7 @@ __device__ inline void turned8(const ls_append_args& a, const float* cs, const v
             const bool second = k >= half;
             const float y = (float)static_cast<const T*>(src)[from + (second ? k - half : k + half)];
             const float co = cs[second ? k - half : k], si = cs[second ? k : k + half];
-            x[i] = second ? x[i] * co + y * si : x[i] * co - y * si;
+            x[i] = turn(x[i], y, co, second ? si : -si);
         }
     }
 }
@@ -117,8 +154,8 @@ __device__ inline void turn_query(const KvqAppendP& p, const float* cs, int64_t 
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float l = x[i], m = y[i];
-            x[i] = l * co[i] - m * si[i];
-            y[i] = m * co[i] + l * si[i];
+            x[i] = turn(l, m, co[i], -si[i]);
+            y[i] = turn(m, l, co[i], si[i]);
         }
         store8<T, true>(a.q_out, to + e, x);
         store8<T, true>(a.q_out, to + half + e, y);
@@ -126,8 +163,59 @@ __device__ inline void turn_query(const KvqAppendP& p, const float* cs, int64_t 
         const int i = PAIR ? 2 * u : u, j = PAIR ? 2 * u + 1 : u + half;
         const float l = (float)static_cast<const T*>(a.q)[from + i], m = (float)static_cast<const T*>(a.q)[from + j];
         const float c = cs[u], s = cs[half + u];
-        static_cast<T*>(a.q_out)[to + i] = (T)(l * c - m * s);
-        static_cast<T*>(a.q_out)[to + j] = (T)(m * c + l * s);
+        static_cast<T*>(a.q_out)[to + i] = (T)turn(l, m, c, -s);
+        static_cast<T*>(a.q_out)[to + j] = (T)turn(m, l, c, s);
+    }
+}
+
+// The same of heads h, h + by, h + 2 by and h + 3 by, in vectors: all loads first, and one of the table.
+constexpr int kHeads = 4;
+template <typename T, bool PAIR>
+__device__ inline void turn_queries(const KvqAppendP& p, const float* cs, int64_t from, int64_t to, int h, int u) {
+    const ls_append_args& a = p.a;
+    constexpr int V = sizeof(T) == 4 ? 4 : 8, N = 8 / V;
+    const int half = a.rot_dim / 2;
+    const bool turns = u < p.q_pairs, second = !PAIR && turns;
+    const int e = turns ? u * 8 : a.rot_dim + (u - p.q_pairs) * 8;
+    Pack<T, V> x[kHeads][N], y[kHeads][N];
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) {
+        if (h + g * p.q_by >= a.n_heads) break;
+        const int64_t at = from + (h + g * p.q_by) * a.q_head_stride + e;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            x[g][n] = load_nt<T, V>(a.q, at + n * V);
+            if (second) y[g][n] = load_nt<T, V>(a.q, at + half + n * V);
+        }
+    }
+    float co[8], si[8];
+    if (turns && PAIR) {
+        const auto c4 = load_pack<float, 4>(cs, u * 4), s4 = load_pack<float, 4>(cs, half + u * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) co[i] = c4.e[i], si[i] = s4.e[i];
+    } else if (turns) {
+        load8<float, true>(cs, e, co);
+        load8<float, true>(cs, half + e, si);
+    }
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) {
+        if (h + g * p.q_by >= a.n_heads) break;
+        const int64_t at = to + (h + g * p.q_by) * a.q_out_head_stride + e;
+        if (turns) {
+#pragma unroll
+            for (int i = 0; i < (PAIR ? 4 : 8); ++i) {
+                T& l = PAIR ? x[g][2 * i / V].e[2 * i % V] : x[g][i / V].e[i % V];
+                T& m = PAIR ? x[g][2 * i / V].e[2 * i % V + 1] : y[g][i / V].e[i % V];
+                const float lf = (float)l, mf = (float)m;
+                l = (T)turn(lf, mf, co[i], -si[i]);
+                m = (T)turn(mf, lf, co[i], si[i]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            store_nt<T, V>(a.q_out, at + n * V, x[g][n]);
+            if (second) store_nt<T, V>(a.q_out, at + half + n * V, y[g][n]);
+        }
     }
 }
 
@@ -137,14 +225,38 @@ __device__ inline uint32_t max_quad(uint32_t v) {
     return v > o ? v : o;
 }
 
-// A lane takes eight pairs of a query head, or eight elements of a key or value, which it
-// quantises with the other three lanes of their group: one read of the data, the largest magnitude over four
-// lanes, one conversion.  blockIdx.x is the token, blockIdx.y 256 of its lanes.
-template <typename T, class C, bool VEC, bool PAIR>
+// Eight elements from e of a key or value are quantised with those of the other three lanes of their group and written.
+template <class C>
+__device__ inline void put8(const KvqAppendP& p, bool value, int64_t page, int64_t place, int h, int e, const float* x) {
+    const ls_kvq_cache& c = p.c;
+    // magnitudes compare as their bits do, infinities and NaN above every number
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+    top = max_quad<0xb1>(top);  // quad_perm [1,0,3,2]
+    top = max_quad<0x4e>(top);  // quad_perm [2,3,0,1]
+    const bool fine = top < 0x7f800000u;
+    const uint32_t byte = fine ? (uint32_t)min(max((int)((top + C::kCarry) >> 23) - C::kBelow, 1), p.most) : 255u;
+    uint32_t w[C::kBits / 4] = {};
+    if (fine) narrow8<C>(x, scale_of(byte), w);
+    if (e >= c.head_dim) return;
+    uint8_t* to = static_cast<uint8_t*>(value ? c.v : c.k) + page * c.page_stride + place * c.token_stride + h * c.head_stride + e * C::kBits / 8;
+    if constexpr (C::kBits == 4)
+        *reinterpret_cast<uint32_t*>(to) = w[0];
+    else
+        *reinterpret_cast<u32x2a*>(to) = u32x2a{w[0], w[1]};
+    if (e % kGroup == 0)
+        (value ? c.v_scale : c.k_scale)[page * c.scale_page_stride + place * c.scale_token_stride + h * c.scale_head_stride + e / kGroup] =
+            (uint8_t)byte;
+}
+
+// A lane takes eight pairs of a query head, or eight elements of a key or value.  STREAM: of four query heads, or
+// of a key and its value.  blockIdx.x is the token, blockIdx.y 256 of its lanes.
+template <typename T, class C, bool VEC, bool PAIR, bool STREAM>
 __global__ __launch_bounds__(256) void kvq_append_kernel(const KvqAppendP p) {
     const ls_append_args& a = p.a;
     const ls_kvq_cache& c = p.c;
-    const int64_t t = blockIdx.x;
+    const int64_t t = STREAM ? in_runs(blockIdx.x, gridDim.x) : blockIdx.x;
     int pos = 0;
     if (a.rot_dim) {
         pos = a.positions[t];
@@ -157,49 +269,30 @@ __global__ __launch_bounds__(256) void kvq_append_kernel(const KvqAppendP p) {
     const int total = keep ? p.total : p.q_total;
     for (int i = blockIdx.y * 256 + threadIdx.x; i < total; i += 256 * gridDim.y) {
         if (i < p.q_total) {
-            const int h = i / p.q_units;
-            if (h < a.n_heads)
-                turn_query<T, VEC, PAIR>(p, cs, t * a.q_token_stride + h * a.q_head_stride,
-                                         t * a.q_out_token_stride + h * a.q_out_head_stride, i - h * p.q_units);
+            const int h = i / p.q_units, u = i - h * p.q_units;
+            if (h >= p.q_by) continue;
+            if constexpr (STREAM)
+                turn_queries<T, PAIR>(p, cs, t * a.q_token_stride, t * a.q_out_token_stride, h, u);
+            else
+                turn_query<T, VEC, PAIR>(p, cs, t * a.q_token_stride + h * a.q_head_stride, t * a.q_out_token_stride + h * a.q_out_head_stride, u);
             continue;
         }
         const int j = i - p.q_total, row = j / p.quads, e = (j - row * p.quads) * 8;
-        const bool value = row >= c.n_kv_heads;
+        const bool value = !STREAM && row >= c.n_kv_heads;
         const int h = value ? row - c.n_kv_heads : row;
-        float x[8] = {};
+        float x[8] = {}, y[8] = {};
         if (e < c.head_dim) {
-            if (value)
-                load8<T, VEC>(a.v, t * a.v_token_stride + h * a.v_head_stride + e, x);
-            else
-                turned8<T, VEC, PAIR>(a, cs, a.k, t * a.k_token_stride + h * a.k_head_stride, e, x);
+            if (value || STREAM) load8<T, VEC>(a.v, t * a.v_token_stride + h * a.v_head_stride + e, value ? x : y);
+            if (!value) turned8<T, VEC, PAIR>(a, cs, a.k, t * a.k_token_stride + h * a.k_head_stride, e, x);
         }
-        // magnitudes compare as their bits do, infinities and NaN above every number
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
-        top = max_quad<0xb1>(top);  // quad_perm [1,0,3,2]
-        top = max_quad<0x4e>(top);  // quad_perm [2,3,0,1]
-        const bool fine = top < 0x7f800000u;
-        const uint32_t byte = fine ? (uint32_t)min(max((int)((top + C::kCarry) >> 23) - C::kBelow, 1), p.most) : 255u;
-        uint32_t w[C::kBits / 4] = {};
-        if (fine) narrow8<C>(x, scale_of(byte), w);
-        if (e < c.head_dim) {
-            uint8_t* to = static_cast<uint8_t*>(value ? c.v : c.k) + page * c.page_stride + place * c.token_stride + h * c.head_stride +
-                          e * C::kBits / 8;
-            if constexpr (C::kBits == 4)
-                *reinterpret_cast<uint32_t*>(to) = w[0];
-            else
-                *reinterpret_cast<u32x2a*>(to) = u32x2a{w[0], w[1]};
-            if (e % kGroup == 0)
-                (value ? c.v_scale : c.k_scale)[page * c.scale_page_stride + place * c.scale_token_stride + h * c.scale_head_stride + e / kGroup] =
-                    (uint8_t)byte;
-        }
+        put8<C>(p, value, page, place, h, e, x);
+        if (STREAM) put8<C>(p, true, page, place, h, e, y);
     }
 }
 
 template <typename T, class C>
 hipError_t kvq_append_type(const ls_kvq_cache& c, const ls_append_args& a, hipStream_t st) {
-    KvqAppendP p{c, a, 0, 0, 0, 0, 0, 0};
+    KvqAppendP p{c, a, 0, 0, 0, 0, 0, 0, 0};
     p.quads = (int)ceil_div(c.head_dim, kGroup) * 4;
     p.most = 127 + (std::is_same_v<T, _Float16> ? C::kMostExp16 : C::kMostExp);
     const bool pair = a.style == LS_ROPE_PAIR;
@@ -211,15 +304,19 @@ hipError_t kvq_append_type(const ls_kvq_cache& c, const ls_append_args& a, hipSt
     for (const void* q : {a.k, a.v, a.q, (const void*)a.q_out}) vec = vec && aligned(q, 16);
     p.q_pairs = vec ? a.rot_dim / (pair ? 8 : 16) : a.rot_dim / 2;
     p.q_units = p.q_pairs + (c.head_dim - a.rot_dim) / (vec ? 8 : 1);
-    p.q_total = (int)round_up((size_t)a.n_heads * p.q_units, 4);
-    p.total = p.q_total + 2 * c.n_kv_heads * p.quads;
+    const int64_t bytes = (int64_t)a.n_tokens * c.head_dim * (a.n_heads + 2 * c.n_kv_heads) * (int64_t)sizeof(T);
+    const bool stream = vec && bytes > kStreamBytes;
+    p.q_by = stream ? (int)ceil_div(a.n_heads, kHeads) : a.n_heads;
+    p.q_total = (int)round_up((size_t)p.q_by * p.q_units, 4);
+    p.total = p.q_total + (stream ? 1 : 2) * c.n_kv_heads * p.quads;
     const dim3 grid(a.n_tokens, (unsigned)std::min<int64_t>(ceil_div(p.total, 256), 65535));
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, p);
         return hipGetLastError();
     };
-    if (pair) return vec ? go(kvq_append_kernel<T, C, true, true>) : go(kvq_append_kernel<T, C, false, true>);
-    return vec ? go(kvq_append_kernel<T, C, true, false>) : go(kvq_append_kernel<T, C, false, false>);
+    if (stream) return pair ? go(kvq_append_kernel<T, C, true, true, true>) : go(kvq_append_kernel<T, C, true, false, true>);
+    if (pair) return vec ? go(kvq_append_kernel<T, C, true, true, false>) : go(kvq_append_kernel<T, C, false, true, false>);
+    return vec ? go(kvq_append_kernel<T, C, true, false, false>) : go(kvq_append_kernel<T, C, false, false, false>);
 }
 
 // ---- read ----------------------------------------------------------------------------------
@@ -229,34 +326,47 @@ struct KvqReadP {
     int units;  // eights of a head
 };
 
-// A lane widens eight elements; blockIdx.x is the token, blockIdx.y 256 of its eights, keys before values.
-template <typename T, class C, bool VEC>
+// A lane widens eight elements, STREAM: of two tokens, with their loads in flight together.  blockIdx.x is the token or two,
+// blockIdx.y 256 of a token's eights, keys before values.
+template <typename T, class C, bool VEC, bool STREAM>
 __global__ __launch_bounds__(256) void kvq_read_kernel(const KvqReadP p) {
     const ls_kvq_read_args& a = p.a;
     const ls_kvq_cache& c = p.c;
-    const int64_t t = blockIdx.x;
-    const int slot = a.slots[t];
-    if (slot < 0 || slot >= c.n_pages * c.page_size) return;
-    const int64_t page = slot / c.page_size, place = slot % c.page_size;
+    constexpr int TOKENS = STREAM ? 2 : 1;
+    const int64_t t0 = (STREAM ? in_runs(blockIdx.x, gridDim.x) : blockIdx.x) * TOKENS;
+    int slot[TOKENS];
+#pragma unroll
+    for (int n = 0; n < TOKENS; ++n) slot[n] = t0 + n < a.n_tokens ? a.slots[t0 + n] : -1;
     for (int i = blockIdx.y * 256 + threadIdx.x; i < 2 * c.n_kv_heads * p.units; i += 256 * gridDim.y) {
         const int row = i / p.units, e = (i - row * p.units) * 8;
         const bool value = row >= c.n_kv_heads;
         const int h = value ? row - c.n_kv_heads : row;
-        const uint8_t* from = static_cast<const uint8_t*>(value ? c.v : c.k) + page * c.page_stride + place * c.token_stride +
-                              h * c.head_stride + e * C::kBits / 8;
-        const uint32_t byte = (value ? c.v_scale : c.k_scale)[page * c.scale_page_stride + place * c.scale_token_stride +
-                                                              h * c.scale_head_stride + e / kGroup];
-        uint32_t w[2];
-        if constexpr (C::kBits == 4) {
-            w[0] = *reinterpret_cast<const uint32_t*>(from);
-        } else {
-            const u32x2a v = *reinterpret_cast<const u32x2a*>(from);
-            w[0] = v[0], w[1] = v[1];
+        const uint8_t* codes = static_cast<const uint8_t*>(value ? c.v : c.k) + h * c.head_stride + e * C::kBits / 8;
+        const uint8_t* scales = (value ? c.v_scale : c.k_scale) + h * c.scale_head_stride + e / kGroup;
+        void* to = value ? a.v : a.k;
+        const int64_t at = value ? h * a.v_head_stride + e : h * a.k_head_stride + e, by = value ? a.v_token_stride : a.k_token_stride;
+        uint32_t w[TOKENS][2];
+        uint8_t byte[TOKENS];
+#pragma unroll
+        for (int n = 0; n < TOKENS; ++n) {
+            if (slot[n] < 0 || slot[n] >= c.n_pages * c.page_size) continue;
+            const int64_t page = slot[n] / c.page_size, place = slot[n] % c.page_size;
+            const uint8_t* from = codes + page * c.page_stride + place * c.token_stride;
+            byte[n] = scales[page * c.scale_page_stride + place * c.scale_token_stride];
+            if constexpr (C::kBits == 4) {
+                w[n][0] = *reinterpret_cast<const uint32_t*>(from);
+            } else {
+                const u32x2a v = *reinterpret_cast<const u32x2a*>(from);
+                w[n][0] = v[0], w[n][1] = v[1];
+            }
         }
-        float x[1][8];
-        widen8<C, float>(w, scale_of(byte), x);
-        store8<T, VEC>(value ? a.v : a.k, value ? t * a.v_token_stride + h * a.v_head_stride + e : t * a.k_token_stride + h * a.k_head_stride + e,
-                       x[0]);
+#pragma unroll
+        for (int n = 0; n < TOKENS; ++n) {
+            if (slot[n] < 0 || slot[n] >= c.n_pages * c.page_size) continue;
+            float x[1][8];
+            widen8<C, float>(w[n], scale_of(byte[n]), x);
+            store8<T, VEC, STREAM>(to, at + (t0 + n) * by, x[0]);
+        }
     }
 }
 
@@ -266,12 +376,14 @@ hipError_t kvq_read_type(const ls_kvq_cache& c, const ls_kvq_read_args& a, hipSt
     const int64_t el = 16 / (int64_t)sizeof(T);
     bool vec = aligned(a.k, 16) && aligned(a.v, 16);
     for (int64_t s : {a.k_token_stride, a.k_head_stride, a.v_token_stride, a.v_head_stride}) vec = vec && s % el == 0;
-    const dim3 grid(a.n_tokens, (unsigned)std::min<int64_t>(ceil_div(2 * c.n_kv_heads * p.units, 256), 65535));
-    if (vec)
-        hipLaunchKernelGGL((kvq_read_kernel<T, C, true>), grid, dim3(256), 0, st, p);
-    else
-        hipLaunchKernelGGL((kvq_read_kernel<T, C, false>), grid, dim3(256), 0, st, p);
-    return hipGetLastError();
+    const unsigned y = (unsigned)std::min<int64_t>(ceil_div(2 * c.n_kv_heads * p.units, 256), 65535);
+    const int64_t bytes = (int64_t)a.n_tokens * 2 * c.n_kv_heads * c.head_dim * (int64_t)sizeof(T);
+    auto go = [&](auto kernel, int tokens) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(a.n_tokens, tokens), y), dim3(256), 0, st, p);
+        return hipGetLastError();
+    };
+    if (vec && bytes > kStreamBytes) return go(kvq_read_kernel<T, C, true, true>, 2);
+    return vec ? go(kvq_read_kernel<T, C, true, false>, 1) : go(kvq_read_kernel<T, C, false, false>, 1);
 }
 
 template <class C>

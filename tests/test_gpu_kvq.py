@@ -305,6 +305,51 @@ def test_tokens_of_more_than_one_launch(ops):
     assert same(out[0].double(), ref) and same(out[1].double(), ref)
 
 
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("heads,kv,dim,rot,style,in_place", [(37, 3, 80, 64, 0, True), (37, 3, 80, 40, 1, False), (0, 21, 128, 128, 0, False),
+                                                             (64, 8, 64, 0, 0, False), (5, 33, 72, 32, 0, True)])
+def test_calls_of_many_bytes_equal_those_of_few(ops, code, dtype, heads, kv, dim, rot, style, in_place):
+    """Calls that pass the caches by (more than 32 MiB of data) write what the same tokens give a few hundred at a time."""
+    dt, page = TYPES[dtype], 16
+    T = (36 << 20) // (dim * (heads + 2 * kv) * dt.itemsize) + 3
+    assert T * dim * (heads + 2 * kv) * dt.itemsize > 32 << 20
+    qkv = rand((T, (heads + 2 * kv) * dim), 3, dt)
+    g = torch.Generator().manual_seed(T)
+    pages = T // page + 3
+    slots = torch.randperm(pages * page, generator=g)[:T].to(torch.int32)
+    positions = torch.randint(0, 50, (T,), generator=g).to(torch.int32)
+    slots[1], slots[T - 1], positions[3], positions[700] = -1, pages * page, -1, 50
+    slots, positions, cs = slots.to(DEV), positions.to(DEV), table(50, rot) if rot else None
+
+    def run(step):
+        cache, data = empty_cache(pages, kv, page, dim, code), qkv.clone()
+        q, k, v = (x.view(T, -1, dim) for x in data.split([heads * dim, kv * dim, kv * dim], 1))
+        o = None if not heads else q if in_place else torch.full((T, heads, dim), 7.0, device=DEV, dtype=dt)
+        for t in range(0, T, step):
+            c = slice(t, t + step)
+            ops.ls_kvq_append(*cache, k[c], v[c], positions[c] if rot else None, slots[c], cs, q=q[c] if heads else None,
+                              q_out=o[c] if heads else None, style=style)
+        return cache, o
+
+    (large, q_large), (small, q_small) = run(T), run(500)
+    for x, y in zip(raw(large), raw(small)):
+        assert same(x, y)
+    if heads:
+        assert same(q_large, q_small)
+    # read, the slots twice over so that there is enough of it
+    n = (36 << 20) // (2 * kv * dim * dt.itemsize) + 1
+    at = slots.repeat(n // T + 1)[:n].contiguous()
+    outs = []
+    for step in (n, 500):
+        out = [torch.full((n, kv, dim), 9.0, dtype=dt, device=DEV) for _ in range(2)]
+        for t in range(0, n, step):
+            ops.ls_kvq_read(*large, at[t:t + step], out[0][t:t + step], out[1][t:t + step])
+        outs.append(out)
+    for x, y in zip(*outs):
+        assert same(x, y)   # the rows written are finite
+
+
 # ---- attention -------------------------------------------------------------------------------------
 def check_attend(ops, *, lens, code="fp4", heads=4, kv=2, dim=64, dt=torch.float16, prefix=0, n_q=1, page=16, layout="head", max_len=None,
                  bad_pages=False, seed=0, std=1.0, poison=True, stride_pad=0, spare=0, touch=None, key_std=1.0):
