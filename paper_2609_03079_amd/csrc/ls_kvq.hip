@@ -9,11 +9,12 @@
 namespace ls {
 namespace {
 
-// Calls whose data is more than the eight L2 caches hold together (4 MiB each) pass them by, and leave a page's tokens to
-// one of them: writing 8192 tokens (64 query heads, 8 key heads of 128, FP4) took 73 us and takes 46, of which 15 by loads and
-// stores that are not kept, 5 by lanes of four heads; reading 32768 tokens of 8 heads (FP8) 51 and 30 (tokens by two 4, stores 15, one
-// L2 for a page 3).  Smaller ones stay in the caches for whoever reads them next.
-constexpr int64_t kStreamBytes = 32 << 20;
+// Calls with more data than this pass the caches by and leave a page's tokens to one die: writing 8192 tokens (64 query
+// heads, 8 key heads of 128, FP4) took 73 us and takes 48, of which 15 by loads and stores that are not kept, 5 by lanes of four
+// heads; reading 32768 tokens of 8 heads (FP8) 51 and 30 (tokens by two 4, stores 15, one die for a page 3).  At the border 512
+// tokens written and read, 20 buffers in turn, take 12.9 and 10.7, 1024 read 8.8 and 6.1, and 512 read from one buffer 5.1 and 4.7.
+// What a die's L2 kept would be no nearer to the next kernel, which runs on all eight.
+constexpr int64_t kStreamBytes = 4 << 20;
 
 // Block b of n, such that runs of 64 are on one die (they take blocks in turn): tokens of a page share cache lines.
 __device__ inline int64_t in_runs(uint32_t b, uint32_t n) {
