@@ -10,7 +10,9 @@
 //
 // Only the row that the token comes from is read, or the two.  They are cut into parts, so that the few sequences of a step fill
 // the card: a first launch adds the parts (bound by reading them), a second finds the part that u sum(w) falls into and the
-// token in it.  With as many sequences as fill the card by themselves, or rows that are one part, a workgroup does both.
+// token in it.  With as many sequences as fill the card by themselves, or rows of up to 8192 tokens, a workgroup does both: a launch
+// less (4000 tokens 9.5 -> 7.5 us, where 16000 would go from 9.1 to 10.1).  Measured: 1 x 4 drafts of 32000 (fp32) 9.0 us, most of it
+// the two launches; 64 x 7 of 131072 20 us, of which the sums 14 (4.8 TB/s of the rows that they read).
 #include <algorithm>
 
 #include "ls_device.h"
@@ -50,7 +52,7 @@ struct Weights {
     // This thread's share of the sum over [begin, end): every N-th token, or every N-th 16 bytes of them (vec; begin is a multiple).
     template <int N>
     __device__ inline double sum(int thread, int begin, int end, bool vec) const {
-        constexpr int V = 16 / sizeof(T), U = 4;
+        constexpr int V = 16 / sizeof(T), U = 16 / V;  // a wave's 1024 tokens at a time
         double s = 0.0;
         int t = begin;
         if (vec) {
@@ -330,10 +332,12 @@ hipError_t verify_type(VerifyP p, void* ws, size_t ws_bytes, int n_cu, hipStream
     const int64_t el = 16 / (int64_t)sizeof(T);
     p.vec = aligned(a.target, 16) && a.target_seq_stride % el == 0 && a.target_token_stride % el == 0 &&
             (!a.draft || (aligned(a.draft, 16) && a.draft_seq_stride % el == 0 && a.draft_token_stride % el == 0));
-    // Parts of 1024 tokens, larger where the workspace or a thread's share of them (8) would not do.
+    // Parts of 1024 tokens, larger where they are more waves than run in two rounds (256 rows of 128256 in bf16:
+    // 52 -> 33 us), or the workspace or a thread's share of them (8) would not do.
     const int64_t bytes = (int64_t)a.n_seqs * 8;  // what a part of each row takes; the decisions as much once
-    const int64_t chunks = std::min({ceil_div(a.vocab, 1024), (int64_t)ws_bytes / bytes - 1, (int64_t)(8 * kPart)});
-    if (a.n_seqs < 2 * n_cu && chunks > 1) {
+    const int64_t at_once = std::max<int64_t>(1, 64 * n_cu / a.n_seqs);
+    const int64_t chunks = std::min({ceil_div(a.vocab, 1024), at_once, (int64_t)ws_bytes / bytes - 1, (int64_t)(8 * kPart)});
+    if (a.n_seqs < 2 * n_cu && a.vocab > 8192 && chunks > 1) {
         p.chunk = (int)round_up((size_t)ceil_div(a.vocab, chunks), 1024);
         p.chunks = (int)ceil_div(a.vocab, p.chunk);
         p.sums = static_cast<double*>(ws);
