@@ -120,8 +120,9 @@ def test_every_number_of_accepted_tokens_and_ragged_batches(ops, V):
     assert got[1][8] == got[1][9] == -1 and np.all(got[0][8:10] == -1)
 
 
-def test_sampled_numbers_at_the_ends(ops):
-    S, V = 8, 3000
+@pytest.mark.parametrize("V", [3000, 11000])
+def test_sampled_numbers_at_the_ends(ops, V):
+    S = 8
     target, drafts, accept, sample, _ = case(S, 0, V, torch.float32, 3)
     target[:, :, 0], target[:, :, -1], target[:, :, 1500] = 0.0, 0.0, 0.0
     sample[:] = torch.tensor([0.0, -1.0, 1.0, 2.0, math.nan, math.inf, 1 - 2.0 ** -24, 1e-30])
@@ -129,8 +130,8 @@ def test_sampled_numbers_at_the_ends(ops):
     assert tokens[0, 0] == tokens[1, 0] == 1 and tokens[2, 0] == tokens[4, 0] == tokens[5, 0] == V - 2
 
 
-def test_weights_that_are_none(ops):
-    V = 700
+@pytest.mark.parametrize("V", [700, 9700])
+def test_weights_that_are_none(ops, V):
     target, drafts, accept, sample, draft = case(6, 2, V, torch.float32, 4)
     accept[:] = 1e30
     draft[0, 0] = target[0, 0]                     # nothing is left over: the target's own
@@ -151,9 +152,10 @@ def test_weights_that_are_none(ops):
     assert run(ops, target, drafts, accept, sample, draft)[0][0, 0] == 123
 
 
-def test_borders_are_decided_exactly(ops):
+@pytest.mark.parametrize("V", [4096, 16384])
+def test_borders_are_decided_exactly(ops, V):
     # u q = p exactly is a refusal, one step less of u an acceptance; equal weights: token floor(u V), in 64 bits
-    S, V = 64, 4096
+    S = 64
     p = torch.full((S, 2, V), 0.25, device=DEV)
     q = torch.full((S, 1, V), 0.5, device=DEV)
     drafts, sample = torch.zeros((S, 1), dtype=torch.int32, device=DEV), torch.arange(S, device=DEV) / S
@@ -166,19 +168,21 @@ def test_borders_are_decided_exactly(ops):
     assert [int(tokens[s, s % 2]) for s in range(S)] == want
 
 
-def test_strides_and_shared_rows(ops):
-    target, drafts, accept, sample, draft = case(4, 3, 500, torch.bfloat16, 9)
-    t = torch.zeros((4, 5, 520), dtype=torch.bfloat16, device=DEV)
-    t[:, 1:, 3:503] = target
-    d = torch.zeros((4, 3, 501), dtype=torch.bfloat16, device=DEV)
+@pytest.mark.parametrize("V", [500, 9100])
+def test_strides_and_shared_rows(ops, V):
+    target, drafts, accept, sample, draft = case(4, 3, V, torch.bfloat16, 9)
+    t = torch.zeros((4, 5, V + 20), dtype=torch.bfloat16, device=DEV)
+    t[:, 1:, 3:V + 3] = target
+    d = torch.zeros((4, 3, V + 1), dtype=torch.bfloat16, device=DEV)
     d[..., 1:] = draft
-    check(ops, t[:, 1:, 3:503], drafts, accept, sample, d[..., 1:])
-    check(ops, target[:1].expand(4, 4, 500), drafts, accept, sample, draft[:1].expand(4, 3, 500))   # one row for all
+    check(ops, t[:, 1:, 3:V + 3], drafts, accept, sample, d[..., 1:])
+    check(ops, target[:1].expand(4, 4, V), drafts, accept, sample, draft[:1].expand(4, 3, V))   # one row for all
 
 
-def test_large_vocabulary(ops):
+@pytest.mark.parametrize("S,V", [(5, 1 << 20), (600, 9001), (300, 20000), (40, 60001)])
+def test_large_vocabulary(ops, S, V):
     # against running sums in 64 bits: a number within 2^-40 of a border is not asked for
-    S, K, V = 5, 2, 1 << 20
+    K = 2
     target, drafts, accept, sample, draft = case(S, K, V, torch.float32, 11, spread=1.0)
     accept[:3], accept[3:] = 1e30, 0.0
     tokens, n = run(ops, target, drafts, accept, sample, draft)
@@ -219,10 +223,11 @@ def test_many_sequences(ops):
     assert torch.equal(tokens[:, 0].long(), (runs[None] <= sample.double()[:, None] * runs[-1]).sum(1)) and not n.any()
 
 
-def test_graph_replays_read_their_arguments_anew():
+@pytest.mark.parametrize("V", [5000, 12000])
+def test_graph_replays_read_their_arguments_anew(V):
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
-        target, drafts, accept, sample, draft = case(6, 3, 5000, torch.float32, 5)
+        target, drafts, accept, sample, draft = case(6, 3, V, torch.float32, 5)
         counts = ints([3, 2, 1, 0, 3, -1])
         tokens, n = torch.zeros((6, 4), dtype=torch.int32, device=DEV), torch.zeros(6, dtype=torch.int32, device=DEV)
         s.synchronize()
