@@ -224,8 +224,8 @@ typedef struct {
     int64_t scale_page_stride, scale_head_stride, scale_token_stride;
 } ls_kvq_cache;
 
-/* ls_kv_append into the quantised cache.  k, v, q and q_out are of `type` (LS_F32, LS_F16 or LS_BF16); keys are turned in fp32 and
- * quantised from there, values from what they are.  With top the largest magnitude of a group, its scale is the smallest
+/* ls_kv_append into the quantised cache.  k, v, q and q_out are of `type` (LS_F32, LS_F16 or LS_BF16); keys are turned in 64 bits and
+ * rounded once, to their codes; values from what they are; q_out is turned in fp32.  With top the largest magnitude of a group, its scale is the smallest
  * power of two with top < 7 * 2^e (LS_FP4) or 464 * 2^e (LS_FP8), no smaller than 2^-126 and no larger than leaves the largest
  * code finite in `type`; a code is the element over the scale, to nearest, ties to the even code, at most the largest code.
  * A group that holds an infinity or NaN gets the scale byte 255 and zeros for codes.  Slots, positions, q and q_out as in

@@ -93,6 +93,16 @@ __device__ inline float turn(float x, float y, float c, float s) {
     return r;
 }
 
+// The same for a key, which is rounded but once, to its code: the products are exact in 64 bits, their sum is off by 2^-53, and
+// what is inexact in fp32 is rounded to odd there, so that it lies on the side of every border between two codes or
+// scales that it was on.  (In fp32 a few of 8 million elements fall to the other side; time: nothing, the data's reading hides it.)
+__device__ inline float turn_key(float x, float y, float c, float s) {
+    const double d = __builtin_fma((double)y, (double)s, (double)x * (double)c);
+    const float f = (float)d;
+    const uint32_t toward_zero = __float_as_uint(f) - (__builtin_fabs((double)f) > __builtin_fabs(d) ? 1u : 0u);
+    return (double)f == d || !(__builtin_fabsf(f) < INFINITY) ? f : __uint_as_float(toward_zero | 1u);
+}
+
 // Elements e .. e + 7 of a head turned to their position.  VEC: whole vectors of them turn or do not, with partners
 // in one vector; otherwise element by element.
 template <typename T, bool VEC, bool PAIR>
@@ -105,8 +115,8 @@ __device__ inline void turned8(const ls_append_args& a, const float* cs, const v
         for (int i = 0; i < 8; i += 2) {
             if (!VEC && e + i >= a.rot_dim) break;
             const float co = cs[(e + i) / 2], si = cs[half + (e + i) / 2], l = x[i], m = x[i + 1];
-            x[i] = turn(l, m, co, -si);
-            x[i + 1] = turn(m, l, co, si);
+            x[i] = turn_key(l, m, co, -si);
+            x[i + 1] = turn_key(m, l, co, si);
         }
     } else if (VEC) {
         const bool second = e >= half;
@@ -115,7 +125,7 @@ __device__ inline void turned8(const ls_append_args& a, const float* cs, const v
         load8<float, true>(cs, second ? e - half : e, co);
         load8<float, true>(cs, second ? e : e + half, si);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = turn(x[i], y[i], co[i], second ? si[i] : -si[i]);
+        for (int i = 0; i < 8; ++i) x[i] = turn_key(x[i], y[i], co[i], second ? si[i] : -si[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -124,7 +134,7 @@ __device__ inline void turned8(const ls_append_args& a, const float* cs, const v
             const bool second = k >= half;
             const float y = (float)static_cast<const T*>(src)[from + (second ? k - half : k + half)];
             const float co = cs[second ? k - half : k], si = cs[second ? k : k + half];
-            x[i] = turn(x[i], y, co, second ? si : -si);
+            x[i] = turn_key(x[i], y, co, second ? si : -si);
         }
     }
 }
@@ -144,7 +154,14 @@ __device__ inline void turn_query(const KvqAppendP& p, const float* cs, int64_t 
             static_cast<T*>(a.q_out)[to + e] = static_cast<const T*>(a.q)[from + e];
         }
     } else if (VEC && PAIR) {
-        turned8<T, true, true>(a, cs, a.q, from, u * 8, x);
+        const auto c4 = load_pack<float, 4>(cs, u * 4), s4 = load_pack<float, 4>(cs, half + u * 4);
+        load8<T, true>(a.q, from + u * 8, x);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float l = x[i], m = x[i + 1];
+            x[i] = turn(l, m, c4.e[i / 2], -s4.e[i / 2]);
+            x[i + 1] = turn(m, l, c4.e[i / 2], s4.e[i / 2]);
+        }
         store8<T, true>(a.q_out, to + u * 8, x);
     } else if (VEC) {
         const int e = u * 8;

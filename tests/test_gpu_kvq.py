@@ -224,6 +224,28 @@ def test_append_at_the_borders(ops, code, dtype):
         assert same(torch.isnan(o), bad.repeat_interleave(32, -1)) and same(s[0, :, :3].transpose(0, 1) == 255, bad)
 
 
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("style", [0, 1])
+def test_turned_keys_are_rounded_once(ops, code, dtype, style):
+    """Codes and scales of turned keys by the definition from the angle's product in 64 bits, whose products of fp32 numbers are exact;
+    quarter turns of numbers between two codes put exact ties among them."""
+    dt, T, kv, dim, page = TYPES[dtype], 3001, 8, 128, 16
+    k = rand((T, kv, dim), 5, dt)
+    k[:64] = (torch.randint(-24, 25, (64, kv, dim), generator=torch.Generator().manual_seed(1)) / 4).to(dt).to(DEV)
+    cs = table(70, dim)
+    cs[60:], cs[62, :64], cs[63, 64:] = 0.0, 1.0, -1.0
+    at = torch.arange(T, dtype=torch.int32, device=DEV)
+    positions = at % 70
+    cache = empty_cache(T // page + 1, kv, page, dim, code)
+    ops.ls_kvq_append(*cache, k, k, positions, at, cs, style=style)
+    ref, _ = rope_ref(k, cs[positions.long()], dim, style)
+    rows, scales = packed(ref, code, dt)
+    pg, pl = at.long() // page, at.long() % page
+    assert same(cache[1][pg, :, pl], scales)
+    assert same(decoded(cache[0].view(torch.uint8)[pg, :, pl].view(cache[0].dtype), scales, dim), decoded(rows, scales, dim))
+
+
 def test_append_keeps_turned_keys_that_overflow_apart(ops):
     # keys near the end of float16 that grow beyond it when they turn are held as the largest number of their group's largest scale
     k = torch.full((1, 1, 64), 65504.0, dtype=torch.float16, device=DEV)
