@@ -144,6 +144,58 @@ __device__ __forceinline__ void by_grain(const AttendP& p, bool paged, Run run) 
         by_page(std::integral_constant<int, 8>{});
 }
 
+// Several query tokens: the last keys are not seen by all of them, and a weight of zero does not keep a value out that is no
+// number.  So such values of these keys are made zeros as they are widened, in shared memory (take_odd: a lane's N elements,
+// where its key is one of them; true in every lane if any lane had one), and added behind the loop, which they happen seldom to need, to the
+// sums of the rows that see them (add_odd: `add(key, d0, v)` with eight elements of each key from `from` that is `mine`).
+template <typename T, int N>
+__device__ __forceinline__ bool take_odd(T* at, bool late) {
+    // exponents of ones: infinities and NaN
+    constexpr uint32_t kOnes = std::is_same_v<T, _Float16> ? 0x7c00 : 0x7f80;
+    bool some = false;
+#pragma unroll
+    for (int j = 0; j < N; j += 8) {
+        const auto v = __builtin_bit_cast(u32x4a, *reinterpret_cast<const vec8<T>*>(at + j));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) some |= (v[i] & kOnes) == kOnes || (v[i] >> 16 & kOnes) == kOnes;
+    }
+    if (!__any(late && some)) return false;
+#pragma unroll 1
+    for (int j = 0; j < N; ++j)
+        if (late && !(fabsf((float)at[j]) < INFINITY)) at[j] = (T)0.f;
+    return true;
+}
+
+template <typename T, class C, typename Mine, typename Add>
+__device__ __forceinline__ void add_odd(const AttendP& p, const Item& it, int from, const uint8_t* v, const uint8_t* scales, Mine mine, Add add) {
+#pragma unroll 1
+    for (int key = from; key < it.end; ++key) {
+        const int id = it.table[key >> p.page_shift], place = key & ((1 << p.page_shift) - 1);
+        if (!mine(key) || (unsigned)id >= (unsigned)p.n_pages) continue;
+        const uint8_t* row = v + id * p.page_stride + place * p.token_stride;
+        const uint8_t* of_row = scales + id * p.s_page + place * p.s_token;
+#pragma unroll 1
+        for (int d0 = 0; d0 < p.D; d0 += 8) {
+            uint32_t w[C::kBits / 4];
+#pragma unroll
+            for (int i = 0; i < C::kBits / 4; ++i) w[i] = *reinterpret_cast<const uint32_t*>(row + d0 * C::kBits / 8 + i * 4);
+            add(key, d0, widened<C, T>(w, of_row[d0 / kGroup]));
+        }
+    }
+}
+
+// Those of four of the elements, the first or second, that are no numbers, zeros beside them and for a row that does not see them.
+template <typename T>
+__device__ __forceinline__ f32x4 odd_of(const vec8<T>& v, bool second, bool seen) {
+    f32x4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = second ? (float)v[4 + e] : (float)v[e];
+        if (!seen || fabsf(x[e]) < INFINITY) x[e] = 0.f;
+    }
+    return x;
+}
+
 constexpr int kThinPad = 8;  // elements
 
 // Up to 16 rows over codes.  The products run on the 16 x 16 x 32 instructions: half the scores, sums and
@@ -239,6 +291,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     T* v_put = vt + n * kPitch + g * kOwn;
     const T* v_get = vt + (4 * g + ((lane & 15) >> 2)) * kPitch + (lane & 3) * 4;
 
+    bool odd = false;  // MULTI: this wave took out values that are no numbers, of keys that not all tokens see
     auto use = [&](Codes& x, int key0) __attribute__((always_inline)) {
         const uint32_t valid = x.valid;
         const bool some = key0 + KT > full || ~valid != 0;  // keys that not every row sees
@@ -270,6 +323,8 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
 #pragma unroll
             for (int f = 0; f < NF; ++f)
                 *reinterpret_cast<vec8<T>*>(v_put + t * 16 * kPitch + f * 8) = widened<C, T>(&x.v[t][f * kOf8], x.vs[t][f * 8 / kGroup]);
+        if (MULTI && it.seq >= 0 && key0 + KT > full)
+            odd |= take_odd<T, kOwn>(v_put, key0 + n >= full) | take_odd<T, kOwn>(v_put + 16 * kPitch, key0 + 16 + n >= full);
         float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         top = pair_max<16>(top);
         top = pair_max<32>(top);
@@ -299,34 +354,8 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
             struct { s16x4 a, b; } both{a, b};
             return __builtin_bit_cast(vec8<T>, both);
         };
-        bool odd = false;
-        if (MULTI && it.seq >= 0 && key0 + KT > full) {  // as above: a weight of zero must keep out a value that is no number
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                const auto v = value(d);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) odd |= key0 + 16 * (j / 4) + 4 * g + j % 4 >= full && !(fabsf((float)v[j]) < INFINITY);
-            }
-        }
-        if (MULTI && __any(odd)) {
-#pragma unroll 1
-            for (int i = 0; i < p.n_q; ++i) {
-                const int seen = full_len + i;
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    auto v = value(d);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (key0 + 16 * (j / 4) + 4 * g + j % 4 >= seen) v[j] = (T)0.f;
-                    const f32x4 y = mma16(v, pr, o[d]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[d][e] = tk == i ? y[e] : o[d][e];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int d = 0; d < ND; ++d) o[d] = mma16(value(d), pr, o[d]);
-        }
+        for (int d = 0; d < ND; ++d) o[d] = mma16(value(d), pr, o[d]);
     };
     // While a tile is used, the codes of the next are on their way, and the page ids of the one behind it.
     // (A loop for each way to load: a branch inside would wait for the loads that each side has under way.)
@@ -349,6 +378,15 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     };
     if (key < it.end) {
         by_grain<kOwn>(p, page_mask >= 15, run);
+    }
+    if (MULTI && odd) {
+        auto own = [&](int key) { return ((key - it.begin) / KT & 1) == wave; };
+        add_odd<T, C>(p, it, max(it.begin, full), vbase, vsbase, own, [&](int key, int d0, const vec8<T>& v) __attribute__((always_inline)) {
+            const f32x4 x = odd_of<T>(v, g & 1, key < limit && (d0 >> 3 & 1) == g >> 1);
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                if (d0 / 16 == d) o[d] += x;
+        });
     }
     l = pair_sum<32>(pair_sum<16>(l));
 
@@ -516,7 +554,8 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
                              x.w, x.s);
         }
     };
-    auto put_values = [&](Values& x, T* buf) __attribute__((always_inline)) {
+    bool odd = false;  // MULTI: this wave took out values that are no numbers, of keys that not all tokens see
+    auto put_values = [&](Values& x, int key0, T* buf) __attribute__((always_inline)) {
         if (!__all(x.there)) {
 #pragma unroll
             for (int j = 0; j < ValueShare::kWords; ++j) x.w[j] = x.there ? x.w[j] : 0;
@@ -526,6 +565,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
         T* to = buf + (wave * 16 + vn) * kPitch + vg * (DP / 4);
 #pragma unroll
         for (int f = 0; f < DP / 32; ++f) *reinterpret_cast<vec8<T>*>(to + f * 8) = widened<C, T>(&x.w[f * kOf8], x.s[f * 8 / kGroup]);
+        if (MULTI && it.seq >= 0 && key0 + wave * 16 + 16 > full) odd |= take_odd<T, DP / 4>(to, key0 + wave * 16 + vn >= full);
     };
     auto clear = [&](Keys& x) __attribute__((always_inline)) {
         if (~x.valid == 0) return;
@@ -591,45 +631,11 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             if (f >= NF - kEarly) val[f - (NF - kEarly)] = value((f - (NF - kEarly)) / ND, (f - (NF - kEarly)) % ND);
             __builtin_amdgcn_sched_barrier(0);
         }
-        bool odd = false;
-        if (MULTI && it.seq >= 0 && key0 + 32 > full) {  // a weight of zero must keep out a value that is no number
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int t = 0; t < ND; ++t) {
-                    const auto v = value(kk, t);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        odd |= key0 + 16 * kk + 8 * (j / 4) + 4 * h + j % 4 >= full && !(fabsf((float)v[j]) < INFINITY);
-                }
-        }
-        if (MULTI && __any(odd)) {
-#pragma unroll 1
-            for (int i = 0; i < p.n_q; ++i) {
-                const int seen = full_len + i;
-#pragma unroll
-                for (int t = 0; t < ND; ++t) {
-                    __builtin_amdgcn_sched_barrier(0);  // one tile's operands at a time: registers
-                    f32x16 x = o[t];
-#pragma unroll
-                    for (int kk = 0; kk < 2; ++kk) {
-                        auto v = value(kk, t);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (key0 + 16 * kk + 8 * (j / 4) + 4 * h + j % 4 >= seen) v[j] = (T)0.f;
-                        x = mma(v, pr[kk], x);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[t][e] = tk == i ? x[e] : o[t][e];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2 * ND; ++i) {
-                if (i + kEarly < 2 * ND) val[i + kEarly] = value((i + kEarly) / ND, (i + kEarly) % ND);
-                o[i % ND] = mma(val[i], pr[i / ND], o[i % ND]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+        for (int i = 0; i < 2 * ND; ++i) {
+            if (i + kEarly < 2 * ND) val[i + kEarly] = value((i + kEarly) / ND, (i + kEarly) % ND);
+            o[i % ND] = mma(val[i], pr[i / ND], o[i % ND]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         s = after;
         __builtin_amdgcn_s_setprio(0);
@@ -647,7 +653,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
         fetch_values(GRAIN, PAGED, key, ids0.v, x);
         fetch_keys(GRAIN, PAGED, key, ids0.k[0], ka);
         fetch_keys(GRAIN, PAGED, key + 32, ids0.k[1], kb);
-        put_values(x, v0);
+        put_values(x, key, v0);
         f32x16 s{};
         clear(ka);
 #pragma unroll
@@ -664,7 +670,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             valid_a = ka.valid;
             fetch_keys(GRAIN, PAGED, key + KT + 32, ids1.k[1], kb);
             if (!idle_wave) use(s, valid_b, key + 32, now + 32 * kPitch, ka);
-            put_values(x, next);
+            put_values(x, key + KT, next);
             key += KT;
             ids1 = ids2;
         };
@@ -676,6 +682,25 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
         }
     };
     if (key < it.end) by_grain<DP / 4>(p, page_mask >= 15, run);
+    if (MULTI && it.seq >= 0) {
+        __shared__ int waves_odd[4];
+        if (lane == 0) waves_odd[wave] = odd;
+        landed();
+        if (waves_odd[0] | waves_odd[1] | waves_odd[2] | waves_odd[3]) {
+            auto all = [](int) { return true; };
+            add_odd<T, C>(p, it, max(it.begin, full), vbase, vsbase, all, [&](int key, int d0, const vec8<T>& v) __attribute__((always_inline)) {
+                const f32x4 x = odd_of<T>(v, h, key < limit);
+#pragma unroll
+                for (int t = 0; t < ND; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (d0 != t * 32 + i * 8) continue;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[t][i * 4 + e] += x[e];
+                    }
+            });
+        }
+    }
     l += other_half(l);
     if (!row_ok) return;
     const int64_t out_row = token * p.H + head;
@@ -712,8 +737,8 @@ enum Shapes { THIN, BROAD, BOTH };
 // Waves a SIMD that the registers are shared out for.
 template <int DP, Shapes S, bool MULTI, class C>
 constexpr int waves_of() {
-    if (S == THIN) return DP <= 64 ? (C::kBits == 4 && !MULTI ? 4 : 3) : DP <= 128 ? (C::kBits == 4 && !MULTI ? 3 : 2) : 1;
-    return DP <= 128 && (S == BOTH || !MULTI) ? 2 : 1;
+    if (S == THIN) return DP <= 64 ? (C::kBits == 4 ? 4 : 3) : DP <= 128 ? (C::kBits == 4 ? 3 : 2) : 1;
+    return DP <= 128 ? 2 : 1;
 }
 
 template <typename T, int DP, Shapes S, bool MULTI, class C>

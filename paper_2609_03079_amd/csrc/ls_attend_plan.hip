@@ -20,23 +20,22 @@ bool plan_attend_codes(const ls_kvq_cache& c, const ls_attend_args& a, size_t ws
     plan->suf_tiles = (int)ceil_div(suf_rows, plan->suf_wide ? 128 : 16);
     plan->alike = plan->pre_wide == plan->suf_wide;
     plan->together = false;
-    // TOKENS: broad workgroups of several tokens, one a compute unit.
-    enum Kind { THIN, BROAD, TOKENS };
+    enum Kind { THIN, BROAD };
     const Kind pre_kind = plan->pre_wide ? BROAD : THIN;
-    const Kind suf_kind = !plan->suf_wide ? THIN : a.n_q > 1 && a.max_len ? TOKENS : BROAD;
+    const Kind suf_kind = plan->suf_wide ? BROAD : THIN;
     // workgroups that run at once on a compute unit, by registers
-    const int thin_cu = dp == 64 ? (bits == 4 && a.n_q == 1 ? 8 : 6) : dp == 128 ? (bits == 4 && a.n_q == 1 ? 6 : 4) : 2;
-    const int broad_cu = dp <= 128 ? 2 : 1;
+    const int thin_cu = dp == 64 ? (bits == 4 ? 8 : 6) : dp == 128 ? (bits == 4 ? 6 : 4) : 2;
+    const int broad_cu = dp == 64 ? 3 : dp == 128 ? 2 : 1;
     // Time of a workgroup among others on its compute unit (us): a start and an end, and the keys.  Thin: the wave's own chain and
     // the unit's share of the memory (5.3 TB/s), which overlap but for the loads that a lone wave has not in flight.  Broad: as
     // measured with the unit full.
     const double key_bytes = 2.0 * ((double)c.head_dim * bits / 8 + (double)ceil_div(c.head_dim, 32));
     auto item_us = [&](Kind kind, int64_t chunk, int64_t at_once) {
         if (kind == THIN) return 4.5 + chunk * std::hypot(0.0118 * (dp + 128) / 256, at_once * key_bytes / (5.3e6 / n_cu));
-        return 4.0 + chunk * dp / 128.0 * (kind == TOKENS ? 0.038 : 0.040);
+        return 4.0 + chunk * dp / 128.0 * 0.040;
     };
     auto run_us = [&](Kind kind, int64_t chunk, int64_t items) {
-        const int64_t per_cu = kind == THIN ? thin_cu : kind == BROAD ? broad_cu : 1, slots = per_cu * n_cu, rest = items % slots;
+        const int64_t per_cu = kind == THIN ? thin_cu : broad_cu, slots = per_cu * n_cu, rest = items % slots;
         return (items / slots) * item_us(kind, chunk, per_cu) + (rest ? item_us(kind, chunk, ceil_div(rest, n_cu)) : 0.0);
     };
     // parts are written, and read by the join, 16 of a row at a time
@@ -66,7 +65,7 @@ bool plan_attend_codes(const ls_kvq_cache& c, const ls_attend_args& a, size_t ws
     if (!a.prefix_len) {
         plan->pre_chunk = plan->suf_chunk = choose(suf_kind, 0, 0, n_suf, a.max_len);
     } else {
-        // one after the other, or in one launch of one shape (where several tokens are broad, by their kernel)
+        // one after the other, or in one launch of one shape
         plan->pre_chunk = choose(pre_kind, n_pre, a.prefix_len, 0, 0);
         double apart = least + 2.0;
         plan->suf_chunk = choose(suf_kind, 0, 0, n_suf, a.max_len);
