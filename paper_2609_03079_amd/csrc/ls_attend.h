@@ -51,6 +51,8 @@ struct AttendP {
     const uint8_t* k_scale;                          // codes only
     const uint8_t* v_scale;
     int64_t s_page, s_head, s_token;
+    int near_units;                                  // sequences times parts whose heads are near each other; 0: heads are apart
+    Div by_near;                                     // eight units' share of workgroups on a die
     int n_pages, page_shift;
     const int32_t* prefix_pages;
     const int32_t* pages;

@@ -144,6 +144,21 @@ __device__ __forceinline__ void by_grain(const AttendP& p, bool paged, Run run) 
         by_page(std::integral_constant<int, 8>{});
 }
 
+// Where a token's heads follow each other in a page, rows of codes and scales are smaller than the cache lines that they share: the
+// heads of a part then run on one die (workgroups take the eight in turn) and read the lines once.  Of the prefix a die has
+// an eighth of the parts and heads; of the sequences every eighth part of each, another one of the next.
+__device__ inline int near(const AttendP& p, bool prefix, int b) {
+    if (!p.near_units) return b;
+    const int eighth = b >> 3, die = b & 7;
+    if (prefix) {
+        const int tiles = p.plan.pre_tiles, turn = p.by_pre_tiles.of(eighth), group = die * p.by_pre_tiles.of(p.pre_items >> 3) + turn;
+        return ((group >> 3) * tiles + eighth - turn * tiles) * 8 + (group & 7);
+    }
+    const int round = p.by_near.of(eighth);
+    if (round * 8 + 8 > p.near_units) return b;
+    return (round * 8 + ((die - round) & 7)) * p.by_near.d + eighth - round * p.by_near.d;
+}
+
 // Several query tokens: the last keys are not seen by all of them, and a weight of zero does not keep a value out that is no
 // number.  So such values of these keys are made zeros as they are widened, in shared memory (take_odd: a lane's N elements,
 // where its key is one of them; true in every lane if any lane had one), and added behind the loop, which they happen seldom to need, to the
@@ -207,7 +222,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     constexpr int NW = 2, KT = 32, kStep = NW * KT, NF = DP / 32, ND = DP / 16;
     constexpr int kOwn = DP / 4, kWords = kOwn * C::kBits / 32, kOf8 = C::kBits / 4, kScales = kOwn > kGroup ? kOwn / kGroup : 1;
     Item it;
-    if (!item_of<16>(p, prefix, b, &it)) return;
+    if (!item_of<16>(p, prefix, near(p, prefix, b), &it)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
 
@@ -454,7 +469,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
     using KeyShare = Share<C, DP / 2>;
     using ValueShare = Share<C, DP / 4>;
     Item it;
-    if (!item_of<128>(p, prefix, b, &it)) return;
+    if (!item_of<128>(p, prefix, near(p, prefix, b), &it)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, h = lane >> 5;    // of keys, and of scores: row n of 32
     const int vn = lane & 15, vg = lane >> 4;  // of values, as they are widened
@@ -778,6 +793,8 @@ hipError_t attend_codes(const ls_kv_cache& shape, const ls_kvq_cache& c, const l
                         hipStream_t st) {
     AttendP p = attend_params(shape, a, plan, ws);
     p.k_scale = c.k_scale, p.v_scale = c.v_scale;
+    p.by_near = Div(p.KV * plan.suf_tiles);
+    p.near_units = c.n_kv_heads > 1 && c.head_stride < c.token_stride ? p.S * std::max(plan.suf_parts, 1) : 0;
     p.s_page = c.scale_page_stride, p.s_head = c.scale_head_stride, p.s_token = c.scale_token_stride;
     auto go = [&](Shapes s, int pre_items, int suf_items) {
         p.pre_items = pre_items;
