@@ -51,8 +51,6 @@ struct AttendP {
     const uint8_t* k_scale;                          // codes only
     const uint8_t* v_scale;
     int64_t s_page, s_head, s_token;
-    int near_units;                                  // sequences times parts whose heads are near each other; 0: heads are apart
-    Div by_near;                                     // eight units' share of workgroups on a die
     int n_pages, page_shift;
     const int32_t* prefix_pages;
     const int32_t* pages;
@@ -64,6 +62,8 @@ struct AttendP {
     float c;                 // scale log2(e): the softmax runs in powers of two
     AttendPlan plan;
     int pre_items, suf_items;  // workgroups of this launch
+    int near_units;          // sequences times parts whose heads are near each other (codes only); 0: heads are apart
+    Div by_near;             // eight units' workgroups, over eight
     int parts;               // partial results per row
     bool direct;             // a row has one part, which is the result
     float* part;             // [rows][parts][D]

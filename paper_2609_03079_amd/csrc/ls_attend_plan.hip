@@ -32,7 +32,7 @@ bool plan_attend_codes(const ls_kvq_cache& c, const ls_attend_args& a, size_t ws
     const double key_bytes = 2.0 * ((double)c.head_dim * bits / 8 + (double)ceil_div(c.head_dim, 32));
     auto item_us = [&](Kind kind, int64_t chunk, int64_t at_once) {
         if (kind == THIN) return 4.5 + chunk * std::hypot(0.0118 * (dp + 128) / 256, at_once * key_bytes / (5.3e6 / n_cu));
-        return 4.0 + chunk * dp / 128.0 * 0.040;
+        return 4.0 + chunk * (dp == 64 ? 0.056 : dp == 128 ? 0.044 : 0.088);
     };
     auto run_us = [&](Kind kind, int64_t chunk, int64_t items) {
         const int64_t per_cu = kind == THIN ? thin_cu : broad_cu, slots = per_cu * n_cu, rest = items % slots;
@@ -40,14 +40,15 @@ bool plan_attend_codes(const ls_kvq_cache& c, const ls_attend_args& a, size_t ws
     };
     // parts are written, and read by the join, 16 of a row at a time
     auto join_us = [&](int64_t parts) { return parts * 2.0 * part_bytes / 5e6 + 0.6 * ceil_div(parts, 16); };
-    // Chunks of whole tiles, at most half of kMaxParts parts and half of the workspace for each of prefix and sequences.
+    // Chunks of whole tiles; prefix and sequences, where there are both, have half of kMaxParts and of the workspace each.
+    const int shares = a.prefix_len && a.max_len ? 2 : 1;
     double least = 0;
     auto choose = [&](Kind kind, int64_t n_pre, int64_t pre_keys, int64_t n_suf, int64_t suf_keys) {
         int64_t best = 0;
         const int64_t most = round_up((size_t)std::max<int64_t>(std::max(pre_keys, suf_keys), 1), 64);
         for (int64_t chunk = 64;; chunk = std::min(most, chunk + std::max<int64_t>(64, chunk / 16 / 64 * 64))) {
             const int64_t pp = ceil_div(pre_keys, chunk), sp = ceil_div(suf_keys, chunk), items = n_pre * pp + n_suf * sp;
-            const bool fits = pp <= kMaxParts / 2 && sp <= kMaxParts / 2 && std::max(pp, sp) * part_bytes <= (int64_t)ws_bytes / 2 &&
+            const bool fits = std::max(pp, sp) <= kMaxParts / shares && std::max(pp, sp) * part_bytes <= (int64_t)ws_bytes / shares &&
                               (n_pre + 8) * (pp + 8) + n_suf * sp < (int64_t)1 << 24;  // 2^32 threads of a launch
             if (fits) {
                 const double t = run_us(kind, chunk, items) + join_us(pp + sp);
