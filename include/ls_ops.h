@@ -225,16 +225,17 @@ typedef struct {
 } ls_kvq_cache;
 
 /* ls_kv_append into the quantised cache.  k, v, q and q_out are of `type` (LS_F32, LS_F16 or LS_BF16); keys are turned in 64 bits and
- * rounded once, to their codes; values from what they are; q_out is turned in fp32.  With top the largest magnitude of a group, its scale is the smallest
- * power of two with top < 7 * 2^e (LS_FP4) or 464 * 2^e (LS_FP8), no smaller than 2^-126 and no larger than leaves the largest
+ * rounded once, to their codes; values from what they are; q_out is turned in fp32.  With top the largest magnitude of a
+ * group, its scale is the smallest power of two with top < 7 * 2^e (LS_FP4) or 464 * 2^e (LS_FP8), no smaller than 2^-126 and no larger than leaves the largest
  * code finite in `type`; a code is the element over the scale, to nearest, ties to the even code, at most the largest code.
  * A group that holds an infinity or NaN gets the scale byte 255 and zeros for codes.  Slots, positions, q and q_out as in
- * ls_kv_append (q_out may be q itself). */
+ * ls_kv_append (q_out may be q itself); of two tokens with one slot any group's codes and scale may stay. */
 ls_status ls_kvq_append(ls_ops* ctx, const ls_kvq_cache* cache, ls_dtype type, const ls_append_args* a);
 
 /* Reads the keys and values of tokens back: k[t] = the row of slots[t], in `type`, rounded once (exact in LS_F32; in the
  * 16-bit types wherever a value is inside their range).  slots: dev int32 [n_tokens]; a token whose slot is
- * outside the cache leaves its rows as they were.  k, v: [n_tokens, n_kv_heads, head_dim]. */
+ * outside the cache leaves its rows as they were.  k, v: [n_tokens, n_kv_heads, head_dim], whose rows
+ * must not overlap. */
 typedef struct {
     int32_t n_tokens;
     ls_dtype type; /* LS_F32, LS_F16 or LS_BF16 */
@@ -263,7 +264,8 @@ ls_status ls_kvq_attend(ls_ops* ctx, const ls_kvq_cache* cache, ls_dtype type, c
  * target: [n_seqs, n_drafts + 1, vocab], draft: [n_seqs, n_drafts, vocab] of `type` (LS_F32, LS_F16, LS_BF16), rows contiguous; draft
  * NULL: q is one at the drafted token (a draft without chance).  drafts: int32 [n_seqs, n_drafts]; counts: int32 [n_seqs] or NULL:
  * sequence s has min(counts[s], n_drafts) drafts; below 0 it is an idle slot: tokens -1, n_accepted -1.
- * accept: fp32 [n_seqs, n_drafts]; sample: fp32 [n_seqs]; tokens: int32 [n_seqs, n_drafts + 1]; n_accepted: int32 [n_seqs]; all on the device.
+ * accept: fp32 [n_seqs, n_drafts]; sample: fp32 [n_seqs]; tokens: int32 [n_seqs, n_drafts + 1]; n_accepted: int32 [n_seqs]; all on the
+ * device, and neither output overlaps an input.
  * 0 <= n_drafts <= 63 (0: tokens drawn from p); 1 <= vocab <= 2^30; n_seqs 0 does nothing. */
 typedef struct {
     int32_t n_seqs, n_drafts, vocab;

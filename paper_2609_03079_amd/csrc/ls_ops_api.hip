@@ -139,6 +139,13 @@ ls_status check_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a
     return LS_OK;
 }
 
+// No two rows of n elements overlap, `a` of them that are by_a apart in each of `b` that are by_b apart, or the other way round.
+bool rows_apart(int64_t a, int64_t by_a, int64_t b, int64_t by_b, int64_t n) {
+    if (a == 1 || b == 1) return a == b || (a == 1 ? by_b : by_a) >= n;
+    const int64_t outer = std::max(by_a, by_b), inner = std::min(by_a, by_b), of_inner = by_a < by_b ? a : b;
+    return inner >= n && (outer - n) / inner >= of_inner - 1;
+}
+
 // Launches an attention that was found right, in as many pieces as it takes.
 template <typename Plan, typename Launch>
 ls_status attend_pieces(ls_ops* c, ls_dtype type, const ls_attend_args* a, const char* what, Plan plan_of, Launch launch) {
@@ -298,7 +305,7 @@ ls_status ls_kvq_read(ls_ops* c, const ls_kvq_cache* kv, const ls_kvq_read_args*
     LS_REQUIRE(a->k && a->v && a->slots, "k, v or slots is NULL");
     for (int64_t s : {a->k_token_stride, a->k_head_stride, a->v_token_stride, a->v_head_stride}) LS_REQUIRE(s >= 0, "negative stride");
     for (const auto& x : {std::make_pair(a->k_token_stride, a->k_head_stride), std::make_pair(a->v_token_stride, a->v_head_stride)})
-        LS_REQUIRE((kv->n_kv_heads == 1 || x.second >= kv->head_dim) && (a->n_tokens == 1 || x.first >= kv->head_dim), "k or v: rows overlap");
+        LS_REQUIRE(rows_apart(a->n_tokens, x.first, kv->n_kv_heads, x.second, kv->head_dim), "k or v: rows overlap");
     LS_REQUIRE(element_aligned(a->k, a->type) && element_aligned(a->v, a->type) && ls::aligned(a->slots, 4), "a pointer is not aligned to its type");
     return launched(c, ls::launch_kvq_read(*kv, *a, c->stream), "ls_kvq_read");
 }
