@@ -213,9 +213,11 @@ __device__ __forceinline__ f32x4 odd_of(const vec8<T>& v, bool second, bool seen
 
 constexpr int kThinPad = 8;  // elements
 
-// Up to 16 rows over codes.  The products run on the 16 x 16 x 32 instructions: half the scores, sums and
-// query operands a lane of the narrow shape, which leaves registers for three waves a SIMD (and the codes need no shared memory on
-// their way).  A lane takes a quarter of a key's row, straight from the cache: key n of the first 16 of a tile and of the
+// Up to 16 rows over codes.  Bound by memory where there are waves enough, by a wave's chain of loads, products and exponentials
+// (12 ns a key of 128) where there are few: 4 sequences of 100001 keys (32 / 8 heads of 128, FP4) take 82 us, 5.3 TB/s (its loads alone 82), 1000
+// keys of 32 heads 5.8.  Two waves take 32 keys each in turn.  The products run on the 16 x 16 x 32 instructions, which need half the scores, sums
+// and query operands a lane that tiles of 32 rows do: 84 registers, three waves a SIMD, and in place of those tiles 8 sequences behind 7901
+// keys 19.4 -> 17.0 us, 16 x 8 tokens of 2000 keys 35.6 -> 23.9.  A lane takes a quarter of a key's row, straight from the cache: key n of the first 16 of a tile and of the
 // second, elements g DP / 4 and on; its scores are those of keys 16 t + 4 g + i and query row n.
 template <typename T, int DP, bool MULTI, class C>
 __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b, T* v0, float (*wave_ml)[2][32]) {
@@ -460,7 +462,10 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
 
 constexpr int kBroadPad = 16;  // elements
 
-// Tiles of 128 query rows, 32 a wave, on the 32 x 32 x 16 instructions.  Each wave widens the keys it multiplies by itself: 32 at a
+// Tiles of 128 query rows, 32 a wave, on the 32 x 32 x 16 instructions.  Bound by vector and matrix instructions: 64 sequences behind
+// 32768 keys (64 / 8 heads of 128, FP4) take 101 us, 680 TFLOP/s, the matrix units busy for 28 us of them and the vector units, which
+// widen codes and take 134 million exponentials, for about 45; the two seldom at once, as a wave's parts depend on each other and two waves
+// a SIMD are all that the registers hold.  Each wave widens the keys it multiplies by itself: 32 at a
 // time, a half of their row a lane, the scores of the next 32 computed while the exponentials of these are.  The values of 64 keys are
 // widened by the four waves together, 16 rows each, for all of them.
 template <typename T, int DP, bool MULTI, class C>
@@ -745,7 +750,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
     }
 }
 
-// Which shapes a launch holds.  BOTH: a broad prefix beside thin sequences, eight workgroups of one after eight of the other (one
+// Which shapes a launch holds (rows of up to 32 are thin: broad ones at 32 rows would leave three waves of four without work).  BOTH: a broad prefix beside thin sequences, eight workgroups of one after eight of the other (one
 // for each XCD).
 enum Shapes { THIN, BROAD, BOTH };
 
