@@ -14,7 +14,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liblsffn.so")
 BINDING = os.path.join(HERE, "_lsops" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["ls_api.hip", "ls_kernels.hip", "ls_decode.hip", "ls_mfma.hip", "ls_hash.hip", "ls_stage.hip",
-           "ls_ops_api.hip", "ls_rows.hip", "ls_linear.hip", "ls_attend.hip", "ls_attend_plan.hip", "ls_attend_fp4.hip", "ls_attend_fp8.hip",
+           "ls_ops_api.hip", "ls_rows.hip", "ls_linear.hip", "ls_attend.hip", "ls_attend_plan.hip", "ls_attend_fp4_f16.hip", "ls_attend_fp4_bf16.hip",
+           "ls_attend_fp8_f16.hip", "ls_attend_fp8_bf16.hip",
            "ls_kvq.hip", "ls_verify.hip"]
 
 HIPCC_FLAGS = [

@@ -1,4 +1,5 @@
-// ls_attend_codes.h - attention over keys and values held in 4 or 8 bits (ls_attend_fp4.hip, ls_attend_fp8.hip).
+// ls_attend_codes.h - attention over keys and values held in 4 or 8 bits (ls_attend_fp4_f16.hip and so on,
+// a file for each code and type: they take minutes to compile).
 //
 // The mathematics and the parts are those of ls_attend.hip; the products run transposed on 16-bit operands, into which the codes are widened
 // (two by one instruction, exactly, their group's power of two among its operands).  What differs is where that happens.  A key's

@@ -318,8 +318,9 @@ ls_status ls_kvq_attend(ls_ops* c, const ls_kvq_cache* kv, ls_dtype type, const 
     if ((st = check_attend(c, &shape, a, "ls_kvq_attend takes f16 and bf16 queries")) != LS_OK || a->n_seqs == 0) return st;
     auto plan = [&](const ls_attend_args& b, ls::AttendPlan* out) { return ls::plan_attend_codes(*kv, b, c->ws_bytes, c->n_cu, out); };
     return attend_pieces(c, type, a, "ls_kvq_attend", plan, [&](const ls_attend_args& b, const ls::AttendPlan& plan) {
-        return kv->code == LS_FP4 ? ls::launch_attend_fp4(*kv, type, b, plan, c->ws, c->stream)
-                                  : ls::launch_attend_fp8(*kv, type, b, plan, c->ws, c->stream);
+        const bool half = type == LS_F16;
+        return kv->code == LS_FP4 ? (half ? ls::launch_attend_fp4_f16 : ls::launch_attend_fp4_bf16)(*kv, b, plan, c->ws, c->stream)
+                                  : (half ? ls::launch_attend_fp8_f16 : ls::launch_attend_fp8_bf16)(*kv, b, plan, c->ws, c->stream);
     });
 }
 

@@ -36,14 +36,12 @@ bool plan_attend(const ls_kv_cache& c, const ls_attend_args& a, size_t ws_bytes,
 hipError_t launch_attend(const ls_kv_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws,
                          hipStream_t st);
 
-// ---- a cache in 4 or 8 bits (ls_kvq.hip, ls_attend_plan.hip, ls_attend_fp4.hip, ls_attend_fp8.hip)
+// ---- a cache in 4 or 8 bits (ls_kvq.hip, ls_attend_plan.hip, ls_attend_fp4_f16.hip and so on)
 hipError_t launch_kvq_append(const ls_kvq_cache& c, ls_dtype type, const ls_append_args& a, hipStream_t st);
 hipError_t launch_kvq_read(const ls_kvq_cache& c, const ls_kvq_read_args& a, hipStream_t st);
 bool plan_attend_codes(const ls_kvq_cache& c, const ls_attend_args& a, size_t ws_bytes, int n_cu, AttendPlan* plan);
-hipError_t launch_attend_fp4(const ls_kvq_cache& c, ls_dtype type, const ls_attend_args& a, const AttendPlan& plan, void* ws,
-                             hipStream_t st);
-hipError_t launch_attend_fp8(const ls_kvq_cache& c, ls_dtype type, const ls_attend_args& a, const AttendPlan& plan, void* ws,
-                             hipStream_t st);
+using LaunchAttendCodes = hipError_t(const ls_kvq_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws, hipStream_t st);
+LaunchAttendCodes launch_attend_fp4_f16, launch_attend_fp4_bf16, launch_attend_fp8_f16, launch_attend_fp8_bf16;
 // The shape of a quantised cache, its codes' places and strides in bytes, for the calls that take either.
 inline ls_kv_cache shape_of(const ls_kvq_cache& c, ls_dtype type) {
     return {c.k, c.v, type, c.n_pages, c.page_size, c.n_kv_heads, c.head_dim, c.page_stride, c.head_stride, c.token_stride};

@@ -38,12 +38,10 @@ static hipError_t planned(const ls_kvq_cache& c, const ls_attend_args& a, const 
                       (int64_t)p.pre_tiles * (p.pre_wide ? 128 : 16) >= rows_pre && (int64_t)p.suf_tiles * (p.suf_wide ? 128 : 16) >= rows_suf;
     return good ? counted() : hipErrorInvalidValue;
 }
-hipError_t launch_attend_fp4(const ls_kvq_cache& c, ls_dtype, const ls_attend_args& a, const AttendPlan& p, void*, hipStream_t) {
-    return planned(c, a, p);
-}
-hipError_t launch_attend_fp8(const ls_kvq_cache& c, ls_dtype, const ls_attend_args& a, const AttendPlan& p, void*, hipStream_t) {
-    return planned(c, a, p);
-}
+hipError_t launch_attend_fp4_f16(const ls_kvq_cache& c, const ls_attend_args& a, const AttendPlan& p, void*, hipStream_t) { return planned(c, a, p); }
+hipError_t launch_attend_fp4_bf16(const ls_kvq_cache& c, const ls_attend_args& a, const AttendPlan& p, void*, hipStream_t) { return planned(c, a, p); }
+hipError_t launch_attend_fp8_f16(const ls_kvq_cache& c, const ls_attend_args& a, const AttendPlan& p, void*, hipStream_t) { return planned(c, a, p); }
+hipError_t launch_attend_fp8_bf16(const ls_kvq_cache& c, const ls_attend_args& a, const AttendPlan& p, void*, hipStream_t) { return planned(c, a, p); }
 hipError_t launch_verify(const ls_verify_args&, void*, size_t, int, hipStream_t) { return counted(); }
 }  // namespace ls
 
