@@ -96,8 +96,9 @@ struct Share {
     }
     // GRAIN: elements that are there or past the row's end together, the whole share or 16 or 8 (and loaded together).
     // SHARED: the addresses are the wave's, the offsets its lanes'.
-    template <typename G, typename S>
-    __device__ __forceinline__ void load(G, S, const uint8_t* codes, const uint8_t* scales, uint32_t c_n, uint32_t s_n, uint32_t (&w)[kWords],
+    // ONCE: codes that the caches need not keep.
+    template <typename G, typename S, typename O>
+    __device__ __forceinline__ void load(G, S, O, const uint8_t* codes, const uint8_t* scales, uint32_t c_n, uint32_t s_n, uint32_t (&w)[kWords],
                                 uint8_t (&s)[kScales]) const {
         constexpr int kTake = G::value * C::kBits / 32;  // words together
         const uint8_t* from = S::value ? wave_address(codes) : codes;
@@ -115,7 +116,7 @@ struct Share {
             } else {
 #pragma unroll
                 for (int k = 0; k < kTake; k += 4) {
-                    const u32x4a v = *(gwords4)(at + k * 4);
+                    const u32x4a v = O::value ? __builtin_nontemporal_load((gwords4)(at + k * 4)) : *(gwords4)(at + k * 4);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) w[i + k + j] = v[j];
                 }
@@ -124,13 +125,17 @@ struct Share {
     }
 };
 
+// Pages of 16 tokens or more whose offsets 32 bits hold, and a page's.
+__device__ inline bool whole_pages(const AttendP& p, bool paged) {
+    return paged && (p.token_stride << p.page_shift) < (int64_t)1 << 31 && (p.s_token << p.page_shift) < (int64_t)1 << 31 &&
+           p.page_stride < (int64_t)1 << 32 && p.s_page < (int64_t)1 << 32;
+}
+
 // Calls run(GRAIN, PAGED) with the grain of shares of OWN elements.  (A loop for each: a branch inside a loop would wait for the
 // loads that either side has under way.)
 template <int OWN, typename Run>
 __device__ __forceinline__ void by_grain(const AttendP& p, bool paged, Run run) {
-    // 32 bits hold the offsets within a page, and a page
-    paged = paged && (p.token_stride << p.page_shift) < (int64_t)1 << 31 && (p.s_token << p.page_shift) < (int64_t)1 << 31 &&
-            p.page_stride < (int64_t)1 << 32 && p.s_page < (int64_t)1 << 32;
+    paged = whole_pages(p, paged);
     auto by_page = [&](auto GRAIN) __attribute__((always_inline)) {
         if (paged)
             run(GRAIN, std::true_type{});
@@ -276,7 +281,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     // PAGED: the 16 keys of a half lie in one page, at an address that the wave shares and places that the lanes keep;
     // otherwise each lane works out its own.
     const Share<C, kOwn> share(g * kOwn, p.D);
-    auto fetch = [&](auto GRAIN, auto PAGED, int key0, const int (&ids)[2], Codes& x) __attribute__((always_inline)) {
+    auto fetch = [&](auto GRAIN, auto PAGED, auto ONCE, int key0, const int (&ids)[2], Codes& x) __attribute__((always_inline)) {
         const uint32_t c_n = decltype(PAGED)::value ? n * (uint32_t)p.token_stride : 0, s_n = decltype(PAGED)::value ? n * (uint32_t)p.s_token : 0;
         x.valid = 0;
 #pragma unroll
@@ -298,8 +303,8 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
                 c_at = id * p.page_stride + place * p.token_stride;
                 s_at = id * p.s_page + place * p.s_token;
             }
-            share.load(GRAIN, PAGED, kbase + c_at, ksbase + s_at, c_n, s_n, x.k[t], x.ks[t]);
-            share.load(GRAIN, PAGED, vbase + c_at, vsbase + s_at, c_n, s_n, x.v[t], x.vs[t]);
+            share.load(GRAIN, PAGED, ONCE, kbase + c_at, ksbase + s_at, c_n, s_n, x.k[t], x.ks[t]);
+            share.load(GRAIN, PAGED, ONCE, vbase + c_at, vsbase + s_at, c_n, s_n, x.v[t], x.vs[t]);
         }
     };
     // The wave's values: rows 16 bytes longer than they are, so that neither eight rows at one place (written) nor 16 rows at 32
@@ -377,12 +382,12 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     };
     // While a tile is used, the codes of the next are on their way, and the page ids of the one behind it.
     // (A loop for each way to load: a branch inside would wait for the loads that each side has under way.)
-    auto run = [&](auto GRAIN, auto PAGED) __attribute__((always_inline)) {
+    auto run_once = [&](auto GRAIN, auto PAGED, auto ONCE) __attribute__((always_inline)) {
         Codes a, b;
-        fetch(GRAIN, PAGED, key, ids0, a);
+        fetch(GRAIN, PAGED, ONCE, key, ids0, a);
         auto tile = [&](Codes& now, Codes& next) __attribute__((always_inline)) {
             const int ids2[2] = {page_id(key + 2 * kStep, 0), page_id(key + 2 * kStep, 1)};
-            fetch(GRAIN, PAGED, key + kStep, ids1, next);  // (past the end: the cache's first rows)
+            fetch(GRAIN, PAGED, ONCE, key + kStep, ids1, next);  // (past the end: the cache's first rows)
             use(now, key);
             key += kStep;
             ids1[0] = ids2[0], ids1[1] = ids2[1];
@@ -394,8 +399,15 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
             if (key >= it.end) break;
         }
     };
+    auto run = [&](auto GRAIN, auto PAGED) __attribute__((always_inline)) { run_once(GRAIN, PAGED, std::false_type{}); };
+    // A sequence's own keys, heads apart, are read by this workgroup alone: past the caches (4 sequences of 100001 keys 87.5 -> 79.9 us;
+    // a prefix read so, which several workgroups share: 8 sequences behind 7901 keys 15.7 -> 16.0).
+    const bool once = it.seq >= 0 && p.plan.suf_tiles == 1 && !p.near_units;
     if (key < it.end) {
-        by_grain<kOwn>(p, page_mask >= 15, run);
+        if (kOwn * C::kBits >= 128 && once && p.D % kOwn == 0 && whole_pages(p, page_mask >= 15))
+            run_once(std::integral_constant<int, kOwn>{}, std::true_type{}, std::true_type{});
+        else
+            by_grain<kOwn>(p, page_mask >= 15, run);
     }
     if (MULTI && odd) {
         auto own = [&](int key) { return ((key - it.begin) / KT & 1) == wave; };
@@ -550,14 +562,14 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             }
             const bool second = n >= 16;
             const uint32_t in = n & 15;
-            key_share.load(GRAIN, std::false_type{}, kbase + (second ? c_at[1] : c_at[0]), ksbase + (second ? s_at[1] : s_at[0]),
+            key_share.load(GRAIN, std::false_type{}, std::false_type{}, kbase + (second ? c_at[1] : c_at[0]), ksbase + (second ? s_at[1] : s_at[0]),
                            in * (uint32_t)p.token_stride, in * (uint32_t)p.s_token, x.w, x.s);
         } else {
             const int at = key0 + n;
             const bool there = (unsigned)id < (unsigned)p.n_pages && at < it.end;
             x.valid = (uint32_t)__ballot(there);
             const int64_t pg = there ? id : 0, place = at & page_mask;
-            key_share.load(GRAIN, std::false_type{}, kbase + pg * p.page_stride + place * p.token_stride,
+            key_share.load(GRAIN, std::false_type{}, std::false_type{}, kbase + pg * p.page_stride + place * p.token_stride,
                            ksbase + pg * p.s_page + place * p.s_token, 0, 0, x.w, x.s);
         }
     };
@@ -567,11 +579,11 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
         if constexpr (decltype(PAGED)::value) {
             const int its = __builtin_amdgcn_readfirstlane(id);
             const int pg = (unsigned)its < (unsigned)p.n_pages ? its : 0, place = first & page_mask;
-            value_share.load(GRAIN, PAGED, vbase + place_of(pg, p.page_stride, place, p.token_stride),
+            value_share.load(GRAIN, PAGED, std::false_type{}, vbase + place_of(pg, p.page_stride, place, p.token_stride),
                              vsbase + place_of(pg, p.s_page, place, p.s_token), vn * (uint32_t)p.token_stride, vn * (uint32_t)p.s_token, x.w, x.s);
         } else {
             const int64_t pg = x.there ? id : 0, place = (first + vn) & page_mask;
-            value_share.load(GRAIN, PAGED, vbase + pg * p.page_stride + place * p.token_stride, vsbase + pg * p.s_page + place * p.s_token, 0, 0,
+            value_share.load(GRAIN, PAGED, std::false_type{}, vbase + pg * p.page_stride + place * p.token_stride, vsbase + pg * p.s_page + place * p.s_token, 0, 0,
                              x.w, x.s);
         }
     };
