@@ -220,11 +220,11 @@ __device__ __forceinline__ f32x4 odd_of(const vec8<T>& v, bool second, bool seen
 constexpr int kThinPad = 8;  // elements
 
 // Up to 16 rows over codes.  Bound by memory where there are waves enough, by a wave's chain of loads, products and exponentials
-// (12 ns a key of 128) where there are few: 4 sequences of 100001 keys (32 / 8 heads of 128, FP4) take 82 us, 5.3 TB/s (its loads alone 82), 1000
-// keys of 32 heads 5.8.  Two waves take 32 keys each in turn.  The products run on the 16 x 16 x 32 instructions, which need half the scores, sums
-// and query operands a lane that tiles of 32 rows do: 84 registers, three waves a SIMD, and in place of those tiles 8 sequences behind 7901
-// keys 19.4 -> 17.0 us, 16 x 8 tokens of 2000 keys 35.6 -> 23.9.  A lane takes a quarter of a key's row, straight from the cache: key n of the first 16 of a tile and of the
-// second, elements g DP / 4 and on; its scores are those of keys 16 t + 4 g + i and query row n.
+// (12 ns a key of 128) where there are few: 4 sequences of 100001 keys (32 / 8 heads of 128, FP4) take 75 us, 5.8 TB/s, 1000 keys of 32 heads
+// 5.8.  Two waves take 32 keys each in turn.  The products run on the 16 x 16 x 32 instructions, which need half the scores, sums
+// and query operands a lane that tiles of 32 rows do: 168 registers, three waves a SIMD, and in place of those tiles 8 sequences behind
+// 7901 keys 19.4 -> 17.0 us, 16 x 8 tokens of 2000 keys 35.6 -> 23.9.  A lane takes a quarter of a key's row, straight from the cache: key n of
+// the first 16 of a tile and of the second, elements g DP / 4 and on; its scores are those of keys 16 t + 4 g + i and query row n.
 template <typename T, int DP, bool MULTI, class C>
 __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b, T* v0, float (*wave_ml)[2][32]) {
     constexpr int NW = 2, KT = 32, kStep = NW * KT, NF = DP / 32, ND = DP / 16;
