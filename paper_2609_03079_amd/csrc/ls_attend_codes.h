@@ -79,20 +79,41 @@ __device__ inline vec8<T> widened(const uint32_t* w, uint8_t scale) {
     return v;
 }
 
-// A lane's share of a row: OWN elements from e on.  What is past a row's end is its start once more: it meets zeros of the
-// query, or becomes columns that are not written.
+// A lane's share of a row: OWN elements from e on.  What is past a row's end (PAD: heads of fewer elements than the lanes have shares
+// of) is loaded from its start once more.  Of a value it becomes columns that are not written.  Of a key it meets zeros of the query, which
+// cancel no infinity (the start's own, or of its codes under another group's scale), so `clear` makes its codes zeros.  Its scale is
+// that of a group of the row, no number only where an element of the row is none.
 template <class C, int OWN>
 struct Share {
     static constexpr int kWords = OWN * C::kBits / 32, kScales = OWN > kGroup ? OWN / kGroup : 1;
     int s_of[kScales], w_of[kWords];
+    uint32_t in = 0;  // bit j: word j is of the row
     __device__ inline Share(int e, int D) {
 #pragma unroll
         for (int i = 0; i < kScales; ++i) s_of[i] = e + i * kGroup < D ? (e + i * kGroup) / kGroup : 0;
 #pragma unroll
         for (int j = 0; j < kWords; ++j) {
             const int w = e + j * (32 / C::kBits);
+            in |= (uint32_t)(w < D) << j;
             w_of[j] = w < D ? w * C::kBits / 8 : 0;
         }
+    }
+    // Of N keys, and only where one has a scale under which a code may be infinite: asking is three instructions of the hundreds that
+    // a tile takes, the zeros 16 to 48 (52 x 5 tokens in heads of 96, FP8: 28.4 us without either, 28.6 asked, 29.3 always cleared).
+    template <typename T, int N>
+    __device__ __forceinline__ void clear(uint32_t (&w)[N][kWords], const uint8_t (&s)[N][kScales]) const {
+        uint32_t top = 0;
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int i = 0; i < kScales; ++i) top = max(top, (uint32_t)s[t][i]);
+        if (!__any(top > 127 + (std::is_same_v<T, _Float16> ? C::kMostExp16 : C::kMostExp))) return;
+        uint32_t bits = in;
+        asm volatile("" : "+v"(bits));  // the masks are worked out here, not kept in registers over the loop
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) w[t][j] &= (uint32_t)__builtin_amdgcn_sbfe((int)bits, j, 1);
     }
     // GRAIN: elements that are there or past the row's end together, the whole share or 16 or 8 (and loaded together).
     // SHARED: the addresses are the wave's, the offsets its lanes'.
@@ -133,7 +154,7 @@ __device__ inline bool whole_pages(const AttendP& p, bool paged) {
 
 // Calls run(GRAIN, PAGED) with the grain of shares of OWN elements.  (A loop for each: a branch inside a loop would wait for the
 // loads that either side has under way.)
-template <int OWN, typename Run>
+template <int OWN, bool PAD, typename Run>
 __device__ __forceinline__ void by_grain(const AttendP& p, bool paged, Run run) {
     paged = whole_pages(p, paged);
     auto by_page = [&](auto GRAIN) __attribute__((always_inline)) {
@@ -142,7 +163,7 @@ __device__ __forceinline__ void by_grain(const AttendP& p, bool paged, Run run) 
         else
             run(GRAIN, std::false_type{});
     };
-    if (p.D % OWN == 0)
+    if (!PAD || p.D % OWN == 0)
         by_page(std::integral_constant<int, OWN>{});
     else if (OWN > 16 && p.D % 16 == 0)
         by_page(std::integral_constant<int, 16>{});
@@ -225,7 +246,7 @@ constexpr int kThinPad = 8;  // elements
 // and query operands a lane that tiles of 32 rows do: 168 registers, three waves a SIMD, and in place of those tiles 8 sequences behind
 // 7901 keys 19.4 -> 17.0 us, 16 x 8 tokens of 2000 keys 35.6 -> 23.9.  A lane takes a quarter of a key's row, straight from the cache: key n of
 // the first 16 of a tile and of the second, elements g DP / 4 and on; its scores are those of keys 16 t + 4 g + i and query row n.
-template <typename T, int DP, bool MULTI, class C>
+template <typename T, int DP, bool MULTI, class C, bool PAD>
 __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b, T* v0, float (*wave_ml)[2][32]) {
     constexpr int NW = 2, KT = 32, kStep = NW * KT, NF = DP / 32, ND = DP / 16;
     constexpr int kOwn = DP / 4, kWords = kOwn * C::kBits / 32, kOf8 = C::kBits / 4, kScales = kOwn > kGroup ? kOwn / kGroup : 1;
@@ -328,6 +349,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
                 for (int i = 0; i < kScales; ++i) x.ks[t][i] = there ? x.ks[t][i] : 0, x.vs[t][i] = there ? x.vs[t][i] : 0;
             }
         }
+        if (PAD) share.template clear<T>(x.k, x.ks);
         f32x4 s[2] = {f32x4{}, f32x4{}};
 #pragma unroll
         for (int f = 0; f < NF; ++f)
@@ -404,10 +426,10 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     // a prefix read so, which several workgroups share: 8 sequences behind 7901 keys 15.7 -> 16.0).
     const bool once = it.seq >= 0 && p.plan.suf_tiles == 1 && !p.near_units;
     if (key < it.end) {
-        if (kOwn * C::kBits >= 128 && once && p.D % kOwn == 0 && whole_pages(p, page_mask >= 15))
+        if (kOwn * C::kBits >= 128 && once && (!PAD || p.D % kOwn == 0) && whole_pages(p, page_mask >= 15))
             run_once(std::integral_constant<int, kOwn>{}, std::true_type{}, std::true_type{});
         else
-            by_grain<kOwn>(p, page_mask >= 15, run);
+            by_grain<kOwn, PAD>(p, page_mask >= 15, run);
     }
     if (MULTI && odd) {
         auto own = [&](int key) { return ((key - it.begin) / KT & 1) == wave; };
@@ -481,7 +503,7 @@ constexpr int kBroadPad = 16;  // elements
 // a SIMD are all that the registers hold.  Each wave widens the keys it multiplies by itself: 32 at a
 // time, a half of their row a lane, the scores of the next 32 computed while the exponentials of these are.  The values of 64 keys are
 // widened by the four waves together, 16 rows each, for all of them.
-template <typename T, int DP, bool MULTI, class C>
+template <typename T, int DP, bool MULTI, class C, bool PAD>
 __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int b, T* v0, T* v1) {
     constexpr int KT = 64, NF = DP / 16, ND = DP / 32, kPitch = DP + kBroadPad, kOf8 = C::kBits / 4;
     using KeyShare = Share<C, DP / 2>;
@@ -538,8 +560,8 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
 
     // As of thin workgroups: only loads, of a masked key those of the cache's first rows, made zeros where they are used.
     struct Keys {
-        uint32_t w[KeyShare::kWords];
-        uint8_t s[KeyShare::kScales];
+        uint32_t w[1][KeyShare::kWords];
+        uint8_t s[1][KeyShare::kScales];
         uint32_t valid;  // bit j: key j of the 32 is not masked
     };
     struct Values {
@@ -563,14 +585,14 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             const bool second = n >= 16;
             const uint32_t in = n & 15;
             key_share.load(GRAIN, std::false_type{}, std::false_type{}, kbase + (second ? c_at[1] : c_at[0]), ksbase + (second ? s_at[1] : s_at[0]),
-                           in * (uint32_t)p.token_stride, in * (uint32_t)p.s_token, x.w, x.s);
+                           in * (uint32_t)p.token_stride, in * (uint32_t)p.s_token, x.w[0], x.s[0]);
         } else {
             const int at = key0 + n;
             const bool there = (unsigned)id < (unsigned)p.n_pages && at < it.end;
             x.valid = (uint32_t)__ballot(there);
             const int64_t pg = there ? id : 0, place = at & page_mask;
             key_share.load(GRAIN, std::false_type{}, std::false_type{}, kbase + pg * p.page_stride + place * p.token_stride,
-                           ksbase + pg * p.s_page + place * p.s_token, 0, 0, x.w, x.s);
+                           ksbase + pg * p.s_page + place * p.s_token, 0, 0, x.w[0], x.s[0]);
         }
     };
     auto fetch_values = [&](auto GRAIN, auto PAGED, int key0, int id, Values& x) __attribute__((always_inline)) {
@@ -601,15 +623,17 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
         if (MULTI && it.seq >= 0 && key0 + wave * 16 + 16 > full) odd |= take_odd<T, DP / 4>(to, key0 + wave * 16 + vn >= full);
     };
     auto clear = [&](Keys& x) __attribute__((always_inline)) {
-        if (~x.valid == 0) return;
-        const bool there = (x.valid >> n) & 1;
+        if (~x.valid != 0) {
+            const bool there = (x.valid >> n) & 1;
 #pragma unroll
-        for (int j = 0; j < KeyShare::kWords; ++j) x.w[j] = there ? x.w[j] : 0;
+            for (int j = 0; j < KeyShare::kWords; ++j) x.w[0][j] = there ? x.w[0][j] : 0;
 #pragma unroll
-        for (int i = 0; i < KeyShare::kScales; ++i) x.s[i] = there ? x.s[i] : 0;
+            for (int i = 0; i < KeyShare::kScales; ++i) x.s[0][i] = there ? x.s[0][i] : 0;
+        }
+        if (PAD) key_share.template clear<T>(x.w, x.s);
     };
     auto score = [&](const Keys& x, int f, f32x16& s) __attribute__((always_inline)) {  // the f-th product of NF
-        s = mma(widened<C, T>(&x.w[f * kOf8], x.s[f * 8 / kGroup]), q[f], s);
+        s = mma(widened<C, T>(&x.w[0][f * kOf8], x.s[0][f * 8 / kGroup]), q[f], s);
     };
     // where this lane finds element 32 t + n of keys 4 h + 0 .. 3 and + 8, by fours, transposed (rows 32 bytes apart in their banks)
     const int v_get = (4 * h + ((lane & 15) >> 2)) * kPitch + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
@@ -714,7 +738,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             now = next, next = used;
         }
     };
-    if (key < it.end) by_grain<DP / 4>(p, page_mask >= 15, run);
+    if (key < it.end) by_grain<DP / 4, PAD>(p, page_mask >= 15, run);
     if (MULTI && it.seq >= 0) {
         __shared__ int waves_odd[4];
         if (lane == 0) waves_odd[wave] = odd;
@@ -771,10 +795,10 @@ enum Shapes { THIN, BROAD, BOTH };
 template <int DP, Shapes S, bool MULTI, class C>
 constexpr int waves_of() {
     if (S == THIN) return DP <= 64 ? (C::kBits == 4 ? 4 : 3) : DP <= 128 ? (C::kBits == 4 ? 3 : 2) : 1;
-    return DP <= 128 ? 2 : 1;
+    return DP <= 64 && C::kBits == 4 ? 3 : DP <= 128 ? 2 : 1;
 }
 
-template <typename T, int DP, Shapes S, bool MULTI, class C>
+template <typename T, int DP, Shapes S, bool MULTI, class C, bool PAD>
 __global__ __launch_bounds__((S == THIN ? 128 : 256), (waves_of<DP, S, MULTI, C>())) void attend_codes_kernel(const AttendP p) {
     constexpr int kThin = 2 * 32 * (DP + kThinPad), kBroad = 64 * (DP + kBroadPad);
     static_assert(kBroad >= kThin, "room for either shape");
@@ -793,20 +817,20 @@ __global__ __launch_bounds__((S == THIN ? 128 : 256), (waves_of<DP, S, MULTI, C>
             if (!prefix) b -= p.pre_items - both / 2;
         }
         if (prefix)
-            attend_broad<T, DP, false, C>(p, true, b, v0, v1);
+            attend_broad<T, DP, false, C, PAD>(p, true, b, v0, v1);
         else if (threadIdx.x < 128)
-            attend_thin<T, DP, MULTI, C>(p, false, b, v0, wave_ml);
+            attend_thin<T, DP, MULTI, C, PAD>(p, false, b, v0, wave_ml);
     } else {
         const bool prefix = b < p.pre_items;
         if (!prefix) b -= p.pre_items;
         if constexpr (S == THIN)
-            attend_thin<T, DP, MULTI, C>(p, prefix, b, v0, wave_ml);
+            attend_thin<T, DP, MULTI, C, PAD>(p, prefix, b, v0, wave_ml);
         else
-            attend_broad<T, DP, MULTI, C>(p, prefix, b, v0, v1);
+            attend_broad<T, DP, MULTI, C, PAD>(p, prefix, b, v0, v1);
     }
 }
 
-template <typename T, int DP, class C>
+template <typename T, int DP, bool PAD, class C>
 hipError_t attend_codes(const ls_kv_cache& shape, const ls_kvq_cache& c, const ls_attend_args& a, const AttendPlan& plan, void* ws,
                         hipStream_t st) {
     AttendP p = attend_params(shape, a, plan, ws);
@@ -823,9 +847,9 @@ hipError_t attend_codes(const ls_kv_cache& shape, const ls_kvq_cache& c, const l
             return hipGetLastError();
         };
         const bool multi = p.n_q > 1 && suf_items;
-        if (s == THIN) return multi ? launch(attend_codes_kernel<T, DP, THIN, true, C>) : launch(attend_codes_kernel<T, DP, THIN, false, C>);
-        if (s == BROAD) return multi ? launch(attend_codes_kernel<T, DP, BROAD, true, C>) : launch(attend_codes_kernel<T, DP, BROAD, false, C>);
-        return multi ? launch(attend_codes_kernel<T, DP, BOTH, true, C>) : launch(attend_codes_kernel<T, DP, BOTH, false, C>);
+        if (s == THIN) return multi ? launch(attend_codes_kernel<T, DP, THIN, true, C, PAD>) : launch(attend_codes_kernel<T, DP, THIN, false, C, PAD>);
+        if (s == BROAD) return multi ? launch(attend_codes_kernel<T, DP, BROAD, true, C, PAD>) : launch(attend_codes_kernel<T, DP, BROAD, false, C, PAD>);
+        return multi ? launch(attend_codes_kernel<T, DP, BOTH, true, C, PAD>) : launch(attend_codes_kernel<T, DP, BOTH, false, C, PAD>);
     };
     return launch_plan<T, DP>(p, plan.pre_wide ? BROAD : THIN, plan.suf_wide ? BROAD : THIN, BOTH, st, go);
 }
@@ -833,9 +857,10 @@ hipError_t attend_codes(const ls_kv_cache& shape, const ls_kvq_cache& c, const l
 template <typename T, class C>
 hipError_t attend_codes_dim(const ls_kvq_cache& c, ls_dtype type, const ls_attend_args& a, const AttendPlan& plan, void* ws, hipStream_t st) {
     const ls_kv_cache shape = shape_of(c, type);
-    if (c.head_dim <= 64) return attend_codes<T, 64, C>(shape, c, a, plan, ws, st);
-    if (c.head_dim <= 128) return attend_codes<T, 128, C>(shape, c, a, plan, ws, st);
-    return attend_codes<T, 256, C>(shape, c, a, plan, ws, st);
+    const int d = c.head_dim;
+    if (d <= 64) return (d == 64 ? attend_codes<T, 64, false, C> : attend_codes<T, 64, true, C>)(shape, c, a, plan, ws, st);
+    if (d <= 128) return (d == 128 ? attend_codes<T, 128, false, C> : attend_codes<T, 128, true, C>)(shape, c, a, plan, ws, st);
+    return (d == 256 ? attend_codes<T, 256, false, C> : attend_codes<T, 256, true, C>)(shape, c, a, plan, ws, st);
 }
 
 }  // namespace

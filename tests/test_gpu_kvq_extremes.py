@@ -1,0 +1,142 @@
+"""The quantised cache where numbers end: heads that do not fill the kernels' 64, 128 or 256 elements, elements that are infinite or
+subnormal in the 16-bit type they are attended in."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2609_03079_amd as lsffn  # noqa: E402, F401
+from test_gpu_kvq import CODES, packed  # noqa: E402
+from test_gpu_ops import BOTH, DEV, attend_ref, ints, ops, rand, within  # noqa: E402, F401
+
+ROWS = [(4, 2, 1), (6, 1, 3), (40, 1, 1), (14, 1, 3)]   # query heads, key heads, tokens: rows of a key head in tiles of 16 and of 128
+
+
+def as_read(ops, codes, scales, dt):
+    """The values of a cache in dt, as a program reads them back, in 64 bits [pages, kv, page, dim]."""
+    pages, kv, page, n = codes.shape
+    dim = 2 * n if codes.dtype == torch.uint8 else n
+    k, v = (torch.empty((pages * page, kv, dim), dtype=dt, device=DEV) for _ in range(2))
+    ops.ls_kvq_read(codes, scales, codes, scales, torch.arange(pages * page, dtype=torch.int32, device=DEV), k, v)
+    return k.double().view(pages, page, kv, dim).transpose(1, 2).contiguous()
+
+
+def check(ops, k, v, q, lens, dt, n_q=1, prefix=0, skip=()):
+    """Attention over pages in their order, the prefix's first and then each sequence's, against 64 bits over the values that
+    ls_kvq_read gives.  skip: pages whose keys have no weight."""
+    total, kv, page, _ = k[0].shape
+    pre, n = -(-prefix // page), -(-max(lens) // page)
+    pages = torch.arange(pre, pre + n * len(lens), dtype=torch.int32).view(len(lens), n)
+    prefix_pages = torch.arange(pre, dtype=torch.int32)
+    assert pre + n * len(lens) <= total
+    scale = 1 / math.sqrt(q.shape[-1])
+    out = torch.full_like(q, 5.0)
+    ops.ls_kvq_attend(q, *k, *v, pages.to(DEV), ints(lens), out, n_q=n_q, max_len=max(lens), prefix_pages=prefix_pages.to(DEV), prefix_len=prefix,
+                      scale=scale)
+    for p in skip:
+        prefix_pages[prefix_pages == p] = -1
+        pages[pages == p] = -1
+    ref, tol = attend_ref(q, as_read(ops, *k, dt), as_read(ops, *v, dt), pages, lens, n_q, max(lens), prefix_pages, prefix, scale)
+    within(out, ref, tol)
+    return out
+
+
+def random_codes(shape, code, most, seed):
+    """Codes of rows [.., dim] up to code number `most` and its negative, one a byte."""
+    g = torch.Generator().manual_seed(seed)
+    sign = 8 if code == "fp4" else 128
+    return (torch.randint(0, most + 1, shape, generator=g) + sign * torch.randint(0, 2, shape, generator=g)).to(torch.uint8)
+
+
+def held(c, code):
+    """Codes one a byte as the cache holds them."""
+    c = c.to(DEV)
+    return c.view(torch.float8_e4m3fn) if code == "fp8" else (c[..., 0::2] | (c[..., 1::2] << 4)).contiguous()
+
+
+def scales_of(shape, dim, exps):
+    """Scale bytes of rows [.., dim], exps: the exponent of each group."""
+    return (torch.tensor(exps) + 127).to(torch.uint8).expand(*shape, -(-dim // 32)).contiguous().to(DEV)
+
+
+# ---- heads that end inside a lane's share ----------------------------------------------------------
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dim", [40, 64, 72, 80, 104, 112, 128, 136, 200, 256])
+@pytest.mark.parametrize("heads,kv,n_q", ROWS)
+@pytest.mark.parametrize("page", [1, 16])
+def test_rows_of_groups_far_apart(ops, code, dim, heads, kv, n_q, page):
+    """A last group of small codes under a large scale, a first one of the largest codes under a small one: every element is a number
+    of float16, but the first group's codes under the last one's scale would not be."""
+    shape, last = (64 // page + 8, kv, page, dim), (dim - 1) // 32
+    # the largest code times the last group's scale: 6 * 2^14, 448 * 2^8; what the group holds: 2 * 2^14, 240 * 2^8
+    most, small, big, little = (7, 4, 14, -3) if code == "fp4" else (0x7E, 0x77, 8, -9)
+    c = random_codes(shape, code, most, dim)
+    c[..., 32 * last:] = random_codes((*shape[:3], dim - 32 * last), code, small, dim + 1)
+    c[..., 0:4] = most
+    exps = [little] * last + [big]
+    k = held(c, code), scales_of(shape[:3], dim, exps)
+    v = packed(rand(shape, 3).double(), code, torch.float16)
+    q = rand((n_q, heads, dim), 5, torch.float16)
+    q[..., 32 * last:] *= 2.0 ** -12
+    out = check(ops, k, v, q, [50], torch.float16, n_q, prefix=9)
+    assert torch.all(torch.isfinite(out))
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dim", [24, 64, 80, 96, 128, 136, 160, 256])
+@pytest.mark.parametrize("heads,kv,n_q", ROWS)
+@pytest.mark.parametrize("page", [1, 16])
+def test_keys_at_minus_infinity(ops, code, dim, heads, kv, n_q, page):
+    """Keys with an element beyond float16, infinite there, whose products with the queries are minus infinity: no weight."""
+    shape = (96 // page, kv, page, dim)
+    codes, scales = packed(rand(shape, 1).double(), code, torch.float16)
+    v = packed(rand(shape, 3).double(), code, torch.float16)
+    gone = [1, 3]
+    for p in gone:
+        raw = codes.view(torch.uint8)
+        raw[p] = 0
+        # element 1, code -6 or -448, times 2^16
+        raw[p, ..., 0 if code == "fp4" else 1] = 0xF0 if code == "fp4" else 0xFE
+        scales[p, ..., 0] = 127 + 16
+    q = rand((n_q, heads, dim), 5, torch.float16)
+    q[..., 1] = q[..., 1].abs() + 0.5
+    out = check(ops, (codes, scales), v, q, [50], torch.float16, n_q, prefix=9, skip=gone)
+    assert torch.all(torch.isfinite(out))
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dim", [64, 80, 256])
+@pytest.mark.parametrize("heads,kv,n_q", ROWS)
+def test_values_in_float16s_ends(ops, code, dim, heads, kv, n_q):
+    """Keys and values of every scale around float16's subnormal numbers, where a code rounds, and up to its largest."""
+    shape = (16, kv, 16, dim)
+    g = torch.Generator().manual_seed(dim)
+    k, v = (packed(rand(shape, i).double(), code, torch.float16) for i in (1, 3))
+    low, high = (-27, 12) if code == "fp4" else (-33, 6)
+    k[1].copy_(torch.randint(low, low + 14, k[1].shape, generator=g) + 127)
+    v[1].copy_(torch.randint(low, high, (*v[1].shape[:2], 1, v[1].shape[3]), generator=g) + 127)   # a head's values of one size
+    q = rand((2 * n_q, heads, dim), 5, torch.float16, 2000.0)
+    check(ops, k, v, q, [70, 33], torch.float16, n_q, prefix=40)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dt", BOTH, ids=["f16", "bf16"])
+@pytest.mark.parametrize("heads", [1, 40])
+@pytest.mark.parametrize("dim", [64, 80])
+def test_one_key_is_its_value(ops, code, dt, heads, dim):
+    """Every scale byte: a row of one key is what ls_kvq_read gives for its value, infinities and NaN included."""
+    shape = (256, 1, 1, dim)
+    k = packed(rand(shape, 1).double(), code, dt)
+    v = held(random_codes(shape, code, 7 if code == "fp4" else 0x7E, 2), code), torch.arange(256, dtype=torch.uint8).view(256, 1, 1, 1).repeat(
+        1, 1, 1, -(-dim // 32)).to(DEV)
+    q = torch.zeros((256, heads, dim), dtype=dt, device=DEV)
+    out = torch.full_like(q, 5.0)
+    ops.ls_kvq_attend(q, *k, *v, torch.arange(256, dtype=torch.int32, device=DEV)[:, None], ints([1] * 256), out, max_len=1, scale=0.125)
+    ref = as_read(ops, *v, dt)[:, :, 0].expand(256, heads, dim)
+    assert torch.equal(torch.isnan(out), torch.isnan(ref))
+    assert torch.equal(out.double().nan_to_num(0, math.inf, -math.inf), ref.nan_to_num(0, math.inf, -math.inf))
