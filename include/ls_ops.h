@@ -249,7 +249,8 @@ ls_status ls_kvq_read(ls_ops* ctx, const ls_kvq_cache* cache, const ls_kvq_read_
 
 /* ls_attend over the quantised cache: the same attention, with the values that ls_kvq_read gives in `type` for keys and values
  * (a value outside the range of LS_F16 is infinite there).  q and out are of `type`: LS_F16 or LS_BF16 (LS_E_UNSUPPORTED for
- * LS_F32); pointers and strides of q and out 16-byte aligned; head_dim at most 256. */
+ * LS_F32); pointers and strides of q and out 16-byte aligned; head_dim at most 256.  A row of LS_BF16 is a number wherever its definition
+ * is, however large its values and many its keys; beside an element above 2^86 one below 2^-80 may lose digits. */
 ls_status ls_kvq_attend(ls_ops* ctx, const ls_kvq_cache* cache, ls_dtype type, const ls_attend_args* a);
 
 /* Decides about drafted tokens: with p the target's probabilities, q those that drafted them and u given random numbers in [0, 1),

@@ -71,6 +71,44 @@ __device__ inline int64_t place_of(int id, int64_t page_stride, int place, int64
 template <typename T>
 constexpr float kSlack = std::is_same_v<T, _Float16> ? 1.f : 8.f;
 
+// The sums of weighted values are divided by the weights' sum when all keys have been seen.  bfloat16 has values of up to 2^127.8: weights
+// of up to 2^8 (kSlack) of some of them, or those of many keys, are beyond fp32 though the row is not.  A wave (thin) or workgroup (broad) one of
+// whose sums came near that (kFar: 128 parts of less can be joined) goes over its keys a second time, those rows' weights smaller by
+// 2^32: 2^22 keys of weights of 2^-24 stay below the largest value.  (Smaller from the start, the products with small values would be
+// lost: fp32 ends at 2^-126.)  Rows are told apart, so that a row's bits do not depend on those beside it.  Others pay for looking at
+// the sums, one instruction for two: 8 sequences behind 7901 keys 16.4 -> 16.6 us, 64 behind 32768 116.5 -> 116.8.
+template <typename T>
+constexpr bool kTwice = !std::is_same_v<T, _Float16>;
+constexpr float kFar = 0x1p118f, kLower = 32.f;
+
+// The lanes among whose sums one is far, or no number.
+template <typename V, int N>
+__device__ __forceinline__ uint64_t far_rows(const V (&o)[N]) {
+    float most = 0.f;
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int e = 0; e < (int)(sizeof(V) / 4); ++e) most = __builtin_elementwise_maximum(most, fabsf(o[d][e]));  // NaN, if one is
+    return __ballot(!(most < kFar));
+}
+
+// A pass of a workgroup over its keys: the first, or the SECOND, which is seldom asked for and looks every key's place up by itself.
+// What follows from the call, the thread and the workgroup is worked out anew in it: kept, it would take registers that the first
+// one needs (as one loop over both, calls of a few keys took 7 to 10 in a hundred more).
+template <bool SECOND>
+struct Pass {
+    const AttendP& p;
+    int thread, b;
+};
+__device__ __forceinline__ Pass<false> first_pass(const AttendP& p, int b) { return {p, (int)threadIdx.x, b}; }
+__device__ __forceinline__ Pass<true> second_pass(int b) {
+    typedef const __attribute__((address_space(4))) AttendP* Argument;
+    Argument p = (Argument)__builtin_amdgcn_kernarg_segment_ptr();  // the kernel's only one
+    int thread = threadIdx.x;
+    asm volatile("" : "+s"(p), "+v"(thread), "+s"(b));
+    return {*(const AttendP*)p, thread, b};
+}
+
 // Eight elements of a lane's codes.
 template <class C, typename T>
 __device__ inline vec8<T> widened(const uint32_t* w, uint8_t scale) {
@@ -154,8 +192,9 @@ __device__ inline bool whole_pages(const AttendP& p, bool paged) {
 
 // Calls run(GRAIN, PAGED) with the grain of shares of OWN elements.  (A loop for each: a branch inside a loop would wait for the
 // loads that either side has under way.)
-template <int OWN, bool PAD, typename Run>
+template <int OWN, bool PAD, bool SECOND, typename Run>
 __device__ __forceinline__ void by_grain(const AttendP& p, bool paged, Run run) {
+    if constexpr (SECOND) return run(std::integral_constant<int, 8>{}, std::false_type{});
     paged = whole_pages(p, paged);
     auto by_page = [&](auto GRAIN) __attribute__((always_inline)) {
         if (paged)
@@ -246,13 +285,14 @@ constexpr int kThinPad = 8;  // elements
 // and query operands a lane that tiles of 32 rows do: 168 registers, three waves a SIMD, and in place of those tiles 8 sequences behind
 // 7901 keys 19.4 -> 17.0 us, 16 x 8 tokens of 2000 keys 35.6 -> 23.9.  A lane takes a quarter of a key's row, straight from the cache: key n of
 // the first 16 of a tile and of the second, elements g DP / 4 and on; its scores are those of keys 16 t + 4 g + i and query row n.
-template <typename T, int DP, bool MULTI, class C, bool PAD>
-__device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b, T* v0, float (*wave_ml)[2][32]) {
+template <typename T, int DP, bool MULTI, class C, bool PAD, bool SECOND>
+__device__ __forceinline__ bool attend_thin(const Pass<SECOND>& pass, bool prefix, float* lift_of_row, T* v0, float (*wave_ml)[2][32]) {
     constexpr int NW = 2, KT = 32, kStep = NW * KT, NF = DP / 32, ND = DP / 16;
     constexpr int kOwn = DP / 4, kWords = kOwn * C::kBits / 32, kOf8 = C::kBits / 4, kScales = kOwn > kGroup ? kOwn / kGroup : 1;
+    const AttendP& p = pass.p;
     Item it;
-    if (!item_of<16>(p, prefix, near(p, prefix, b), &it)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (!item_of<16>(p, prefix, near(p, prefix, pass.b), &it)) return false;
+    const int lane = pass.thread & 63, wave = __builtin_amdgcn_readfirstlane(pass.thread >> 6);
     const int n = lane & 15, g = lane >> 4;
 
     int key = it.begin + wave * KT;
@@ -263,7 +303,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     int ids0[2] = {page_id(key, 0), page_id(key, 1)}, ids1[2] = {page_id(key + kStep, 0), page_id(key + kStep, 1)};
     it.len = it.seq < 0 ? p.prefix_len : min(p.lens[it.seq], p.max_len);
     it.end = min(it.end, it.len);
-    if (it.begin >= it.end && !p.direct) return;
+    if (it.begin >= it.end && !p.direct) return false;
 
     const int row = it.row0 + n;
     const bool row_ok = row < it.rows;
@@ -286,6 +326,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
 #pragma unroll
     for (auto& x : o) x = f32x4{};
     float m = -INFINITY, l = 0.f;
+    const float lift = SECOND ? *lift_of_row : kLift<T>;
 
     const uint8_t* kbase = static_cast<const uint8_t*>(p.k) + it.kv * p.head_stride;
     const uint8_t* vbase = static_cast<const uint8_t*>(p.v) + it.kv * p.head_stride;
@@ -373,7 +414,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         top = pair_max<16>(top);
         top = pair_max<32>(top);
-        const float next = top * p.c - kLift<T>;
+        const float next = top * p.c - lift;
         const bool grown = next > m + kSlack<T>;
         if (__any(grown)) {
             const float to = grown ? next : m, scale = grown ? __builtin_amdgcn_exp2f(m - next) : 1.f;  // m = -inf: 0
@@ -426,10 +467,19 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
     // a prefix read so, which several workgroups share: 8 sequences behind 7901 keys 15.7 -> 16.0).
     const bool once = it.seq >= 0 && p.plan.suf_tiles == 1 && !p.near_units;
     if (key < it.end) {
-        if (kOwn * C::kBits >= 128 && once && (!PAD || p.D % kOwn == 0) && whole_pages(p, page_mask >= 15))
+        if (!SECOND && kOwn * C::kBits >= 128 && once && (!PAD || p.D % kOwn == 0) && whole_pages(p, page_mask >= 15))
             run_once(std::integral_constant<int, kOwn>{}, std::true_type{}, std::true_type{});
         else
-            by_grain<kOwn, PAD>(p, page_mask >= 15, run);
+            by_grain<kOwn, PAD, SECOND>(p, page_mask >= 15, run);
+    }
+    if (kTwice<T> && !SECOND) {
+        uint64_t rows = far_rows(o);
+        if (__builtin_expect(rows != 0, false)) {
+            rows |= rows >> 32;
+            rows |= rows >> 16;
+            *lift_of_row = (rows >> n) & 1 ? kLift<T> - kLower : kLift<T>;
+            return true;
+        }
     }
     if (MULTI && odd) {
         auto own = [&](int key) { return ((key - it.begin) / KT & 1) == wave; };
@@ -468,7 +518,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         }
     }
     __syncthreads();
-    if (wave == 1 || !row_ok) return;
+    if (wave == 1 || !row_ok) return false;
     const int64_t out_row = token * p.H + head;
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
@@ -492,6 +542,7 @@ __device__ __forceinline__ void attend_thin(const AttendP& p, bool prefix, int b
         at[0] = top;
         at[1] = sum;
     }
+    return false;
 }
 
 
@@ -503,14 +554,15 @@ constexpr int kBroadPad = 16;  // elements
 // a SIMD are all that the registers hold.  Each wave widens the keys it multiplies by itself: 32 at a
 // time, a half of their row a lane, the scores of the next 32 computed while the exponentials of these are.  The values of 64 keys are
 // widened by the four waves together, 16 rows each, for all of them.
-template <typename T, int DP, bool MULTI, class C, bool PAD>
-__device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int b, T* v0, T* v1) {
+template <typename T, int DP, bool MULTI, class C, bool PAD, bool SECOND>
+__device__ __forceinline__ bool attend_broad(const Pass<SECOND>& pass, bool prefix, float* lift_of_row, T* v0, T* v1) {
     constexpr int KT = 64, NF = DP / 16, ND = DP / 32, kPitch = DP + kBroadPad, kOf8 = C::kBits / 4;
     using KeyShare = Share<C, DP / 2>;
     using ValueShare = Share<C, DP / 4>;
+    const AttendP& p = pass.p;
     Item it;
-    if (!item_of<128>(p, prefix, near(p, prefix, b), &it)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (!item_of<128>(p, prefix, near(p, prefix, pass.b), &it)) return false;
+    const int lane = pass.thread & 63, wave = __builtin_amdgcn_readfirstlane(pass.thread >> 6);
     const int n = lane & 31, h = lane >> 5;    // of keys, and of scores: row n of 32
     const int vn = lane & 15, vg = lane >> 4;  // of values, as they are widened
 
@@ -526,7 +578,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
     Ids ids0 = page_ids(key), ids1 = page_ids(key + KT);
     it.len = it.seq < 0 ? p.prefix_len : min(p.lens[it.seq], p.max_len);
     it.end = min(it.end, it.len);
-    if (it.begin >= it.end && !p.direct) return;
+    if (it.begin >= it.end && !p.direct) return false;
 
     const int row = it.row0 + wave * 32 + n;
     const bool row_ok = row < it.rows, idle_wave = it.row0 + wave * 32 >= it.rows;  // (which only widens values)
@@ -549,6 +601,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
 #pragma unroll
     for (auto& x : o) x = f32x16{};
     float m = -INFINITY, l = 0.f;
+    const float lift = SECOND ? *lift_of_row : kLift<T>;
 
     const uint8_t* kbase = static_cast<const uint8_t*>(p.k) + it.kv * p.head_stride;
     const uint8_t* vbase = static_cast<const uint8_t*>(p.v) + it.kv * p.head_stride;
@@ -653,7 +706,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         top = pair_max<32>(top);
-        const float next = top * p.c - kLift<T>;
+        const float next = top * p.c - lift;
         const bool grown = next > m + kSlack<T>;
         if (__any(grown)) {
             const float to = grown ? next : m, scale = grown ? __builtin_amdgcn_exp2f(m - next) : 1.f;  // m = -inf: 0
@@ -738,7 +791,18 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
             now = next, next = used;
         }
     };
-    if (key < it.end) by_grain<DP / 4, PAD>(p, page_mask >= 15, run);
+    if (key < it.end) by_grain<DP / 4, PAD, SECOND>(p, page_mask >= 15, run);
+    if (kTwice<T> && !SECOND) {
+        __shared__ int waves_far[4];
+        uint64_t rows = far_rows(o);
+        if (lane == 0) waves_far[wave] = rows != 0;
+        landed();
+        if (__builtin_expect(waves_far[0] | waves_far[1] | waves_far[2] | waves_far[3], 0)) {
+            rows |= rows >> 32;
+            *lift_of_row = (rows >> n) & 1 ? kLift<T> - kLower : kLift<T>;
+            return true;
+        }
+    }
     if (MULTI && it.seq >= 0) {
         __shared__ int waves_odd[4];
         if (lane == 0) waves_odd[wave] = odd;
@@ -759,7 +823,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
         }
     }
     l += other_half(l);
-    if (!row_ok) return;
+    if (!row_ok) return false;
     const int64_t out_row = token * p.H + head;
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -785,6 +849,7 @@ __device__ __forceinline__ void attend_broad(const AttendP& p, bool prefix, int 
         at[0] = m;
         at[1] = l;
     }
+    return false;
 }
 
 // Which shapes a launch holds (rows of up to 32 are thin: broad ones at 32 rows would leave three waves of four without work).  BOTH: a broad prefix beside thin sequences, eight workgroups of one after eight of the other (one
@@ -804,6 +869,17 @@ __global__ __launch_bounds__((S == THIN ? 128 : 256), (waves_of<DP, S, MULTI, C>
     static_assert(kBroad >= kThin, "room for either shape");
     __shared__ __attribute__((aligned(16))) T v0[S == THIN ? kThin : kBroad], v1[S == THIN ? 1 : kBroad];
     __shared__ float wave_ml[2][2][32];
+    auto thin = [&](int b, bool prefix) __attribute__((always_inline)) {
+        float lift;
+        if (__builtin_expect((attend_thin<T, DP, MULTI, C, PAD>(first_pass(p, b), prefix, &lift, v0, wave_ml)), false))
+            attend_thin<T, DP, MULTI, C, PAD>(second_pass(b), prefix, &lift, v0, wave_ml);
+    };
+    auto broad = [&](auto SEVERAL, int b, bool prefix) __attribute__((always_inline)) {
+        constexpr bool several = decltype(SEVERAL)::value;
+        float lift;
+        if (__builtin_expect((attend_broad<T, DP, several, C, PAD>(first_pass(p, b), prefix, &lift, v0, v1)), false))
+            attend_broad<T, DP, several, C, PAD>(second_pass(b), prefix, &lift, v0, v1);
+    };
     int b = blockIdx.x;
     if constexpr (S == BOTH) {
         const int both = 2 * min(p.pre_items, p.suf_items / 8 * 8);  // pre_items is a multiple of 8
@@ -817,16 +893,16 @@ __global__ __launch_bounds__((S == THIN ? 128 : 256), (waves_of<DP, S, MULTI, C>
             if (!prefix) b -= p.pre_items - both / 2;
         }
         if (prefix)
-            attend_broad<T, DP, false, C, PAD>(p, true, b, v0, v1);
+            broad(std::false_type{}, b, true);
         else if (threadIdx.x < 128)
-            attend_thin<T, DP, MULTI, C, PAD>(p, false, b, v0, wave_ml);
+            thin(b, false);
     } else {
         const bool prefix = b < p.pre_items;
         if (!prefix) b -= p.pre_items;
         if constexpr (S == THIN)
-            attend_thin<T, DP, MULTI, C, PAD>(p, prefix, b, v0, wave_ml);
+            thin(b, prefix);
         else
-            attend_broad<T, DP, MULTI, C, PAD>(p, prefix, b, v0, v1);
+            broad(std::bool_constant<MULTI>{}, b, prefix);
     }
 }
 

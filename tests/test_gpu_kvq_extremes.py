@@ -140,3 +140,57 @@ def test_one_key_is_its_value(ops, code, dt, heads, dim):
     ref = as_read(ops, *v, dt)[:, :, 0].expand(256, heads, dim)
     assert torch.equal(torch.isnan(out), torch.isnan(ref))
     assert torch.equal(out.double().nan_to_num(0, math.inf, -math.inf), ref.nan_to_num(0, math.inf, -math.inf))
+
+
+# ---- values near the end of bfloat16 ---------------------------------------------------------------
+def rising(shape, code, n_keys, step):
+    """Keys whose score with a query of ones in element 0 is `step` powers of two for every 64 keys that they come later, up to 6 of them."""
+    x = torch.zeros(shape, dtype=torch.float64)
+    pages, _, page, _ = shape
+    at = (torch.arange(pages)[:, None] * page + torch.arange(page)).clamp(max=n_keys - 1) // 64
+    level = torch.tensor([0.0, 1.0, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64)   # numbers of both codes under the scale one
+    x[..., 0] = level[at.clamp(max=5)][:, None]
+    x[..., 1] = 6.0 if code == "fp4" else 448.0   # keeps the scale at one; the query is zero there
+    return x.to(DEV)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("heads,kv,n_q", ROWS)
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("top", [119, 122, 125])
+def test_large_values_and_a_rising_maximum(ops, code, heads, kv, n_q, dim, top):
+    """A row's maximum that grows by less than what its sums are rescaled for, beside values near the end of bfloat16: weights that
+    are far above one for a while must not make an infinity of them."""
+    dt = torch.bfloat16
+    shape = (48, kv, 16, dim)
+    k = packed(rising(shape, code, 600, 7), code, dt)
+    v = packed(rand(shape, 3).double(), code, dt)
+    v[1].fill_(127 + top - (0 if code == "fp4" else 6))
+    q = torch.zeros((n_q, heads, dim), dtype=dt, device=DEV)
+    q[..., 0] = 7 * math.log(2) * math.sqrt(dim) * (1 + rand((n_q, heads), 7) * 0.01)
+    for prefix, n in ((0, 600), (300, 300)):
+        out = check(ops, k, v, q, [n], dt, n_q, prefix=prefix)
+        assert torch.all(torch.isfinite(out))
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("heads,kv,n_q", ROWS)
+@pytest.mark.parametrize("dim", [64, 80, 256])
+@pytest.mark.parametrize("top", [100, 112, 117, 120, 125])
+def test_sums_of_large_values(ops, code, heads, kv, n_q, dim, top):
+    """Thousands of keys of nearly one weight, whose values are near the end of bfloat16: their mean is a number, though neither their
+    sum nor that of a part of them is one."""
+    dt = torch.bfloat16
+    shape = (180, kv, 64, dim)
+    k = packed(rand(shape, 1).double(), code, dt)
+    v = packed(rand(shape, 3).abs().double(), code, dt)
+    v[1].fill_(127 + top - (0 if code == "fp4" else 6))
+    q = rand((2 * n_q, heads, dim), 5, dt, 0.5)
+    for prefix, lens in ((0, [4000, 1]), (5000, [100, 2900]), (5000, [0, -1])):
+        out = check(ops, k, v, q, lens, dt, n_q, prefix=prefix)
+        assert torch.all(torch.isfinite(out))
+    # a late value that is no number is seen by the last token alone
+    if n_q > 1:
+        v[1][(4000 - 1) // 64, :, (4000 - 1) % 64] = 255
+        out = check(ops, k, v, q, [4000, 1], dt, n_q)
+        assert torch.all(torch.isfinite(out[:n_q - 1])) and torch.all(torch.isnan(out[n_q - 1])) and torch.all(torch.isfinite(out[n_q:]))
