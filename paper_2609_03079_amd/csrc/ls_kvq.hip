@@ -101,11 +101,12 @@ __device__ inline float turn(float x, float y, float c, float s) {
 // The same for a key, which is rounded but once, to its code: the products are exact in 64 bits, their sum is off by 2^-53, and
 // what is inexact in fp32 is rounded to odd there, so that it lies on the side of every border between two codes or
 // scales that it was on.  (In fp32 a few of 8 million elements fall to the other side; time: nothing, the data's reading hides it.)
+// A finite key beyond fp32 becomes its largest number, which is odd, and with it the largest code of the largest scale.
 __device__ inline float turn_key(float x, float y, float c, float s) {
     const double d = __builtin_fma((double)y, (double)s, (double)x * (double)c);
     const float f = (float)d;
     const uint32_t toward_zero = __float_as_uint(f) - (__builtin_fabs((double)f) > __builtin_fabs(d) ? 1u : 0u);
-    return (double)f == d || !(__builtin_fabsf(f) < INFINITY) ? f : __uint_as_float(toward_zero | 1u);
+    return (double)f == d || d != d ? f : __uint_as_float(toward_zero | 1u);
 }
 
 // Elements e .. e + 7 of a head turned to their position.  VEC: whole vectors of them turn or do not, with partners

@@ -1,5 +1,5 @@
 """The quantised cache where numbers end: heads that do not fill the kernels' 64, 128 or 256 elements, elements that are infinite or
-subnormal in the 16-bit type they are attended in."""
+subnormal in the 16-bit type they are attended in, sums and turned keys beyond fp32."""
 import math
 
 import pytest
@@ -11,8 +11,8 @@ if not torch.cuda.is_available():  # pragma: no cover
     pytest.skip("needs a GPU", allow_module_level=True)
 
 import paper_2609_03079_amd as lsffn  # noqa: E402, F401
-from test_gpu_kvq import CODES, packed  # noqa: E402
-from test_gpu_ops import BOTH, DEV, attend_ref, ints, ops, rand, within  # noqa: E402, F401
+from test_gpu_kvq import CODES, decoded, empty_cache, packed, same  # noqa: E402
+from test_gpu_ops import BOTH, DEV, attend_ref, ints, ops, rand, rope_ref, within  # noqa: E402, F401
 
 ROWS = [(4, 2, 1), (6, 1, 3), (40, 1, 1), (14, 1, 3)]   # query heads, key heads, tokens: rows of a key head in tiles of 16 and of 128
 
@@ -194,3 +194,32 @@ def test_sums_of_large_values(ops, code, heads, kv, n_q, dim, top):
         v[1][(4000 - 1) // 64, :, (4000 - 1) % 64] = 255
         out = check(ops, k, v, q, [4000, 1], dt, n_q)
         assert torch.all(torch.isfinite(out[:n_q - 1])) and torch.all(torch.isnan(out[n_q - 1])) and torch.all(torch.isfinite(out[n_q:]))
+
+
+# ---- turned keys -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 5000])
+@pytest.mark.parametrize("dim,rot,style", [(128, 128, 0), (128, 128, 1), (80, 40, 0), (72, 10, 1)])
+def test_turned_keys_beyond_fp32_are_numbers(ops, code, dtype, T, dim, rot, style):
+    """Keys that grow beyond the largest fp32 number when they turn are finite in 64 bits, where they are turned: they fall to the
+    largest code of the largest scale.  Infinities and NaN still make their group none."""
+    top = torch.finfo(dtype).max
+    k = rand((T, 2, dim), 5, torch.float32).clamp(-1, 1).mul(top).to(dtype)
+    k[0, 0, :rot] = top
+    cs = torch.full((3, rot), math.sqrt(0.5), device=DEV)   # (a c - b s, b c + a s): (0, 1.41 top) where a = b
+    cs[1, rot // 2:] *= -1
+    cs[2] = 2.0   # no rotation, but a table all the same: up to 4 top
+    at = torch.arange(T, dtype=torch.int32, device=DEV)
+    cache = empty_cache(T // 16 + 1, 2, 16, dim, code)
+    ops.ls_kvq_append(*cache, k, k, at % 3, at, cs, style=style)
+    ref, _ = rope_ref(k, cs[(at % 3).long()], rot, style)
+    assert torch.all(torch.isfinite(ref)) and torch.any(ref.abs() > torch.finfo(torch.float32).max)
+    pg, pl = at.long() // 16, at.long() % 16
+    for c, s, x in ((*cache[:2], ref), (*cache[2:], k.double())):
+        rows, scales = packed(x, code, dtype)
+        assert same(s[pg, :, pl], scales)
+        assert same(decoded(c.view(torch.uint8)[pg, :, pl].view(c.dtype), scales, dim), decoded(rows, scales, dim))
+    k[:, 0, 0], k[:, 1, 1] = math.inf, math.nan
+    ops.ls_kvq_append(*cache, k, k, at % 3, at, cs, style=style)
+    assert torch.all(cache[1][pg, :, pl][..., 0] == 255) and torch.all(cache[3][pg, :, pl][..., 0] == 255)
