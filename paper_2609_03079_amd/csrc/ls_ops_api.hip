@@ -139,11 +139,19 @@ ls_status check_attend(ls_ops* c, const ls_kv_cache* kv, const ls_attend_args* a
     return LS_OK;
 }
 
-// No two rows of n elements overlap, `a` of them that are by_a apart in each of `b` that are by_b apart, or the other way round.
+// No two rows of n elements overlap, `a` of them that are by_a apart in each of `b` that are by_b apart.
 bool rows_apart(int64_t a, int64_t by_a, int64_t b, int64_t by_b, int64_t n) {
     if (a == 1 || b == 1) return a == b || (a == 1 ? by_b : by_a) >= n;
     const int64_t outer = std::max(by_a, by_b), inner = std::min(by_a, by_b), of_inner = by_a < by_b ? a : b;
-    return inner >= n && (outer - n) / inner >= of_inner - 1;
+    if (inner < n) return false;
+    if ((outer - n) / inner >= of_inner - 1) return true;  // one nested in the other
+    // otherwise two rows that are j of the b apart: the nearest are as many of the a apart the other way, or one more
+    for (int64_t j = 1; j < b; ++j) {
+        const __int128 off = (__int128)j * by_b;
+        const int64_t i = (int64_t)std::min<__int128>(a - 1, off / by_a);
+        if (off - (__int128)i * by_a < n || (i + 1 < a && (__int128)(i + 1) * by_a - off < n)) return false;
+    }
+    return true;
 }
 
 // Launches an attention that was found right, in as many pieces as it takes.

@@ -223,3 +223,16 @@ def test_turned_keys_beyond_fp32_are_numbers(ops, code, dtype, T, dim, rot, styl
     k[:, 0, 0], k[:, 1, 1] = math.inf, math.nan
     ops.ls_kvq_append(*cache, k, k, at % 3, at, cs, style=style)
     assert torch.all(cache[1][pg, :, pl][..., 0] == 255) and torch.all(cache[3][pg, :, pl][..., 0] == 255)
+
+
+# ---- rows that are not nested ----------------------------------------------------------------------
+@pytest.mark.parametrize("code", CODES)
+def test_read_into_rows_between_each_other(ops, code):
+    """Tokens 16 elements apart and heads 24: each row has its place, though neither lies within the other's."""
+    cache = [*packed(rand((1, 2, 4, 8), 1).double(), code, torch.float16), *packed(rand((1, 2, 4, 8), 2).double(), code, torch.float16)]
+    base = torch.full((2, 72), 7.0, dtype=torch.float16, device=DEV)
+    k, v = (x.as_strided((3, 2, 8), (16, 24, 1), x.storage_offset()) for x in base)
+    ops.ls_kvq_read(*cache, ints([2, 0, 3]), k, v)
+    at = torch.tensor([2, 0, 3], device=DEV)
+    assert same(k.double(), decoded(*cache[:2], 8)[0, :, at].transpose(0, 1)) and same(v.double(), decoded(*cache[2:], 8)[0, :, at].transpose(0, 1))
+    assert torch.all(base[:, 8:16] == 7) and torch.all(base[:, 64:] == 7)
