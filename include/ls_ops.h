@@ -229,7 +229,7 @@ typedef struct {
  * group, its scale is the smallest power of two with top < 7 * 2^e (LS_FP4) or 464 * 2^e (LS_FP8), no smaller than 2^-126 and no larger than leaves the largest
  * code finite in `type`; a code is the element over the scale, to nearest, ties to the even code, at most the largest code.
  * A group that holds an infinity or NaN gets the scale byte 255 and zeros for codes.  Slots, positions, q and q_out as in
- * ls_kv_append (q_out may be q itself); of two tokens with one slot any group's codes and scale may stay. */
+ * ls_kv_append (q_out may be q itself; of tokens that share a slot, which they must not, a row may hold parts of each). */
 ls_status ls_kvq_append(ls_ops* ctx, const ls_kvq_cache* cache, ls_dtype type, const ls_append_args* a);
 
 /* Reads the keys and values of tokens back: k[t] = the row of slots[t], in `type`, rounded once (exact in LS_F32; in the
@@ -249,8 +249,8 @@ ls_status ls_kvq_read(ls_ops* ctx, const ls_kvq_cache* cache, const ls_kvq_read_
 
 /* ls_attend over the quantised cache: the same attention, with the values that ls_kvq_read gives in `type` for keys and values
  * (a value outside the range of LS_F16 is infinite there).  q and out are of `type`: LS_F16 or LS_BF16 (LS_E_UNSUPPORTED for
- * LS_F32); pointers and strides of q and out 16-byte aligned; head_dim at most 256.  A row of LS_BF16 is a number wherever its definition
- * is, however large its values and many its keys; beside an element above 2^86 one below 2^-80 may lose digits. */
+ * LS_F32); pointers and strides of q and out 16-byte aligned; head_dim at most 256.  Values of LS_BF16 may be as large as the type's, and
+ * their keys as many as there may be (scores are fp32, as ever); beside an element above 2^86 one below 2^-80 may lose digits. */
 ls_status ls_kvq_attend(ls_ops* ctx, const ls_kvq_cache* cache, ls_dtype type, const ls_attend_args* a);
 
 /* Decides about drafted tokens: with p the target's probabilities, q those that drafted them and u given random numbers in [0, 1),

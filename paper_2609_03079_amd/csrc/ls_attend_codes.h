@@ -194,20 +194,27 @@ __device__ inline bool whole_pages(const AttendP& p, bool paged) {
 // loads that either side has under way.)
 template <int OWN, bool PAD, bool SECOND, typename Run>
 __device__ __forceinline__ void by_grain(const AttendP& p, bool paged, Run run) {
-    if constexpr (SECOND) return run(std::integral_constant<int, 8>{}, std::false_type{});
-    paged = whole_pages(p, paged);
-    auto by_page = [&](auto GRAIN) __attribute__((always_inline)) {
-        if (paged)
-            run(GRAIN, std::true_type{});
-        else
-            run(GRAIN, std::false_type{});
-    };
-    if (!PAD || p.D % OWN == 0)
-        by_page(std::integral_constant<int, OWN>{});
-    else if (OWN > 16 && p.D % 16 == 0)
-        by_page(std::integral_constant<int, 16>{});
-    else
-        by_page(std::integral_constant<int, 8>{});
+    if constexpr (SECOND) {
+        run(std::integral_constant<int, 8>{}, std::false_type{});
+    } else {
+        paged = whole_pages(p, paged);
+        auto by_page = [&](auto GRAIN) __attribute__((always_inline)) {
+            if (paged)
+                run(GRAIN, std::true_type{});
+            else
+                run(GRAIN, std::false_type{});
+        };
+        if constexpr (!PAD) {
+            by_page(std::integral_constant<int, OWN>{});
+        } else {
+            if (p.D % OWN == 0)
+                by_page(std::integral_constant<int, OWN>{});
+            else if (OWN > 16 && p.D % 16 == 0)
+                by_page(std::integral_constant<int, 16>{});
+            else
+                by_page(std::integral_constant<int, 8>{});
+        }
+    }
 }
 
 // Where a token's heads follow each other in a page, rows of codes and scales are smaller than the cache lines that they share: the
@@ -280,11 +287,13 @@ __device__ __forceinline__ f32x4 odd_of(const vec8<T>& v, bool second, bool seen
 constexpr int kThinPad = 8;  // elements
 
 // Up to 16 rows over codes.  Bound by memory where there are waves enough, by a wave's chain of loads, products and exponentials
-// (12 ns a key of 128) where there are few: 4 sequences of 100001 keys (32 / 8 heads of 128, FP4) take 75 us, 5.8 TB/s, 1000 keys of 32 heads
-// 5.8.  Two waves take 32 keys each in turn.  The products run on the 16 x 16 x 32 instructions, which need half the scores, sums
-// and query operands a lane that tiles of 32 rows do: 168 registers, three waves a SIMD, and in place of those tiles 8 sequences behind
-// 7901 keys 19.4 -> 17.0 us, 16 x 8 tokens of 2000 keys 35.6 -> 23.9.  A lane takes a quarter of a key's row, straight from the cache: key n of
-// the first 16 of a tile and of the second, elements g DP / 4 and on; its scores are those of keys 16 t + 4 g + i and query row n.
+// (12 ns a key of 128) where there are few: 4 sequences of 100001 keys (32 / 8 heads of 128, FP4) take 80 us with their join, 5.4 TB/s (alone,
+// 77 in the best of 30 launches and 88 in the median), 1000 keys of 32 heads 6.1 and 6.9.  Two waves take 32 keys each in turn.  The
+// products run on the 16 x 16 x 32 instructions, which need half the scores, sums and query operands a lane that tiles of 32 rows do:
+// 168 registers, three waves a SIMD, and in place of those tiles 8 sequences behind 7901 keys 19.4 -> 17.0 us, 16 x 8 tokens of 2000 keys
+// 35.6 -> 23.9.  A lane takes a quarter of a key's row, straight from the cache: key n of the first 16 of a tile and of the second,
+// elements g DP / 4 and on; its scores are those of keys 16 t + 4 g + i and query row n.
+// True: the pass has to be taken again (kTwice), lift_of_row then says with what weights this lane's row.
 template <typename T, int DP, bool MULTI, class C, bool PAD, bool SECOND>
 __device__ __forceinline__ bool attend_thin(const Pass<SECOND>& pass, bool prefix, float* lift_of_row, T* v0, float (*wave_ml)[2][32]) {
     constexpr int NW = 2, KT = 32, kStep = NW * KT, NF = DP / 32, ND = DP / 16;
@@ -549,11 +558,11 @@ __device__ __forceinline__ bool attend_thin(const Pass<SECOND>& pass, bool prefi
 constexpr int kBroadPad = 16;  // elements
 
 // Tiles of 128 query rows, 32 a wave, on the 32 x 32 x 16 instructions.  Bound by vector and matrix instructions: 64 sequences behind
-// 32768 keys (64 / 8 heads of 128, FP4) take 101 us, 680 TFLOP/s, the matrix units busy for 28 us of them and the vector units, which
-// widen codes and take 134 million exponentials, for about 45; the two seldom at once, as a wave's parts depend on each other and two waves
-// a SIMD are all that the registers hold.  Each wave widens the keys it multiplies by itself: 32 at a
-// time, a half of their row a lane, the scores of the next 32 computed while the exponentials of these are.  The values of 64 keys are
-// widened by the four waves together, 16 rows each, for all of them.
+// 32768 keys (64 / 8 heads of 128, FP4) take 108 us in the median of 30 launches, 640 TFLOP/s (102 in the best; FP8 115 and 111).  Of
+// 181 thousand clocks the matrix units are busy for 66 thousand and the vector units, which widen codes and take 134 million exponentials, for
+// about 100; the two seldom at once, as a wave's parts depend on each other and two waves a SIMD are all that the registers hold.  Each
+// wave widens the keys it multiplies by itself: 32 at a time, a half of their row a lane, the scores of the next 32 computed while the
+// exponentials of these are.  The values of 64 keys are widened by the four waves together, 16 rows each, for all of them.
 template <typename T, int DP, bool MULTI, class C, bool PAD, bool SECOND>
 __device__ __forceinline__ bool attend_broad(const Pass<SECOND>& pass, bool prefix, float* lift_of_row, T* v0, T* v1) {
     constexpr int KT = 64, NF = DP / 16, ND = DP / 32, kPitch = DP + kBroadPad, kOf8 = C::kBits / 4;
@@ -871,14 +880,16 @@ __global__ __launch_bounds__((S == THIN ? 128 : 256), (waves_of<DP, S, MULTI, C>
     __shared__ float wave_ml[2][2][32];
     auto thin = [&](int b, bool prefix) __attribute__((always_inline)) {
         float lift;
-        if (__builtin_expect((attend_thin<T, DP, MULTI, C, PAD>(first_pass(p, b), prefix, &lift, v0, wave_ml)), false))
-            attend_thin<T, DP, MULTI, C, PAD>(second_pass(b), prefix, &lift, v0, wave_ml);
+        const bool again = attend_thin<T, DP, MULTI, C, PAD>(first_pass(p, b), prefix, &lift, v0, wave_ml);
+        if constexpr (kTwice<T>)
+            if (__builtin_expect(again, false)) attend_thin<T, DP, MULTI, C, PAD>(second_pass(b), prefix, &lift, v0, wave_ml);
     };
     auto broad = [&](auto SEVERAL, int b, bool prefix) __attribute__((always_inline)) {
         constexpr bool several = decltype(SEVERAL)::value;
         float lift;
-        if (__builtin_expect((attend_broad<T, DP, several, C, PAD>(first_pass(p, b), prefix, &lift, v0, v1)), false))
-            attend_broad<T, DP, several, C, PAD>(second_pass(b), prefix, &lift, v0, v1);
+        const bool again = attend_broad<T, DP, several, C, PAD>(first_pass(p, b), prefix, &lift, v0, v1);
+        if constexpr (kTwice<T>)
+            if (__builtin_expect(again, false)) attend_broad<T, DP, several, C, PAD>(second_pass(b), prefix, &lift, v0, v1);
     };
     int b = blockIdx.x;
     if constexpr (S == BOTH) {

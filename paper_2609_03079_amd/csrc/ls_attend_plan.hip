@@ -28,7 +28,7 @@ bool plan_attend_codes(const ls_kvq_cache& c, const ls_attend_args& a, size_t ws
     const int broad_cu = dp == 64 ? 3 : dp == 128 ? 2 : 1;
     // Time of a workgroup among others on its compute unit (us): a start and an end, and the keys.  Thin: the wave's own chain and
     // the unit's share of the memory (5.3 TB/s), which overlap but for the loads that a lone wave has not in flight.  Broad: as
-    // measured with the unit full.
+    // measured with the unit full, of FP4 (FP8 takes 115 us where FP4 takes 108, a part of any length as much more).
     const double key_bytes = 2.0 * ((double)c.head_dim * bits / 8 + (double)ceil_div(c.head_dim, 32));
     auto item_us = [&](Kind kind, int64_t chunk, int64_t at_once) {
         if (kind == THIN) return 4.5 + chunk * std::hypot(0.0118 * (dp + 128) / 256, at_once * key_bytes / (5.3e6 / n_cu));

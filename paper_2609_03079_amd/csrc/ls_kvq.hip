@@ -3,8 +3,11 @@
 //
 //   top = max |x_i| of 32;  2^e the smallest power of two with top < 7 * 2^e (4 bits) or 464 * 2^e (8);  code_i = x_i / 2^e, rounded
 //
-// Bound by memory: every element is read and written once.  8192 tokens of 64 + 2 x 8 heads of 128 are written in 48 us (bf16 to FP4,
-// 6.3 TB/s), 32768 of 8 heads read in 29 (FP8 to bf16, 6.8 TB/s).  Single tokens take 3.2 and 1.9 us, three dependent loads and one.
+// Bound by memory: every element is read and written once.  8192 tokens of 64 + 2 x 8 heads of 128 are written in 49 us (bf16 to FP4,
+// 6.3 TB/s), 32768 of 8 heads read in 29 (FP8 to bf16, 6.9 TB/s).  Single tokens take 3.7 and 2.1 us, three dependent loads and one.  (Medians
+// of 30 launches.)  Where not all of a call comes in vectors of 16 bytes whose partners do too (a half-style turn of 40 of 80
+// elements, of 56 of 112) it goes element by element: 4096 tokens of 10 + 2 x 5 heads of 80 written and read take 31 us, not 18, of
+// 16 + 2 x 16 heads of 112 60, not 29.
 #include <algorithm>
 
 #include "ls_codes.h"

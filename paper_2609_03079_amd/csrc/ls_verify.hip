@@ -11,8 +11,10 @@
 // Only the row that the token comes from is read, or the two.  They are cut into parts, so that the few sequences of a step fill
 // the card: a first launch adds the parts (bound by reading them), a second finds the part that u sum(w) falls into and the
 // token in it.  With as many sequences as fill the card by themselves, or rows of up to 8192 tokens, a workgroup does both: a launch
-// less (4000 tokens 9.5 -> 7.5 us, where 16000 would go from 9.1 to 10.1).  Measured: 1 x 4 drafts of 32000 (fp32) 9.0 us, most of it
-// the two launches; 64 x 7 of 131072 20 us, of which the sums 14 (4.8 TB/s of the rows that they read).
+// less (4000 tokens 9.5 -> 7.5 us, where 16000 would go from 9.1 to 10.1).  Measured: 1 x 4 drafts of 32000 (fp32) 9.5 us, most of it
+// the two launches; 64 x 7 of 131072 20.3 us, of which the sums 14 (4.7 TB/s of the rows that they read).  Rows that do not all begin at
+// multiples of 16 bytes (an odd vocabulary) are read an element a lane, eight in flight: 64 x 7 of 131071 23.7 us, in bfloat16 18.6
+// against 17.2 of 131072.
 #include <algorithm>
 
 #include "ls_device.h"
