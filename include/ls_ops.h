@@ -184,7 +184,7 @@ ls_status ls_kv_append(ls_ops* ctx, const ls_kv_cache* cache, const ls_append_ar
  * 16-byte aligned.  1 <= n_q <= 16; prefix_len, max_len < 2^22; scale > 0.
  * Scores, the softmax's maxima and sums and the outputs are fp32; probabilities are rounded to
  * the cache's type for the product with the values (to a step of 2^-31 of the row's largest, at
- * the finest, in f16).
+ * the finest, in f16; in bf16 those below 2^-126 of it count as zero).
  * LS_E_CAPACITY if the workspace cannot hold the parts of one split
  * (n_seqs n_q n_heads 2 (head_dim + 2) floats; of more than 2^20 rows n_seqs n_q n_heads as many
  * whole sequences as 2^20 hold are taken at a time). */
